@@ -344,6 +344,137 @@ int moara_kernel_stats(moara_state* st, int32_t kernel, int64_t* out_launches, d
 /* Zero the accumulated per-kernel statistics (synchronises the stream). */
 int moara_reset_kernel_stats(moara_state* st, void* stream);
 
+/* ------------------------------------------------------------------------------------
+ * Operators of a training step beside the projected matrices' update: the norm of all
+ * gradients and their clipping (the paper clips at 1.0), AdamW for the parameters that are
+ * not projected (Appendix D), and the routing of tokens to experts, whose counts say which
+ * experts' matrices a step is for. They hold no state: every buffer is the caller's, lists
+ * travel in the kernels' arguments, nothing is allocated and nothing synchronises, so a call
+ * can be captured in a graph (its pointers and numbers are then the graph's). They act on the
+ * current device. Pointers need the alignment of their element type only; vectors are
+ * wide loads from any such address. Results do not depend on timing: the same arguments
+ * give the same bits.
+ * ------------------------------------------------------------------------------------ */
+
+/* One gradient tensor: `count` consecutive elements of type `dtype` on the GPU. A null
+ * `grad` or a count of 0 is a tensor without a gradient: skipped. */
+typedef struct {
+  void* grad;
+  int64_t count;
+  int32_t dtype;    /* MOARA_F32 or MOARA_BF16 */
+  int32_t reserved;
+} moara_grad_tensor;
+
+/* Bytes of the workspace of moara_grad_norm (device memory, 8-byte aligned). */
+#define MOARA_GRAD_NORM_WORKSPACE 16384
+
+/* out[0] = the 2-norm over all elements of all tensors, out[1] = min(1, max_norm /
+ * (out[0] + 1e-6)), the coefficient that clips them to max_norm. Squares are summed in 64
+ * bits. A norm that is not finite (or over the largest fp32) gives the coefficient NaN, on
+ * which moara_adamw_step changes nothing and moara_grad_scale clears the gradients.
+ * tensors: host array, read during the call. out: two floats of device memory.
+ * max_norm > 0 (infinity: the coefficient is 1).
+ * Errors: MOARA_E_ARG, MOARA_E_SHAPE (a count below 0 or over 2^40), MOARA_E_HIP. */
+int moara_grad_norm(const moara_grad_tensor* tensors, int32_t n, float max_norm, float* out, void* workspace,
+                    void* stream);
+
+/* Multiplies every element by *coef (device memory, e.g. out + 1 of moara_grad_norm) in
+ * place; a coefficient of 1 leaves them unread, NaN sets them to zero (moara_step on a zero
+ * gradient decays its moments). Errors as moara_grad_norm. */
+int moara_grad_scale(const moara_grad_tensor* tensors, int32_t n, const float* coef, void* stream);
+
+typedef struct {
+  double beta1, beta2;  /* in [0, 1) */
+  double eps;           /* > 0, added to the root of the second moment */
+  int32_t bits;         /* of the moments: 32, or 8 */
+  int32_t reserved;
+} moara_adamw_config;
+
+/* One parameter tensor of an AdamW step: `count` consecutive elements. */
+typedef struct {
+  void* param;            /* updated in place */
+  const void* grad;       /* null: no gradient, the tensor and its moments stay as they are */
+  void* exp_avg;          /* first and second moment: fp32, or 8-bit codes (below); zeros at the start */
+  void* exp_avg_sq;
+  void* scales;           /* 8 bits: 2 ceil(count / 32) bytes; zeros at the start. 32 bits: not read */
+  int64_t count;
+  int64_t step;           /* t >= 1: this tensor's step, counted by the caller */
+  double lr;
+  double weight_decay;    /* decoupled: p (1 - lr weight_decay) */
+  int32_t param_dtype, grad_dtype;  /* MOARA_F32 or MOARA_BF16, each on its own */
+} moara_adamw_tensor;
+
+/* beta = (0.9, 0.999), eps = 1e-6 (Appendix D), moments of 32 bits. */
+int moara_adamw_default_config(moara_adamw_config* out);
+
+/* One AdamW step over n tensors (decoupled weight decay, bias correction):
+ *   g <- clip g;  m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2;
+ *   p <- p (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),
+ * computed in fp32 whatever the types, rounded to the parameter's type (nearest even) once.
+ * clip: one float of device memory (out + 1 of moara_grad_norm) or null for 1. Where it is
+ * NaN nothing is changed (the caller's t counts that step all the same).
+ *
+ * Moments of 8 bits. The elements of a tensor are cut into blocks of 32; scales holds two
+ * bytes for each, the biased binary exponents e of the block's largest finite |m| and of its
+ * largest finite v, one more where the significand is over 1.75, at least 18 and 35.
+ *   m: E4M3 codes of m / 2^(e - 135), to nearest even; 0x7f where m is not finite.
+ *   v: unsigned E5M3 codes: the code 8 E + f stands for (8 + f) 2^(E - 1) (f where E = 0)
+ *      times 2^(e - 160); 254 is the largest, 255 NaN (v not finite). Rounded up or down at
+ *      random with v as the mean: with beta2 = 0.999 a step moves v by a few thousandths,
+ *      less than half the distance of neighbouring codes, and rounding to nearest would
+ *      leave it where it is. A v above zero never becomes 0, which would divide by eps.
+ * The random bits of element i of tensor j are a function of (seed, j, i): give every step
+ * another seed. The update of p uses the moments before their rounding.
+ * Errors: MOARA_E_ARG, MOARA_E_SHAPE (a count below 0 or over 2^40), MOARA_E_HIP. */
+int moara_adamw_step(const moara_adamw_config* cfg, const moara_adamw_tensor* tensors, int32_t n, const float* clip,
+                     uint64_t seed, void* stream);
+
+enum { MOARA_SOFTMAX = 0, MOARA_SIGMOID = 1 };
+
+typedef struct {
+  int32_t experts;        /* E, at most 1024 */
+  int32_t top_k;          /* experts of a token, at most 64 and at most those of the kept groups */
+  int32_t groups;         /* groups of E / groups consecutive experts, at most 64; 1: no groups */
+  int32_t top_groups;     /* groups a token's experts come from */
+  int32_t group_best;     /* a group counts with its best expert (1) or the sum of its two best (2) */
+  int32_t score;          /* MOARA_SOFTMAX or MOARA_SIGMOID of the logits */
+  int32_t renormalise;    /* nonzero: a token's weights are divided by their sum */
+  int32_t logits_dtype;   /* MOARA_F32 or MOARA_BF16 */
+  float scale;            /* factor on the weights */
+} moara_route_config;
+
+/* 64 experts, 6 a token, one group, softmax, no renormalisation, fp32 logits, scale 1. */
+int moara_route_default_config(moara_route_config* out);
+
+/* Routes every token to top_k experts. With s the scores of its logits and c = s + bias:
+ * the top_groups best groups by their best (or two best) c are kept, and of their experts
+ * the top_k largest c are chosen, in falling order, the lowest index first among equals. The
+ * weights are s (without the bias) of the chosen experts, over their sum if renormalise, times
+ * scale. Scores and sums are fp32 (the softmax's sum 64 bits).
+ *   logits: tokens x experts, row_stride elements from one row to the next.
+ *   bias:   experts floats, or null. -infinity takes an expert out.
+ *   mask:   tokens bytes, or null; a token with 0 is not routed.
+ *   out_index, out_weight: tokens x top_k. Index -1 and weight 0 where no expert is left to
+ *           choose: a masked token, a bias of -infinity, a score that is NaN (a softmax row
+ *           with a NaN or +infinite logit, or with none above -infinity, has no scores).
+ *   counts: experts int64, or null: the tokens each expert was given are added to them.
+ * Errors: MOARA_E_ARG, MOARA_E_SHAPE (tokens below 0, overlapping rows), MOARA_E_UNSUPPORTED
+ * (over the limits above), MOARA_E_HIP. */
+int moara_route(const moara_route_config* cfg, const void* logits, int64_t tokens, int64_t row_stride, const float* bias,
+                const uint8_t* mask, int32_t* out_index, float* out_weight, int64_t* counts, void* stream);
+
+/* Gradient of the logits (tokens x experts, contiguous, the logits' type) from that of the
+ * weights (tokens x top_k), for the logits and the indices of a moara_route call; an index
+ * outside [0, experts) has no weight. The choice itself has no gradient, nor has the bias.
+ * Errors as moara_route. */
+int moara_route_backward(const moara_route_config* cfg, const void* logits, int64_t tokens, int64_t row_stride,
+                         const int32_t* index, const float* grad_weight, void* out_grad, void* stream);
+
+/* The balancing bias's step, after the last moara_route of a training step: bias[e] moves by
+ * rate towards an even load (up where counts[e] is below their mean, down above it), and the
+ * counts are set to zero. Errors: MOARA_E_ARG, MOARA_E_HIP. */
+int moara_route_balance(int32_t experts, int64_t* counts, float* bias, float rate, void* stream);
+
 /* Number of matrices in the state and one matrix's resolved layout. */
 int moara_matrix_info(const moara_state* st, int32_t mat, int64_t* rows, int64_t* cols,
                       int32_t* rank, int32_t* side, int32_t* n_blocks);

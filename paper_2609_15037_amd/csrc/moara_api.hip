@@ -16,6 +16,7 @@
 #include "common.h"
 #include "gemm.h"
 #include "refresh.h"
+#include "train.h"
 
 
 namespace {
@@ -31,6 +32,19 @@ int fail(int code, const char* fmt, ...) {
   g_err = buf;
   return code;
 }
+
+}  // namespace
+
+int moara_fail(int code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return fail(code, "%s", buf);
+}
+
+namespace {
 
 #define HIP_TRY(expr)                                                                   \
   do {                                                                                  \

@@ -1,0 +1,69 @@
+// Operators a training step needs beside the projected matrices: gradient norm and clipping, AdamW
+// over lists of tensors, routing of tokens to experts. Lists of tensors travel in the kernels'
+// arguments (at most 4 KB), so a call needs no device descriptors, no copy and no workspace for them.
+#pragma once
+#include "common.h"
+
+// A failed call's status with its message for moara_last_error (moara_api.hip holds the message).
+__attribute__((visibility("hidden"))) int moara_fail(int code, const char* fmt, ...);
+
+// ---------------------------------------------------------------- gradient norm, clipping
+constexpr int GRAD_MAX = 160;
+struct GradList {
+  void* g[GRAD_MAX];
+  int64_t count[GRAD_MAX];
+  uint32_t start[GRAD_MAX];     // first tile
+  uint32_t bf16[(GRAD_MAX + 31) / 32];   // bit i: tensor i is bf16
+  int n;
+  uint32_t tiles;
+};
+constexpr int NORM_WGS = 2048;  // partial sums; the workspace of moara_grad_norm holds them
+uint32_t grad_tiles(int64_t count);
+// first: the partial sums are stored, else added to
+hipError_t launch_grad_norm(const GradList& l, double* partial, bool first, hipStream_t st);
+hipError_t launch_grad_norm_end(const double* partial, float max_norm, float* out, hipStream_t st);
+hipError_t launch_grad_scale(const GradList& l, const float* coef, hipStream_t st);
+
+// ---------------------------------------------------------------- AdamW
+constexpr int ADAMW_MAX = 48;
+struct AdamwTensor {
+  void* p;
+  const void* g;
+  void* m;
+  void* v;
+  uint8_t* scales;              // 8 bits: two exponents for each block of 32
+  int64_t count;
+  float decay;                  // 1 - lr weight_decay
+  float lr;                     // lr / (1 - beta1^t)
+  float rbc2;                   // 1 / (1 - beta2^t)
+  uint32_t start;               // first workgroup
+  uint32_t key0, key1;          // random bits of the 8-bit second moment
+};
+struct AdamwList {
+  AdamwTensor t[ADAMW_MAX];
+  const float* clip;
+  float b1, c1, b2, c2, eps;    // c = 1 - b
+  int n;
+};
+uint32_t adamw_tiles(int64_t count);
+hipError_t launch_adamw(const AdamwList& l, bool p_bf16, bool g_bf16, int bits, uint32_t total, hipStream_t st);
+
+// ---------------------------------------------------------------- routing to experts
+struct RouteParams {
+  const void* logits;
+  int64_t tokens, ld;           // ld: elements from one token's logits to the next one's
+  const float* bias;            // null: none
+  const uint8_t* mask;          // null: every token is routed
+  int32_t* index;
+  float* weight;                // forward: out; backward: the gradient of the weights
+  unsigned long long* counts;   // null: not wanted
+  void* grad;                   // backward: tokens x experts, type of the logits
+  int E, k, groups, top_groups, group_best;
+  uint32_t group_size, group_inv;   // group of expert e: (e * group_inv) >> 20
+  int sigmoid, renorm, bf16;
+  float scale;
+};
+constexpr int ROUTE_MAX_EXPERTS = 1024, ROUTE_MAX_K = 64, ROUTE_MAX_GROUPS = 64;
+hipError_t launch_route(const RouteParams& p, hipStream_t st);
+hipError_t launch_route_backward(const RouteParams& p, hipStream_t st);
+hipError_t launch_route_balance(int E, long long* counts, float* bias, float rate, hipStream_t st);

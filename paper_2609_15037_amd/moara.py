@@ -28,6 +28,8 @@ MOARA_F32, MOARA_BF16 = 0, 1
 MOARA_T_P, MOARA_T_EXP_AVG, MOARA_T_EXP_AVG_SQ, MOARA_T_MAG_AVG, MOARA_T_MAG_AVG_SQ, MOARA_T_STEP = range(6)
 MOARA_KERN_DECOMPOSE, MOARA_KERN_PROJECT, MOARA_KERN_BACKPROJ, MOARA_KERN_REFRESH, MOARA_KERN_ALIGN = range(5)
 MOARA_NUM_KERNELS = 5
+MOARA_SOFTMAX, MOARA_SIGMOID = 0, 1
+MOARA_GRAD_NORM_WORKSPACE = 16384
 
 EXPORTED = (
     "moara_default_config", "moara_allocate_ranks", "moara_resolve_matrix", "moara_state_bytes",
@@ -37,6 +39,8 @@ EXPORTED = (
     "moara_set_tensor", "moara_refresh_info",
     "moara_set_timing", "moara_kernel_stats", "moara_reset_kernel_stats", "moara_matrix_info",
     "moara_destroy_state", "moara_last_error", "moara_version",
+    "moara_grad_norm", "moara_grad_scale", "moara_adamw_default_config", "moara_adamw_step",
+    "moara_route_default_config", "moara_route", "moara_route_backward", "moara_route_balance",
 )
 
 
@@ -68,6 +72,29 @@ class moara_matrix_desc(ctypes.Structure):
         ("module", ctypes.c_int32), ("rank_override", ctypes.c_int32),
         ("side", ctypes.c_int32), ("reserved", ctypes.c_int32),
     ]
+
+
+class moara_grad_tensor(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("count", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class moara_adamw_config(ctypes.Structure):
+    _fields_ = [("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("bits", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class moara_adamw_tensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("exp_avg", ctypes.c_void_p),
+                ("exp_avg_sq", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("count", ctypes.c_int64),
+                ("step", ctypes.c_int64), ("lr", ctypes.c_double), ("weight_decay", ctypes.c_double),
+                ("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32)]
+
+
+class moara_route_config(ctypes.Structure):
+    _fields_ = [("experts", ctypes.c_int32), ("top_k", ctypes.c_int32), ("groups", ctypes.c_int32),
+                ("top_groups", ctypes.c_int32), ("group_best", ctypes.c_int32), ("score", ctypes.c_int32),
+                ("renormalise", ctypes.c_int32), ("logits_dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 _lib = None
@@ -106,6 +133,15 @@ def lib():
         "moara_destroy_state": (None, [vp]),
         "moara_last_error": (ctypes.c_char_p, []),
         "moara_version": (ctypes.c_char_p, []),
+        # lists of tensors travel as the address of a NumPy array of the structure
+        "moara_grad_norm": (ctypes.c_int, [vp, i32, ctypes.c_float, vp, vp, vp]),
+        "moara_grad_scale": (ctypes.c_int, [vp, i32, vp, vp]),
+        "moara_adamw_default_config": (ctypes.c_int, [P(moara_adamw_config)]),
+        "moara_adamw_step": (ctypes.c_int, [P(moara_adamw_config), vp, i32, vp, ctypes.c_uint64, vp]),
+        "moara_route_default_config": (ctypes.c_int, [P(moara_route_config)]),
+        "moara_route": (ctypes.c_int, [P(moara_route_config), vp, i64, i64, vp, vp, vp, vp, vp, vp]),
+        "moara_route_backward": (ctypes.c_int, [P(moara_route_config), vp, i64, i64, vp, vp, vp, vp]),
+        "moara_route_balance": (ctypes.c_int, [i32, vp, vp, ctypes.c_float, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -391,3 +427,244 @@ def moara_matrix_info(st: State, mat: int):
     _check(lib().moara_matrix_info(st.handle, int(mat), ctypes.byref(a), ctypes.byref(b), ctypes.byref(r),
                                    ctypes.byref(s), ctypes.byref(k)))
     return a.value, b.value, r.value, s.value, k.value
+
+
+# ---------------------------------------------------------------- gradient norm, clipping, AdamW, routing
+
+_RECORDS = {t: np.dtype(t) for t in (moara_grad_tensor, moara_adamw_tensor)}
+
+
+def _dtype_id(t, what: str) -> int:
+    import torch
+    if t.dtype == torch.float32:
+        return MOARA_F32
+    if t.dtype == torch.bfloat16:
+        return MOARA_BF16
+    raise ValueError(f"{what}: need float32 or bfloat16, got {t.dtype}")
+
+
+def _dense(t) -> bool:
+    """Whether the elements fill the tensor's memory without gaps, in whatever order of the axes."""
+    if t.is_contiguous():
+        return True
+    order = sorted((s, i) for i, s in enumerate(t.stride()))
+    return t.permute([i for _, i in reversed(order)]).is_contiguous()
+
+
+def _on_gpu(t, device: Optional[int], what: str) -> int:
+    import torch
+    if t.layout != torch.strided or not t.is_cuda:
+        raise ValueError(f"{what}: need a strided CUDA tensor, got {t.layout} on {t.device}")
+    if device is not None and t.get_device() != device:
+        raise ValueError(f"{what} is on {t.device}, the others are on cuda:{device}")
+    return t.get_device()
+
+
+def _vector(t, device, dtype, count, what: str) -> int:
+    """Address of a contiguous tensor of that type and element count."""
+    _on_gpu(t, device, what)
+    if t.dtype != dtype or t.numel() != count or not t.is_contiguous():
+        raise ValueError(f"{what}: need {count} contiguous elements of {dtype}, got {tuple(t.shape)} {t.dtype} "
+                         f"contiguous={t.is_contiguous()}")
+    return t.data_ptr()
+
+
+def _call(device: Optional[int], stream, fn, *args):
+    """fn(*args, stream) with the tensors' device current; stream None: the device's current torch stream."""
+    import torch
+    if device is None or device == torch.cuda.current_device():
+        s = _stream_ptr(torch.cuda.current_stream() if stream is None else stream)
+        _check(fn(*args, s))
+    else:
+        with torch.cuda.device(device):
+            s = _stream_ptr(torch.cuda.current_stream() if stream is None else stream)
+            _check(fn(*args, s))
+
+
+class GradArgs:
+    """The marshalled list of gradient tensors for moara_grad_norm and moara_grad_scale, checked once:
+    float32 or bfloat16 without gaps; None where a parameter has no gradient. Holds the tensors and
+    the norm's workspace. Calls that share it run on one stream, or in an order the caller keeps."""
+
+    def __init__(self, grads):
+        import torch
+        self.keep = [g for g in grads if g is not None]
+        self.device = None
+        self.rec = np.zeros(len(self.keep), dtype=_RECORDS[moara_grad_tensor])
+        rows = []
+        for i, g in enumerate(self.keep):
+            self.device = _on_gpu(g, self.device, f"grads[{i}]")
+            if not _dense(g):
+                raise ValueError(f"grads[{i}]: strides {g.stride()} of shape {tuple(g.shape)} leave gaps")
+            rows.append((g.data_ptr(), g.numel(), _dtype_id(g, f"grads[{i}]"), 0))
+        if rows:
+            self.rec[:] = rows
+        self.ptr, self.n = self.rec.ctypes.data, len(rows)
+        where = torch.cuda.current_device() if self.device is None else self.device
+        self.workspace = torch.empty(MOARA_GRAD_NORM_WORKSPACE, dtype=torch.uint8, device=f"cuda:{where}")
+
+
+def moara_grad_norm(grads, max_norm: float, out=None, stream=None, args: Optional[GradArgs] = None):
+    """moara_grad_norm of the C ABI: a float32 tensor of the norm over all gradients and of the
+    coefficient that clips them to max_norm (nothing is copied to the host). With `args` (a GradArgs
+    of the same tensors) `grads` is ignored."""
+    import torch
+    a = GradArgs(grads) if args is None else args
+    if out is None:
+        out = torch.empty(2, dtype=torch.float32, device=a.workspace.device)
+    _call(a.workspace.get_device(), stream, lib().moara_grad_norm, a.ptr, a.n, float(max_norm),
+          _vector(out, a.workspace.get_device(), torch.float32, 2, "out"), a.workspace.data_ptr())
+    return out
+
+
+def moara_grad_scale(grads, coef, stream=None, args: Optional[GradArgs] = None):
+    """moara_grad_scale of the C ABI: the gradients times coef (a float32 tensor of one element on the
+    GPU), in place."""
+    import torch
+    a = GradArgs(grads) if args is None else args
+    _call(a.workspace.get_device(), stream, lib().moara_grad_scale, a.ptr, a.n,
+          _vector(coef, a.workspace.get_device(), torch.float32, 1, "coef"))
+
+
+def moara_adamw_default_config(**overrides) -> moara_adamw_config:
+    c = moara_adamw_config()
+    _check(lib().moara_adamw_default_config(ctypes.byref(c)))
+    for k, v in overrides.items():
+        setattr(c, k, v)
+    return c
+
+
+MOARA_ADAMW_BLOCK = 32
+
+
+def moara_adamw_state(param, bits: int):
+    """The moments of a parameter at the start: (exp_avg, exp_avg_sq, scales), flat and zero; float32 with
+    scales None for 32 bits, uint8 codes for 8."""
+    import torch
+    if bits not in (8, 32):
+        raise ValueError(f"moments of {bits} bits (8 or 32)")
+    n = param.numel()
+    z = lambda k, t: torch.zeros(k, dtype=t, device=param.device)
+    if bits == 32:
+        return z(n, torch.float32), z(n, torch.float32), None
+    return z(n, torch.uint8), z(n, torch.uint8), z(2 * -(-n // MOARA_ADAMW_BLOCK), torch.uint8)
+
+
+class AdamWArgs:
+    """The marshalled tensors of moara_adamw_step, checked once: parameters and gradients float32 or
+    bfloat16 without gaps and of the same strides, moments as moara_adamw_state gives them (of any
+    shape with the parameter's element count), `scales` a list for moments of 8 bits. A gradient may be
+    None (its tensor is not stepped). weight_decay: one number or one for each tensor."""
+
+    def __init__(self, params, grads, exp_avgs, exp_avg_sqs, scales=None, weight_decay=0.0):
+        import torch
+        n = len(params)
+        if any(len(x) != n for x in (grads, exp_avgs, exp_avg_sqs)) or (scales is not None and len(scales) != n):
+            raise ValueError("one gradient, one pair of moments and one scales tensor for each parameter")
+        self.bits = 32 if scales is None else 8
+        self.keep = (list(params), list(exp_avgs), list(exp_avg_sqs), None if scales is None else list(scales))
+        self.device = None
+        self.rec = np.zeros(n, dtype=_RECORDS[moara_adamw_tensor])
+        mdt = torch.float32 if scales is None else torch.uint8
+        for i, p in enumerate(params):
+            self.device = dev = _on_gpu(p, self.device, f"params[{i}]")
+            if not _dense(p):
+                raise ValueError(f"params[{i}]: strides {p.stride()} of shape {tuple(p.shape)} leave gaps")
+            k = p.numel()
+            r = self.rec[i]
+            r["param"], r["count"], r["param_dtype"] = p.data_ptr(), k, _dtype_id(p, f"params[{i}]")
+            r["exp_avg"] = _vector(exp_avgs[i], dev, mdt, k, f"exp_avgs[{i}]")
+            r["exp_avg_sq"] = _vector(exp_avg_sqs[i], dev, mdt, k, f"exp_avg_sqs[{i}]")
+            if scales is not None:
+                r["scales"] = _vector(scales[i], dev, mdt, 2 * -(-k // MOARA_ADAMW_BLOCK), f"scales[{i}]")
+        if len({int(a) for a, k in zip(self.rec["param"], self.rec["count"]) if k}) < sum(self.rec["count"] > 0):
+            raise ValueError("a parameter occurs twice")
+        self.rec["weight_decay"] = weight_decay
+        self.set_grads(grads)
+        self.ptr, self.n = self.rec.ctypes.data, n
+
+    def set_grads(self, grads):
+        """Other gradient tensors for the same parameters."""
+        ptrs, types = [], []
+        for i, (p, g) in enumerate(zip(self.keep[0], grads)):
+            if g is None:
+                ptrs.append(0)
+                types.append(MOARA_F32)
+                continue
+            _on_gpu(g, self.device, f"grads[{i}]")
+            if g.shape != p.shape or (g.stride() != p.stride() and not (g.is_contiguous() and p.is_contiguous())):
+                raise ValueError(f"grads[{i}]: shape {tuple(g.shape)}, strides {g.stride()}; the parameter's are "
+                                 f"{tuple(p.shape)}, {p.stride()}")
+            ptrs.append(g.data_ptr())
+            types.append(_dtype_id(g, f"grads[{i}]"))
+        self.grads = list(grads)
+        self.rec["grad"], self.rec["grad_dtype"] = ptrs, types
+
+
+def moara_adamw_step(args: AdamWArgs, cfg: moara_adamw_config, lr, step, clip=None, seed: int = 0, stream=None):
+    """moara_adamw_step of the C ABI on the tensors of `args`. lr and step (t >= 1): one number or one for
+    each tensor. clip: a float32 tensor of one element on the GPU, e.g. moara_grad_norm(...)[1:]."""
+    import torch
+    if cfg.bits != args.bits:
+        raise ValueError(f"moments of {args.bits} bits, configuration of {cfg.bits}")
+    args.rec["lr"] = lr
+    args.rec["step"] = step
+    c = None if clip is None else _vector(clip, args.device, torch.float32, 1, "clip")
+    _call(args.device, stream, lib().moara_adamw_step, ctypes.byref(cfg), args.ptr, args.n, c, seed & (2 ** 64 - 1))
+
+
+def moara_route_default_config(**overrides) -> moara_route_config:
+    c = moara_route_config()
+    _check(lib().moara_route_default_config(ctypes.byref(c)))
+    for k, v in overrides.items():
+        setattr(c, k, v)
+    return c
+
+
+def _route_logits(cfg, logits):
+    dev = _on_gpu(logits, None, "logits")
+    if logits.dim() != 2 or logits.shape[1] != cfg.experts or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError(f"logits: need tokens x {cfg.experts} with unit stride along the experts, got "
+                         f"{tuple(logits.shape)}, strides {logits.stride()}")
+    cfg.logits_dtype = _dtype_id(logits, "logits")
+    tokens = logits.shape[0]
+    return dev, tokens, (logits.stride(0) if tokens > 1 else cfg.experts)
+
+
+def moara_route(cfg: moara_route_config, logits, bias=None, mask=None, counts=None, stream=None):
+    """moara_route of the C ABI: (index int32, weight float32), both tokens x top_k. logits: tokens x experts,
+    float32 or bfloat16, rows any distance apart (cfg.logits_dtype follows). bias: float32, one for each
+    expert; mask: bool or uint8, one for each token; counts: int64, one for each expert, added to."""
+    import torch
+    dev, tokens, ld = _route_logits(cfg, logits)
+    if mask is not None and mask.dtype != torch.uint8:
+        mask = mask.view(torch.uint8) if mask.dtype == torch.bool else mask
+    b = None if bias is None else _vector(bias, dev, torch.float32, cfg.experts, "bias")
+    m = None if mask is None else _vector(mask, dev, torch.uint8, tokens, "mask")
+    c = None if counts is None else _vector(counts, dev, torch.int64, cfg.experts, "counts")
+    index = torch.empty((tokens, cfg.top_k), dtype=torch.int32, device=logits.device)
+    weight = torch.empty((tokens, cfg.top_k), dtype=torch.float32, device=logits.device)
+    _call(dev, stream, lib().moara_route, ctypes.byref(cfg), logits.data_ptr(), tokens, ld, b, m, index.data_ptr(),
+          weight.data_ptr(), c)
+    return index, weight
+
+
+def moara_route_backward(cfg: moara_route_config, logits, index, grad_weight, stream=None):
+    """moara_route_backward of the C ABI: the gradient of the logits, contiguous, of their type. index: as
+    moara_route gave it; grad_weight: float32, tokens x top_k."""
+    import torch
+    dev, tokens, ld = _route_logits(cfg, logits)
+    i = _vector(index, dev, torch.int32, tokens * cfg.top_k, "index")
+    w = _vector(grad_weight, dev, torch.float32, tokens * cfg.top_k, "grad_weight")
+    grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    _call(dev, stream, lib().moara_route_backward, ctypes.byref(cfg), logits.data_ptr(), tokens, ld, i, w, grad.data_ptr())
+    return grad
+
+
+def moara_route_balance(counts, bias, rate: float, stream=None):
+    """moara_route_balance of the C ABI: one step of the balancing bias, in place; the counts end at zero."""
+    import torch
+    dev = _on_gpu(counts, None, "counts")
+    n = counts.numel()
+    c = _vector(counts, dev, torch.int64, n, "counts")
+    _call(dev, stream, lib().moara_route_balance, n, c, _vector(bias, dev, torch.float32, n, "bias"), float(rate))
