@@ -1,5 +1,7 @@
 // Routing of tokens to experts: scores, selection (groups, top-k), weights, their gradient, and the step
 // of the balancing bias.
+#include <float.h>
+
 #include "train.h"
 
 namespace {
@@ -124,16 +126,14 @@ template <int LANES, int V> __device__ __forceinline__ Row softmax_row(const flo
 }
 
 // u_j of the chosen experts, one a lane (lanes without one: there = false): the score itself, or its share
-// of the chosen ones' sum. Softmax shares come from the logits, so that they exist where scores underflow.
+// of the chosen ones' sum, from the logits less their largest, so that shares exist where scores underflow
+// (the sigmoid as exp(min(l, 0)) / (1 + exp(-|l|))). No share where every chosen logit is -inf.
 template <int LANES> __device__ __forceinline__ float chosen_share(float l, bool there, const Row& r, const RouteParams& p) {
   if (!p.renorm) return there ? score(l, r, p.sigmoid) : 0.f;
-  float u;
-  if (p.sigmoid) {
-    u = there ? score(l, r, 1) : 0.f;
-  } else {
-    const float top = max_of<LANES>(there ? l : -__builtin_inff());
-    u = there ? expf(l - top) : 0.f;
-  }
+  const float x = p.sigmoid ? fminf(l, 0.f) : l;
+  const float top = max_of<LANES>(there ? x : -FLT_MAX);
+  float u = there ? expf(x - fmaxf(top, -FLT_MAX)) : 0.f;
+  if (p.sigmoid) u /= 1.f + expf(-fabsf(l));
   const float total = sum_of<LANES>(u);
   return total > 0.f ? u / total : 0.f;
 }

@@ -1,0 +1,664 @@
+"""The operators beside the projected update on the GPU, against the 64-bit oracle."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import train_oracle as O
+from tests.harness import have_gpu, rng
+
+pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not have_gpu(), reason="needs an MI355X GPU")]
+
+F32, BF16 = torch.float32, torch.bfloat16
+EPS32 = 2.0 ** -24          # unit roundoff of fp32
+
+
+def _M():
+    from paper_2609_15037_amd import moara as M
+    return M
+
+
+def _views(arrays, dtype, gap):
+    """The arrays in one buffer, `gap` sentinel elements before each and after the last: (buffer, views, check),
+    check() says whether the sentinels are as they were."""
+    mark = 171 if dtype == torch.uint8 else 123.0
+    total = sum(a.size for a in arrays) + gap * (len(arrays) + 1)
+    buf = torch.full((total,), mark, dtype=dtype, device="cuda")
+    views, at, guard = [], gap, torch.ones(total, dtype=torch.bool, device="cuda")
+    for a in arrays:
+        v = buf[at:at + a.size]
+        v.copy_(torch.from_numpy(np.ascontiguousarray(a)).to("cuda").to(dtype))
+        guard[at:at + a.size] = False
+        views.append(v)
+        at += a.size + gap
+    return buf, views, lambda: bool((buf[guard] == mark).all())
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy() if t.is_floating_point() else t.cpu().numpy()
+
+
+SIZES = [1, 2, 7, 8, 9, 31, 32, 33, 63, 65, 2047, 2048, 2049, 8191, 8192, 8193, 20001]
+
+
+# ---------------------------------------------------------------- norm and clipping
+
+# rounding of the norm to fp32 and of the coefficient's two operations
+NORM_TOL = 4 * EPS32
+
+
+@pytest.mark.parametrize("gap", [0, 1, 8])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "mixed"])
+def test_norm_and_clip_over_lists_of_every_size(kind, gap):
+    M = _M()
+    sizes = SIZES + [0, 3] * 90                     # more tensors than one launch takes
+    g = rng(1, gap)
+    arrays = [np.float32(0.01 * (i + 1) * g.standard_normal(n)) for i, n in enumerate(sizes)]
+    types = [F32 if kind == "f32" or (kind == "mixed" and i % 2) else BF16 for i in range(len(sizes))]
+    checks, views = [], [None] * len(sizes)
+    for dt in (F32, BF16):
+        at = [i for i, t in enumerate(types) if t == dt]
+        if at:
+            _, v, c = _views([arrays[i] for i in at], dt, gap)
+            checks.append(c)
+            for i, x in zip(at, v):
+                views[i] = x
+    before = [_np(v) for v in views]
+    norm, coef = O.grad_norm(before, 1.0)
+    assert coef < 0.5
+    out = M.moara_grad_norm(views, 1.0)
+    np.testing.assert_allclose(_np(out), [norm, coef], rtol=NORM_TOL)
+    again = M.moara_grad_norm(views, 1.0)
+    assert torch.equal(out, again)
+    assert float(M.moara_grad_norm(views, math.inf)[1]) == 1.0
+    M.moara_grad_scale(views, out[1:])
+    c = np.float32(float(out[1]))
+    for v, b, t in zip(views, before, types):
+        want = torch.from_numpy(b.astype(np.float32) * c).to(t)     # one product, rounded once to the type
+        if t == F32:
+            assert torch.equal(v.cpu(), want)
+        else:       # the product rounds to fp32 first
+            assert torch.equal(v.cpu(), want)
+    assert all(f() for f in checks)
+    M.moara_grad_scale(views, torch.ones(1, device="cuda"))
+    assert all(torch.equal(v.cpu(), torch.from_numpy(b.astype(np.float32) * c).to(t)) for v, b, t in
+               zip(views, before, types))
+
+
+@pytest.mark.parametrize("big", [1e30, 1e-30, 3e-42])
+def test_norm_where_squares_leave_fp32(big):
+    M = _M()
+    a = np.float32(big) * np.ones(5000, np.float32)
+    out = _np(M.moara_grad_norm([torch.from_numpy(a).cuda()], 1.0))
+    norm, coef = O.grad_norm([a], 1.0)
+    np.testing.assert_allclose(out, [norm, coef], rtol=NORM_TOL, atol=2.0 ** -150)
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_norm_that_is_not_finite_clears_gradients(bad, dtype):
+    M = _M()
+    x = torch.randn(3000, device="cuda").to(dtype)
+    x[1234] = bad
+    y = torch.randn(17, device="cuda")
+    out = M.moara_grad_norm([x, y], 1.0)
+    assert not math.isfinite(float(out[0])) and math.isnan(float(out[1]))
+    M.moara_grad_scale([x, y], out[1:])
+    assert not x.any() and not y.any()
+
+
+def test_norm_of_nothing():
+    M = _M()
+    for grads in ([], [None], [torch.empty(0, device="cuda")], [torch.zeros(5, device="cuda")]):
+        assert M.moara_grad_norm(grads, 1.0).tolist() == [0.0, 1.0]
+        M.moara_grad_scale(grads, torch.ones(1, device="cuda"))
+
+
+def test_norm_of_transposed_gradients_and_refusal_of_gaps():
+    M = _M()
+    x = torch.randn(40, 50, device="cuda")
+    assert torch.equal(M.moara_grad_norm([x.t()], 1.0), M.moara_grad_norm([x], 1.0))
+    for bad in (x[:, :7], x[::2], x.double(), x.cpu(), x.half()):
+        with pytest.raises(ValueError):
+            M.moara_grad_norm([bad], 1.0)
+
+
+# ---------------------------------------------------------------- AdamW
+
+HYPER = dict(beta1=0.875, beta2=1 - 2.0 ** -10, eps=2.0 ** -20)     # exact in fp32
+LR, DECAY = 2.0 ** -7, 0.125
+
+
+def _inputs(sizes, seed, zeros=False):
+    g = rng(seed, 3)
+    p = [np.float32(0.02 * g.standard_normal(n)) for n in sizes]
+    gr = [np.float32(1e-3 * g.standard_normal(n) * np.exp(g.standard_normal(n))) for n in sizes]
+    m = [np.float32(0 if zeros else 3e-4) * np.float32(g.standard_normal(n)) for n in sizes]
+    v = [np.float32(0 if zeros else 1e-6) * np.float32(0.5 + g.random(n)) for n in sizes]
+    return p, gr, m, v
+
+
+def _bf16(x):
+    return torch.from_numpy(np.asarray(x, np.float64)).to(BF16).double().numpy()
+
+
+def _check_param(got, want, before, dtype):
+    """fp32: the update's own error, a few roundings of quotients and roots, and the result's rounding;
+    bf16: that rounding, to nearest, besides."""
+    tol = 8 * EPS32 * np.abs(want - before) + 3 * EPS32 * np.abs(want) + 2.0 ** -149
+    if dtype == BF16:
+        tol = tol + 2.0 ** -8 * np.abs(want)       # half a unit of 8 bits is at most 2^-8 of the value
+    assert np.all(np.abs(got - want) <= tol), float(np.max(np.abs(got - want) / tol))
+
+
+@pytest.mark.parametrize("gap", [0, 1, 3])
+@pytest.mark.parametrize("pt,gt", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
+def test_adamw_32_bits_over_a_list_of_every_size(pt, gt, gap):
+    M = _M()
+    sizes = SIZES + [5, 0] * 20                     # more tensors than one launch takes
+    P, G, Mo, V = _inputs(sizes, 11 + gap)
+    bufs = [_views(x, t, gap) for x, t in ((P, pt), (G, gt), (Mo, F32), (V, F32))]
+    p, g, m, v = (b[1] for b in bufs)
+    before = [[_np(x) for x in y] for y in (p, g, m, v)]
+    steps = [1 + 7 * (i % 3) for i in range(len(sizes))]
+    clip = torch.tensor([0.375], device="cuda")
+    grads = [None if i == 4 else x for i, x in enumerate(g)]
+    args = M.AdamWArgs(p, grads, m, v, weight_decay=[DECAY * (i % 2) for i in range(len(sizes))])
+    M.moara_adamw_step(args, M.moara_adamw_default_config(**HYPER), LR, steps, clip=clip)
+    for i, n in enumerate(sizes):
+        b = [x[i] for x in before]
+        if i == 4:
+            assert all(np.array_equal(_np(x[i]), y) for x, y in zip((p, g, m, v), b))
+            continue
+        m1, v1 = O.moments(0.375 * b[1], b[2], b[3], HYPER["beta1"], HYPER["beta2"])
+        want = O.adamw_param(b[0], m1, v1, steps[i], LR, decay=DECAY * (i % 2), **HYPER)
+        # two products and a sum of terms that may cancel: roundings relative to the terms
+        np.testing.assert_array_less(np.abs(_np(m[i]) - m1), 3 * EPS32 * (np.abs(b[2]) + np.abs(b[1])) + 2.0 ** -149)
+        np.testing.assert_array_less(np.abs(_np(v[i]) - v1), 4 * EPS32 * v1 + 2.0 ** -149)
+        d = np.abs(_np(m[i]) - m1) / np.maximum(np.abs(m1), 1e-30) * np.abs(want - b[0])   # m's error in the update
+        _check_param(_np(p[i]) - np.clip(_np(p[i]) - want, -d, d), want, b[0], pt)
+    assert all(b[2]() for b in bufs)
+
+
+def test_adamw_matches_torch_over_several_steps():
+    M = _M()
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = [torch.randn(s, generator=g, device="cuda") for s in ((300, 40), (40,), (1,))]
+    ref = [torch.nn.Parameter(t.clone()) for t in x]
+    opt = torch.optim.AdamW(ref, lr=1e-2, betas=(0.9, 0.999), eps=1e-6, weight_decay=0.1)
+    state = [M.moara_adamw_state(t, 32) for t in x]
+    cfg = M.moara_adamw_default_config()
+    args = M.AdamWArgs(x, [None] * 3, [s[0] for s in state], [s[1] for s in state], weight_decay=0.1)
+    for step in range(1, 11):
+        grads = [torch.randn(t.shape, generator=g, device="cuda") for t in x]
+        for r, gr in zip(ref, grads):
+            r.grad = gr
+        opt.step()
+        args.set_grads(grads)
+        M.moara_adamw_step(args, cfg, 1e-2, step)
+    for a, b in zip(x, ref):        # ten updates of about 1e-2, each with the roundings of a few operations
+        torch.testing.assert_close(a, b.detach(), rtol=2e-6, atol=2e-6)
+
+
+def _codes_agree(got, want, n, what):
+    """fp32 and fp64 round alike except where the value lies within the fp32 error (2^-22 of it) of a
+    boundary between codes (at least 2^-4 of it apart): neighbours, and rarely."""
+    off = np.abs(got.astype(int) - want.astype(int))
+    assert off.max(initial=0) <= 1, what
+    assert off.sum() <= 3 + 16 * n * 2.0 ** -17, (what, int(off.sum()))
+
+
+@pytest.mark.parametrize("gap", [0, 1, 3])
+@pytest.mark.parametrize("pt,gt,zeros", [(F32, F32, False), (F32, BF16, True), (BF16, F32, True), (BF16, BF16, False)])
+def test_adamw_8_bits_over_a_list_of_every_size(pt, gt, zeros, gap):
+    M = _M()
+    sizes = SIZES + [5, 0] * 20
+    P, G, Mo, V = _inputs(sizes, 21 + gap, zeros)
+    seed = 0x1234567890ABCDEF
+    em = [O.block_exponents(x, 18) for x in Mo]
+    ev = [O.block_exponents(x, 35) for x in V]
+    if zeros:       # the state as it is allocated
+        em, ev = [0 * e for e in em], [0 * e for e in ev]
+    mc = [np.zeros(n, np.uint8) if zeros else O.encode_m(x, e) for x, e, n in zip(Mo, em, sizes)]
+    vc = [np.zeros(n, np.uint8) if zeros else O.encode_v(x, e, O.random16(0, n, 5, 0)) for x, e, n in zip(V, ev, sizes)]
+    sc = [np.stack([a, b], 1).astype(np.uint8).reshape(-1) for a, b in zip(em, ev)]
+    bufs = [_views(x, t, gap) for x, t in ((P, pt), (G, gt), (mc, torch.uint8), (vc, torch.uint8), (sc, torch.uint8))]
+    p, g, m, v, s = (b[1] for b in bufs)
+    before = [[_np(x) for x in y] for y in (p, g)]
+    args = M.AdamWArgs(p, g, m, v, s, weight_decay=DECAY)
+    M.moara_adamw_step(args, M.moara_adamw_default_config(bits=8, **HYPER), LR, 3, seed=seed)
+    for i, n in enumerate(sizes):
+        m0 = O.decode_m(mc[i], np.maximum(em[i], 18))
+        v0 = O.decode_v(vc[i], ev[i])
+        gi = before[1][i]
+        m1, v1 = O.moments(gi, m0, v0, HYPER["beta1"], HYPER["beta2"])
+        want = O.adamw_param(before[0][i], m1, v1, 3, LR, decay=DECAY, **HYPER)
+        d = 3 * EPS32 * (np.abs(m0) + np.abs(gi)) / np.maximum(np.abs(m1), 1e-30) * np.abs(want - before[0][i])
+        _check_param(_np(p[i]) - np.clip(_np(p[i]) - want, -d, d), want, before[0][i], pt)
+        em1, ev1 = O.block_exponents(m1, 18), O.block_exponents(v1, 35)
+        got = s[i].cpu().numpy().reshape(-1, 2)
+        # an exponent differs where the largest value is within rounding of 1.75 2^e: none of these inputs
+        assert np.array_equal(got[:, 0], em1) and np.array_equal(got[:, 1], ev1), i
+        _codes_agree(m[i].cpu().numpy(), O.encode_m(m1, em1), n, "m")
+        _codes_agree(v[i].cpu().numpy(), O.encode_v(v1, ev1, O.random16(0, n, seed, i)), n, "v")
+    assert all(b[2]() for b in bufs)
+
+
+def _step8(g, m=None, v=None, seed=0, hyper=HYPER, t=1):
+    """One 8-bit step from zero (or given) state of one fp32 tensor: (param, m codes, v codes, scales)."""
+    M = _M()
+    x = torch.from_numpy(np.asarray(g, np.float32)).cuda()
+    p = torch.zeros_like(x)
+    mm, vv, ss = M.moara_adamw_state(x, 8)
+    if m is not None:
+        em, ev = O.block_exponents(m, 18), O.block_exponents(v, 35)
+        mm.copy_(torch.from_numpy(O.encode_m(m, em)))
+        vv.copy_(torch.from_numpy(O.encode_v(v, ev, np.full(v.size, 32768))))
+        ss.copy_(torch.from_numpy(np.stack([em, ev], 1).astype(np.uint8).reshape(-1)))
+    M.moara_adamw_step(M.AdamWArgs([p], [x], [mm], [vv], [ss]), M.moara_adamw_default_config(bits=8, **hyper), 0.5, t,
+                       seed=seed)
+    return p.cpu().numpy(), mm.cpu().numpy(), vv.cpu().numpy(), ss.cpu().numpy().reshape(-1, 2)
+
+
+def test_adamw_8_bits_every_magnitude_fp32_has():
+    """Blocks from the smallest to the largest gradients: exponents at both ends of their range."""
+    g = np.zeros((42, 32), np.float32)
+    for i in range(42):
+        g[i] = np.float32(10.0) ** np.float32(i - 22) * (1 + np.arange(32, dtype=np.float32) / 32)
+    g = g.reshape(-1)
+    p, m, v, s = _step8(g, hyper=dict(beta1=0.5, beta2=0.5, eps=1e-30))
+    m1, v1 = np.float64(g) / 2, np.float64(np.float32(np.float32(g) * np.float32(g))) / 2   # v as fp32 holds it
+    em, ev = O.block_exponents(m1, 18), O.block_exponents(v1, 35)
+    assert np.array_equal(s[:, 0], em) and np.array_equal(s[:, 1], ev)
+    _codes_agree(m, O.encode_m(m1, em), g.size, "m")
+    _codes_agree(v, O.encode_v(v1, ev, O.random16(0, g.size, 0, 0)), g.size, "v")
+    back = O.decode_v(v, s[:, 1].astype(int))
+    assert np.all(back[(v1 > 0) & np.isfinite(v1)] > 0)
+    fine = (v1 > 1e-30) & (v1 < 1e38)
+    assert np.all(np.abs(back[fine] / v1[fine] - 1) <= 0.125)
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_adamw_8_bits_values_that_are_not_finite_stay_in_their_place(bad):
+    g = np.float32(rng(3, 1).standard_normal(100))
+    clean = _step8(g)
+    h = g.copy()
+    h[[0, 37, 99]] = bad
+    p, m, v, s = _step8(h)
+    at = np.zeros(100, bool)
+    at[[0, 37, 99]] = True
+    assert np.all(m[at] == 0x7F) and np.all(v[at] == 255) and np.all(np.isnan(p[at]))
+    keep = ~at & (s == clean[3]).all(axis=1).repeat(32)[:100]       # in blocks that kept their exponents
+    assert np.array_equal(p[~at], clean[0][~at])
+    assert np.array_equal(m[keep], clean[1][keep]) and np.array_equal(v[keep], clean[2][keep])
+    # and stay there at the next step, whose gradient is finite
+    em, ev = s[:, 0].astype(int), s[:, 1].astype(int)
+    M = _M()
+    x, pp = torch.from_numpy(g).cuda(), torch.zeros(100, device="cuda")
+    mm, vv, ss = (torch.from_numpy(np.ascontiguousarray(a)).cuda() for a in (m, v, s.reshape(-1)))
+    M.moara_adamw_step(M.AdamWArgs([pp], [x], [mm], [vv], [ss]), M.moara_adamw_default_config(bits=8, **HYPER), 0.5, 2)
+    assert np.all(mm.cpu().numpy()[at] == 0x7F) and np.all(vv.cpu().numpy()[at] == 255)
+    assert np.all(np.isfinite(pp.cpu().numpy()[~at])) and np.all(np.isnan(pp.cpu().numpy()[at]))
+
+
+def test_adamw_8_bits_wide_blocks_never_store_a_positive_square_as_zero():
+    g = np.full(64, 1e-8, np.float32)
+    g[0], g[40] = 1e4, 1e2
+    p, m, v, s = _step8(g)
+    assert np.all(v > 0)
+    assert np.all(np.abs(p) <= 0.5 * 1.001)
+
+
+def test_adamw_8_bits_second_moment_keeps_its_mean():
+    """Over many seeds the decoded second moment has the exact one as its mean: a stored value is off by at most
+    a spacing d (1/8 of it at most, uniform weights give a variance up to d^2 / 4)."""
+    n, seeds = 4096, 64
+    g0 = rng(9, 2)
+    g = np.float32(1e-3 * g0.standard_normal(n))
+    v = 1e-6 * (0.5 + g0.random(n))
+    total = np.zeros(n)
+    for seed in range(seeds):
+        _, _, vc, s = _step8(g, np.zeros(n), v, seed=seed * 0x9E3779B97F4A7C15 % 2 ** 64, t=100)
+        total += O.decode_v(vc, s[:, 1].astype(int))
+    start = O.decode_v(O.encode_v(v, O.block_exponents(v, 35), np.full(n, 32768)), O.block_exponents(v, 35))
+    v1 = O.moments(np.float64(g), 0.0, start, HYPER["beta1"], HYPER["beta2"])[1]
+    z = (total / seeds - v1) / (v1 / 16 / math.sqrt(seeds))     # at most one standard deviation each
+    assert abs(z.mean()) <= 5 / math.sqrt(n) and np.abs(z).max() <= 6
+
+
+def test_adamw_8_bits_second_moment_follows_a_change_of_scale():
+    """With beta2 = 0.999 a step moves v by a thousandth: 1500 steps of gradients three times as large bring it
+    to 9 (1 - 0.999^1500) + 0.999^1500 = 7.2 times its start, on average over the elements."""
+    M = _M()
+    n = 1 << 15
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    p = torch.zeros(n, device="cuda")
+    m, v, s = M.moara_adamw_state(p, 8)
+    v0 = np.full(n, 1e-6)
+    ev = O.block_exponents(v0, 35)
+    v.copy_(torch.from_numpy(O.encode_v(v0, ev, np.full(n, 32768))))
+    s.copy_(torch.from_numpy(np.stack([0 * ev + 18, ev], 1).astype(np.uint8).reshape(-1)))
+    start = O.decode_v(v.cpu().numpy(), ev).mean()
+    g = torch.empty(n, device="cuda")
+    args = M.AdamWArgs([p], [g], [m], [v], [s])
+    cfg = M.moara_adamw_default_config(bits=8)
+    for t in range(1500):
+        g.normal_(0, 3e-3, generator=gen)
+        M.moara_adamw_step(args, cfg, 1e-4, t + 1000, seed=t)
+    got = O.decode_v(v.cpu().numpy(), s.cpu().numpy().reshape(-1, 2)[:, 1].astype(int)).mean()
+    want = 9e-6 * (1 - 0.999 ** 1500) + start * 0.999 ** 1500
+    assert abs(got / want - 1) < 0.02, got / want       # 32768 elements that stray by about a third each: 0.2 %
+
+
+def test_adamw_step_with_a_clip_that_is_nan_changes_nothing():
+    M = _M()
+    nan = torch.full((1,), math.nan, device="cuda")
+    for bits in (32, 8):
+        x = torch.randn(777, device="cuda")
+        st = M.moara_adamw_state(x, bits)
+        before = [t.clone() for t in (x, *st) if t is not None]
+        args = M.AdamWArgs([x], [torch.ones_like(x)], [st[0]], [st[1]], None if bits == 32 else [st[2]])
+        M.moara_adamw_step(args, M.moara_adamw_default_config(bits=bits), 0.1, 1, clip=nan)
+        assert all(torch.equal(a, b) for a, b in zip(before, [t for t in (x, *st) if t is not None]))
+
+
+def test_adamw_transposed_parameter_and_refusals():
+    M = _M()
+    x = torch.randn(30, 20, device="cuda")
+    y, g = x.clone(), torch.randn(30, 20, device="cuda")
+    cfg = M.moara_adamw_default_config()
+    for p, q in ((x, g), (y.t(), g.t())):
+        st = M.moara_adamw_state(p, 32)
+        M.moara_adamw_step(M.AdamWArgs([p], [q], [st[0]], [st[1]]), cfg, 0.1, 1)
+    assert torch.equal(x, y)
+    a, b, _ = M.moara_adamw_state(x, 32)
+    c, d, s = M.moara_adamw_state(x, 8)
+    for args in (([x.half()], [g], [a], [b]), ([x[:, ::2]], [g[:, ::2]], [a], [b]), ([x], [g.t()], [a], [b]),
+                 ([x], [g], [a[1:]], [b]), ([x], [g], [c], [d]), ([x], [g], [c], [d], [s[:-1]]), ([x.cpu()], [g], [a], [b]),
+                 ([x, x], [g, g], [a, a], [b, b]), ([x], [g.cpu()], [a], [b]), ([x], [], [a], [b])):
+        with pytest.raises(ValueError):
+            M.AdamWArgs(*args)
+    ok = M.AdamWArgs([x], [g], [a], [b])
+    with pytest.raises(ValueError):
+        M.moara_adamw_step(ok, M.moara_adamw_default_config(bits=8), 0.1, 1)
+    for kw in (dict(beta1=1.0), dict(beta2=-0.1), dict(eps=0.0), dict(eps=math.nan)):
+        with pytest.raises(M.MoaraError) as e:
+            M.moara_adamw_step(ok, M.moara_adamw_default_config(**kw), 0.1, 1)
+        assert e.value.status == M.MOARA_E_ARG
+    for lr, step in ((math.inf, 1), (0.1, 0)):
+        with pytest.raises(M.MoaraError):
+            M.moara_adamw_step(ok, cfg, lr, step)
+
+
+def test_adamw_8_bits_past_2_to_the_31_elements():
+    M = _M()
+    n, k = (1 << 31) + 5000, 4096 + 17
+    g0 = rng(31, 1)
+    gt = np.float32(1e-3 * g0.standard_normal(k))
+    p = torch.zeros(n, dtype=BF16, device="cuda")
+    g = torch.zeros(n, dtype=BF16, device="cuda")
+    g[n - k:] = torch.from_numpy(gt).cuda().to(BF16)
+    m, v, s = M.moara_adamw_state(p, 8)
+    M.moara_adamw_step(M.AdamWArgs([p], [g], [m], [v], [s]), M.moara_adamw_default_config(bits=8, **HYPER), LR, 1, seed=77)
+    first = n - k - (n - k) % 32                    # whole blocks
+    x = _np(g[first:])
+    m1, v1 = O.moments(x, 0.0, 0.0, HYPER["beta1"], HYPER["beta2"])
+    em, ev = O.block_exponents(m1, 18), O.block_exponents(v1, 35)
+    _codes_agree(m[first:].cpu().numpy(), O.encode_m(m1, em), k, "m")
+    _codes_agree(v[first:].cpu().numpy(), O.encode_v(v1, ev, O.random16(first, n - first, 77, 0)), k, "v")
+    assert np.array_equal(s[first // 16:].cpu().numpy().reshape(-1, 2), np.stack([em, ev], 1))
+    assert not m[:first].any() and not v[:first].any() and not p[:first].any()
+    norm = M.moara_grad_norm([g], 1.0)
+    np.testing.assert_allclose(float(norm[0]), O.grad_norm([x], 1.0)[0], rtol=NORM_TOL)
+
+
+# ---------------------------------------------------------------- routing
+
+ROUTES = [
+    # tokens, experts, k, groups, top_groups, group_best
+    (1, 1, 1, 1, 1, 1), (5, 3, 3, 1, 1, 1), (33, 8, 2, 1, 1, 1), (100, 64, 6, 1, 1, 1), (17, 66, 5, 1, 1, 1),
+    (40, 128, 16, 1, 1, 1), (64, 160, 6, 8, 3, 1), (50, 256, 8, 8, 4, 2), (9, 250, 8, 5, 2, 2), (20, 256, 17, 1, 1, 1),
+    (21, 257, 9, 1, 1, 1), (13, 512, 12, 16, 5, 2), (7, 1024, 64, 64, 32, 2), (6, 1023, 31, 33, 7, 1),
+    (30, 64, 4, 64, 8, 1), (30, 64, 3, 32, 4, 2), (18, 60, 3, 20, 2, 2),
+]
+
+
+def _logits(T, E, seed, dtype):
+    g = rng(seed, T, E)
+    return torch.from_numpy(np.float32(1.5 * g.standard_normal((T, E)))).cuda().to(dtype), g
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("sigmoid,renorm,biased", [(0, 0, 0), (0, 1, 1), (1, 0, 0), (1, 1, 1), (0, 0, 1)])
+def test_route_and_its_gradient(sigmoid, renorm, biased, dtype):
+    M = _M()
+    for T, E, k, groups, top_groups, best in ROUTES:
+        x, g = _logits(T, E, 41, dtype)
+        bias = np.float32(0.1 * g.standard_normal(E)) if biased else None
+        mask = g.random(T) < 0.8 if biased else None
+        counts = torch.full((E,), 5, dtype=torch.int64, device="cuda")
+        cfg = M.moara_route_default_config(experts=E, top_k=k, groups=groups, top_groups=top_groups, group_best=best,
+                                           score=sigmoid, renormalise=renorm, scale=1.5)
+        index, weight = M.moara_route(cfg, x, bias=None if bias is None else torch.from_numpy(bias).cuda(),
+                                      mask=None if mask is None else torch.from_numpy(mask).cuda(), counts=counts)
+        L = _np(x)
+        ri, rw, c = O.route(L, k, bool(sigmoid), None if bias is None else bias.astype(np.float64), mask, groups, top_groups, best,
+                            bool(renorm), 1.5)
+        got = index.cpu().numpy()
+        # scores are at most 1 (and the bias 0.5): experts whose c differ by less than 1e-6 may change places
+        differ = got != ri
+        if differ.any():
+            a = np.take_along_axis(c, np.maximum(got, 0), 1)[differ]
+            b = np.take_along_axis(c, np.maximum(ri, 0), 1)[differ]
+            assert np.all(np.abs(a - b) <= 1e-6), (T, E)
+        assert np.array_equal(got < 0, ri < 0)
+        want = O.weights(L, got, bool(sigmoid), bool(renorm), 1.5)
+        np.testing.assert_allclose(_np(weight), want, rtol=16 * EPS32 * max(1, math.log2(E)), atol=1e-12)
+        n = np.bincount(got[got >= 0], minlength=E)
+        assert np.array_equal(counts.cpu().numpy(), 5 + n)
+        # gradient: the formula's by torch in 64 bits, and differences of the weights
+        dw = torch.from_numpy(np.float32(g.standard_normal((T, k)))).cuda()
+        grad = M.moara_route_backward(cfg, x, index, dw)
+        leaf = torch.from_numpy(L).requires_grad_(True)
+        s = torch.sigmoid(leaf) if sigmoid else torch.softmax(leaf, 1)
+        there = torch.from_numpy(got >= 0)
+        at = torch.where(there, s.gather(1, torch.from_numpy(np.maximum(got, 0)).long()), 0.0)
+        if renorm:
+            total = at.sum(1, keepdim=True)
+            at = at / torch.where(total > 0, total, 1.0)
+        (1.5 * at * dw.double().cpu()).sum().backward()
+        ref = leaf.grad.numpy()
+        size = np.abs(ref).max(axis=1, keepdims=True) + np.abs(_np(dw)).max(axis=1, keepdims=True) * want.max(axis=1, keepdims=True)
+        tol = 32 * EPS32 * size + 1e-12
+        if dtype == BF16:
+            tol = tol + 2.0 ** -8 * np.abs(ref)
+        assert np.all(np.abs(_np(grad) - ref) <= tol), (T, E, float((np.abs(_np(grad) - ref) / tol).max()))
+        h, e = 2.0 ** -12, int(g.integers(E))
+        up, down = L.copy(), L.copy()
+        up[:, e] += h
+        down[:, e] -= h
+        slope = ((O.weights(up, got, bool(sigmoid), bool(renorm), 1.5) - O.weights(down, got, bool(sigmoid), bool(renorm), 1.5))
+                 * _np(dw)).sum(axis=1) / (2 * h)
+        np.testing.assert_allclose(_np(grad)[:, e], slope, atol=float(size.max()) * (1e-6 + (2.0 ** -8 if dtype == BF16 else 0)),
+                                   rtol=0)
+
+
+@pytest.mark.parametrize("E,k,groups,top", [(64, 6, 1, 1), (256, 8, 8, 4), (300, 20, 1, 1), (512, 8, 64, 8)])
+@pytest.mark.parametrize("sigmoid", [0, 1])
+def test_route_ties_go_to_the_lowest_index(E, k, groups, top, sigmoid):
+    M = _M()
+    cfg = M.moara_route_default_config(experts=E, top_k=k, groups=groups, top_groups=top, score=sigmoid)
+    x = torch.zeros(3, E, device="cuda")
+    x[1, E // 2:] = 1.0         # the second half ties above the first
+    x[2, ::2] = -2.0            # the odd ones tie above the even ones
+    index, _ = M.moara_route(cfg, x)
+    want, _, _ = O.route(_np(x), k, bool(sigmoid), groups=groups, top_groups=top)
+    assert np.array_equal(index.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("E,k", [(64, 6), (300, 20)])
+@pytest.mark.parametrize("renorm", [0, 1])
+@pytest.mark.parametrize("sigmoid", [0, 1])
+def test_route_rows_that_leave_little_or_nothing(sigmoid, renorm, E, k):
+    M = _M()
+    inf = math.inf
+    x, g = _logits(12, E, 51, F32)
+    x[0] = -inf                             # softmax: no scores; sigmoid: all zero
+    x[1, 3] = math.nan
+    x[2, 5] = inf
+    x[3, 4:] = -inf                         # fewer experts with a score above zero than k
+    x[4] = 3.0e38
+    x[5] = -3.0e38
+    x[6] = -200.0                           # sigmoid scores underflow
+    x[7, 1:] = -250.0                       # softmax scores underflow
+    x[8] = torch.finfo(F32).min
+    mask = torch.ones(12, dtype=torch.bool, device="cuda")
+    mask[9] = False
+    bias = torch.zeros(E, device="cuda")
+    cfg = M.moara_route_default_config(experts=E, top_k=k, score=sigmoid, renormalise=renorm)
+    for b in (bias, torch.where(torch.arange(E, device="cuda") < E - k + 2, -inf, bias)):
+        index, weight = M.moara_route(cfg, x, bias=b, mask=mask)
+        ri, rw, _ = O.route(_np(x), k, bool(sigmoid), _np(b), _np(mask), renorm=bool(renorm))
+        assert np.array_equal(index.cpu().numpy(), ri)
+        np.testing.assert_allclose(_np(weight), rw, rtol=64 * EPS32, atol=2e-38)
+        grad = M.moara_route_backward(cfg, x, index, torch.randn(12, k, device="cuda"))
+        fine = ~np.isin(np.arange(12), [1, 2])      # rows whose logits are numbers or -inf
+        assert np.all(np.isfinite(_np(grad)[fine]))
+        assert not grad[9].any()
+
+
+def test_route_strided_logits_no_tokens_and_refusals():
+    M = _M()
+    cfg = M.moara_route_default_config(experts=60, top_k=4)
+    wide = torch.randn(50, 77, device="cuda")
+    for view in (wide[:, 3:63], wide[::3, 17:], wide[4:5, 1:61]):
+        a, b = M.moara_route(cfg, view), M.moara_route(cfg, view.contiguous())
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+        dw = torch.randn(view.shape[0], 4, device="cuda")
+        assert torch.equal(M.moara_route_backward(cfg, view, a[0], dw),
+                           M.moara_route_backward(cfg, view.contiguous(), a[0], dw))
+    none = M.moara_route(cfg, wide[:0, :60])
+    assert none[0].shape == (0, 4) and M.moara_route_backward(cfg, wide[:0, :60], *none).shape == (0, 60)
+    x = wide[:, :60].contiguous()
+    for bad in (x[:, :59], x.t().contiguous().t(), x.double(), x.cpu(), x[0]):
+        with pytest.raises(ValueError):
+            M.moara_route(cfg, bad)
+    for kw in (dict(bias=torch.zeros(59, device="cuda")), dict(mask=torch.ones(49, dtype=torch.bool, device="cuda")),
+               dict(counts=torch.zeros(60, dtype=torch.int32, device="cuda")), dict(bias=torch.zeros(60))):
+        with pytest.raises(ValueError):
+            M.moara_route(cfg, x, **kw)
+    i, w = M.moara_route(cfg, x)
+    for bad in ((i.long(), w), (i[:, :3], w), (i, w.double())):
+        with pytest.raises(ValueError):
+            M.moara_route_backward(cfg, x, *bad)
+
+
+def test_route_past_2_to_the_31_logits():
+    M = _M()
+    T, E = (1 << 21) + 37, 1024
+    x = torch.zeros(T, E, dtype=BF16, device="cuda")
+    tail = torch.randn(64, E, device="cuda").to(BF16)
+    x[-64:] = tail
+    cfg = M.moara_route_default_config(experts=E, top_k=8, renormalise=1)
+    counts = torch.zeros(E, dtype=torch.int64, device="cuda")
+    index, weight = M.moara_route(cfg, x, counts=counts)
+    i, w = M.moara_route(cfg, tail)
+    assert torch.equal(index[-64:], i) and torch.equal(weight[-64:], w)
+    assert int(counts.sum()) == 8 * T and int(counts[0]) >= T - 64
+    dw = torch.randn(T, 8, device="cuda")
+    grad = M.moara_route_backward(cfg, x, index, dw)
+    assert torch.equal(grad[-64:], M.moara_route_backward(cfg, tail, i, dw[-64:].contiguous()))
+
+
+@pytest.mark.parametrize("E", [1, 8, 64, 256, 1000])
+def test_balance_moves_the_bias_towards_an_even_load(E):
+    M = _M()
+    g = rng(61, E)
+    counts = g.integers(0, 50, E)
+    bias = np.float32(0.1 * g.standard_normal(E))
+    c, b = torch.from_numpy(counts).cuda(), torch.from_numpy(bias).cuda()
+    M.moara_route_balance(c, b, 2.0 ** -10)
+    np.testing.assert_allclose(_np(b), O.balance(counts, bias.astype(np.float64), 2.0 ** -10), rtol=0, atol=EPS32)
+    assert not c.any()
+
+
+# ---------------------------------------------------------------- streams, graphs, C refusals
+
+def _busy(x):
+    """Work that keeps the current stream occupied for a while, its result in x."""
+    y = torch.ones(4096, 4096, device="cuda")
+    for _ in range(6):
+        y = y @ y / 4096
+    x.mul_(y[0, 0])
+
+
+def test_calls_run_on_the_current_stream():
+    M = _M()
+    st = torch.cuda.Stream()
+    x = torch.randn(5000, device="cuda")
+    logits = torch.randn(300, 64, device="cuda")
+    cfg = M.moara_route_default_config(renormalise=1)
+    want_n = M.moara_grad_norm([x], 1.0)
+    want = M.moara_route(cfg, logits)
+    g = torch.zeros_like(x)
+    l2 = torch.zeros_like(logits)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        g.copy_(x)
+        _busy(g)
+        l2.copy_(logits)
+        n = M.moara_grad_norm([g], 1.0)
+        got = M.moara_route(cfg, l2)
+        grad = M.moara_route_backward(cfg, l2, *got)
+        p = torch.zeros_like(g)
+        s = M.moara_adamw_state(p, 8)
+        M.moara_adamw_step(M.AdamWArgs([p], [g], [s[0]], [s[1]], [s[2]]), M.moara_adamw_default_config(bits=8), 0.1, 1, clip=n[1:])
+    st.synchronize()
+    assert torch.equal(n, want_n) and all(torch.equal(a, b) for a, b in zip(got, want))
+    assert torch.equal(grad, M.moara_route_backward(cfg, logits, *want))
+    q = torch.zeros_like(x)
+    r = M.moara_adamw_state(q, 8)
+    M.moara_adamw_step(M.AdamWArgs([q], [x], [r[0]], [r[1]], [r[2]]), M.moara_adamw_default_config(bits=8), 0.1, 1,
+                       clip=want_n[1:])
+    assert torch.equal(p, q) and all(torch.equal(a, b) for a, b in zip(s, r))
+
+
+def test_calls_in_a_captured_graph():
+    """Captured once, replayed on new inputs between eager work; every replay equals the eager calls."""
+    M = _M()
+    E, T = 64, 500
+    cfg = M.moara_route_default_config(score=M.MOARA_SIGMOID, renormalise=1)
+    acfg = M.moara_adamw_default_config(bits=8)
+    x, g = torch.randn(T, E, device="cuda"), torch.randn(9000, device="cuda")
+    p, bias, counts = torch.randn(9000, device="cuda"), torch.zeros(E, device="cuda"), torch.zeros(E, dtype=torch.int64, device="cuda")
+    dw = torch.randn(T, 6, device="cuda")
+    s = M.moara_adamw_state(p, 8)
+    args, gargs, out = M.AdamWArgs([p], [g], [s[0]], [s[1]], [s[2]]), M.GradArgs([g]), torch.empty(2, device="cuda")
+
+    def calls():
+        M.moara_grad_norm(None, 1.0, out=out, args=gargs)
+        M.moara_adamw_step(args, acfg, 1e-3, 5, clip=out[1:], seed=9)
+        i, w = M.moara_route(cfg, x, bias=bias, counts=counts)
+        d = M.moara_route_backward(cfg, x, i, dw)
+        M.moara_route_balance(counts, bias, 1e-3)
+        return i, w, d
+
+    calls()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        res = calls()
+    state = [p, bias, counts, *s, out]
+    for k in range(4):
+        x.normal_(generator=torch.Generator(device="cuda").manual_seed(k))
+        g.normal_(generator=torch.Generator(device="cuda").manual_seed(50 + k))
+        before = [t.clone() for t in state]
+        want = [t.clone() for t in calls()] + [t.clone() for t in state]
+        for t, b in zip(state, before):
+            t.copy_(b)
+        torch.cuda.synchronize()
+        graph.replay()
+        got = [t.clone() for t in res] + [t.clone() for t in state]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), k
