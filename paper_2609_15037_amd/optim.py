@@ -12,8 +12,13 @@ decay, bias correction, GaLore scale 0.25 and T = 200).
 The learning rate of both groups comes from `param_groups`, so torch's LR
 schedulers drive it; `warmup_cosine` gives the paper's schedule (10 % linear
 warmup, cosine decay to 0.1 of the peak). Gradient clipping (the paper clips at
-1.0 for 7B) stays with the training loop (`torch.nn.utils.clip_grad_norm_`),
-before `step()`.
+1.0 for 7B) is the training loop's (`torch.nn.utils.clip_grad_norm_`, before
+`step()`), or `step()`'s own with `max_grad_norm`: the library's norm over every
+gradient, without a copy to the host.
+
+The AdamW step of the other parameters is torch's by default. `adamw_bits = 32` or
+`8` takes the library's instead: all tensors in a launch or two, moments in fp32
+whatever the parameters' type, or in 8 bits (2.06 bytes a parameter for both).
 
     targets, others = moara_targets(model)          # [(param, module id)], [param]
     opt = MoARa(targets, others, lr=1e-2, rank_table=..., block_size=64)
@@ -77,6 +82,61 @@ def warmup_cosine(total_steps: int, warmup_frac: float = 0.1, min_ratio: float =
     return f
 
 
+class _AdamW:
+    """The library's AdamW over a list of parameters: their moments, and each one's step count (parameters
+    without a gradient are not stepped)."""
+
+    def __init__(self, params: Sequence[torch.nn.Parameter], cfg: M.moara_adamw_config, weight_decay: float, seed: int):
+        self.params, self.cfg, self.weight_decay, self.seed = list(params), cfg, float(weight_decay), int(seed)
+        self.steps = np.zeros(len(self.params), dtype=np.int64)
+        self.calls = 0
+        self.state = None
+        self.args: Optional[M.AdamWArgs] = None
+
+    def _make(self) -> None:
+        if self.state is None:
+            self.state = [M.moara_adamw_state(p, self.cfg.bits) for p in self.params]
+
+    def _grad(self, p: torch.nn.Parameter) -> Optional[torch.Tensor]:
+        g = p.grad
+        if g is None or (g.layout == torch.strided and g.stride() == p.stride()):
+            return g
+        return torch.empty_like(p, dtype=g.dtype).copy_(g.to_dense() if g.layout != torch.strided else g)
+
+    def step(self, lr: float, clip: Optional[torch.Tensor]) -> None:
+        self._make()
+        grads = [self._grad(p) for p in self.params]
+        where = tuple(p.data_ptr() for p in self.params)    # a parameter's storage may have been replaced
+        if self.args is None or where != self.where:
+            self.args = M.AdamWArgs([p.detach() for p in self.params], grads, *([s[k] for s in self.state] for k in (0, 1)),
+                                    scales=[s[2] for s in self.state] if self.cfg.bits == 8 else None,
+                                    weight_decay=self.weight_decay)
+            self.where = where
+        else:
+            self.args.set_grads(grads)
+        self.steps += np.array([g is not None for g in grads])
+        self.calls += 1
+        M.moara_adamw_step(self.args, self.cfg, lr, np.maximum(self.steps, 1), clip=clip,
+                           seed=(self.seed << 32) + self.calls)
+
+    def state_dict(self) -> Dict:
+        self._make()
+        return {"bits": self.cfg.bits, "steps": self.steps.tolist(), "calls": self.calls, "seed": self.seed,
+                "state": [[None if t is None else t.cpu().clone() for t in s] for s in self.state]}
+
+    def load_state_dict(self, sd: Dict) -> None:
+        if sd["bits"] != self.cfg.bits or len(sd["state"]) != len(self.params):
+            raise ValueError(f"the state is of {len(sd['state'])} parameters with moments of {sd['bits']} bits, the optimizer "
+                             f"has {len(self.params)} with {self.cfg.bits}")
+        self._make()
+        for s, saved in zip(self.state, sd["state"]):
+            for t, x in zip(s, saved):
+                if t is not None:
+                    t.copy_(x)
+        self.steps[:] = sd["steps"]
+        self.calls, self.seed = int(sd["calls"]), int(sd["seed"])
+
+
 class MoARa(torch.optim.Optimizer):
     """MoARa for the projected weights (C library), AdamW for the other parameters.
 
@@ -84,6 +144,13 @@ class MoARa(torch.optim.Optimizer):
              dtype fp32 or bf16 (all the same), at least two axes (flattened by the
              first axis, Appendix B.1).
     others:  the remaining parameters (AdamW).
+    adamw_bits: None: torch.optim.AdamW steps the others; 32 or 8: the library's AdamW, its
+             moments of that many bits (parameters fp32 or bf16).
+    adamw_weight_decay, adamw_seed: of the library's AdamW (the seed of the 8-bit moments' rounding).
+    max_grad_norm: None, or the norm that step() clips the gradients of all parameters to. Gradients
+             of the targets are scaled in place, so are the others' with torch's AdamW. A norm that is
+             not finite clears the targets' gradients (their moments decay) and leaves the others alone.
+             `grad_norm` holds the last step's norm, on the GPU.
     rank_table: per-module ranks r_tau (MOARA_NUM_MODULES entries, 0 = unused); see
              moara_allocate_ranks for the Phase 3 rule.
     Other keyword arguments go to moara_default_config (block_size, scale,
@@ -92,7 +159,15 @@ class MoARa(torch.optim.Optimizer):
 
     def __init__(self, targets: Sequence[Tuple[torch.nn.Parameter, int]], others: Iterable[torch.nn.Parameter],
                  lr: float = 1e-2, betas=(0.9, 0.999), eps: float = 1e-6, rank_table: Sequence[int] = (),
-                 block_size: int = 64, scale: float = 0.25, refresh_interval: int = 200, **config):
+                 block_size: int = 64, scale: float = 0.25, refresh_interval: int = 200,
+                 adamw_bits: Optional[int] = None, adamw_weight_decay: float = 0.0, adamw_seed: int = 0,
+                 max_grad_norm: Optional[float] = None, **config):
+        if adamw_bits not in (None, 8, 32):
+            raise ValueError(f"adamw_bits must be None, 8 or 32, got {adamw_bits}")
+        if adamw_weight_decay and adamw_bits is None:
+            raise ValueError("adamw_weight_decay needs adamw_bits 8 or 32")
+        if max_grad_norm is not None and not max_grad_norm > 0:
+            raise ValueError(f"max_grad_norm must be positive, got {max_grad_norm}")
         targets = list(targets)
         others = list(others)
         if not targets:
@@ -113,7 +188,15 @@ class MoARa(torch.optim.Optimizer):
         self._descs = M.make_descs([(tuple(t.shape), m) for t, m in targets])
         self._st: Optional[M.State] = None
         self._g32: List[Optional[torch.Tensor]] = [None] * len(targets)
-        self._adamw = torch.optim.AdamW(others, lr=lr, betas=tuple(betas), eps=eps, weight_decay=0.0) if others else None
+        self._adamw = self._own = None
+        if others and adamw_bits is None:
+            self._adamw = torch.optim.AdamW(others, lr=lr, betas=tuple(betas), eps=eps, weight_decay=0.0)
+        elif others:
+            self._own = _AdamW(others, M.moara_adamw_default_config(beta1=float(betas[0]), beta2=float(betas[1]),
+                                                                   eps=float(eps), bits=adamw_bits),
+                               adamw_weight_decay, adamw_seed)
+        self._max_norm = max_grad_norm
+        self.grad_norm: Optional[torch.Tensor] = None
 
     def _device(self):
         """The target weights' GPU as the current device: the library's calls act on the
@@ -154,6 +237,7 @@ class MoARa(torch.optim.Optimizer):
             with torch.enable_grad():
                 loss = closure()
         tg = self.param_groups[0]
+        coef = self._clip() if self._max_norm is not None else None
         with self._device():
             if self._st is None:
                 self._st = M.moara_create_state(self._cfg, self._descs)
@@ -167,7 +251,26 @@ class MoARa(torch.optim.Optimizer):
             for g in self._adamw.param_groups:   # the schedule drives both groups
                 g["lr"] = og["lr"]
             self._adamw.step()
+        if self._own is not None:
+            self._own.step(float(self.param_groups[1]["lr"]), coef)
         return loss
+
+    def _clip(self) -> torch.Tensor:
+        """Norm of all gradients; the targets' (with torch's AdamW all) scaled to the limit in place. Returns the
+        coefficient. Runs on the current stream; the library's step, on the default one, waits for it."""
+        params = [p for g in self.param_groups for p in g["params"]]
+        for p in params:
+            if p.grad is not None and (p.grad.layout != torch.strided or not p.grad.is_contiguous()):
+                p.grad = (p.grad.to_dense() if p.grad.layout != torch.strided else p.grad).contiguous()
+        with self._device():
+            norm = M.moara_grad_norm([p.grad for p in params], self._max_norm)
+            scaled = self.param_groups[0]["params"] if self._own is not None else params
+            M.moara_grad_scale([p.grad for p in scaled], norm[1:])
+            here = torch.cuda.current_stream()
+            if here.cuda_stream != 0:
+                torch.cuda.default_stream().wait_stream(here)
+        self.grad_norm = norm[0]
+        return norm[1:]
 
     def state_dict(self) -> Dict:
         """Library state (projectors, moments, magnitude moments, step counters) as CPU
@@ -189,14 +292,19 @@ class MoARa(torch.optim.Optimizer):
                     lib.append(d)
         # the AdamW part is copied: torch's state_dict hands out the live moment tensors, and
         # loading those into another optimizer would alias the two
-        return {"moara": lib, "adamw": copy.deepcopy(self._adamw.state_dict()) if self._adamw else None,
-                "lr": [g["lr"] for g in self.param_groups]}
+        out = {"moara": lib, "adamw": copy.deepcopy(self._adamw.state_dict()) if self._adamw else None,
+               "lr": [g["lr"] for g in self.param_groups]}
+        if self._own is not None:
+            out["adamw_own"] = self._own.state_dict()
+        return out
 
     def load_state_dict(self, sd: Dict) -> None:
         for g, lr in zip(self.param_groups, sd["lr"]):
             g["lr"] = lr
         if self._adamw is not None and sd["adamw"] is not None:
             self._adamw.load_state_dict(sd["adamw"])
+        if self._own is not None and sd.get("adamw_own") is not None:
+            self._own.load_state_dict(sd["adamw_own"])
         if sd["moara"] is None:
             return
         with self._device():

@@ -1,0 +1,69 @@
+"""Expert routing for torch models over the library's operators (moara_route, its backward pass and the
+balancing bias's step).
+
+    router = ExpertRouter(d_model, experts=64, top_k=6)
+    index, weight = router(x)               # tokens x top_k; differentiable in x and the router's weight
+    load = router.load()                    # tokens of each expert since the last balance(), on the host
+    loss.backward(); opt.step()
+    router.balance(1e-3)                    # moves the bias, starts the counts again
+
+An expert without tokens has no gradient: the MoARa optimizer skips its matrices.
+"""
+from __future__ import annotations
+
+from typing import Optional, Tuple
+
+import numpy as np
+import torch
+
+from . import moara as M
+
+
+class _Route(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, cfg, bias, mask, counts):
+        index, weight = M.moara_route(cfg, logits, bias=bias, mask=mask, counts=counts)
+        ctx.cfg = cfg
+        ctx.save_for_backward(logits, index)
+        ctx.mark_non_differentiable(index)
+        return index, weight
+
+    @staticmethod
+    def backward(ctx, _, grad_weight):
+        logits, index = ctx.saved_tensors
+        grad = M.moara_route_backward(ctx.cfg, logits, index, grad_weight.float().contiguous())
+        return grad, None, None, None, None
+
+
+def route(logits: torch.Tensor, cfg: M.moara_route_config, bias: Optional[torch.Tensor] = None,
+          mask: Optional[torch.Tensor] = None, counts: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Indices and weights (tokens x top_k) of the experts of each row of logits; differentiable in the logits."""
+    return _Route.apply(logits, cfg, bias, mask, counts)
+
+
+class ExpertRouter(torch.nn.Module):
+    """A linear router: fp32 logits of each token, its top_k experts and their weights.
+
+    Keyword arguments are moara_route_config's (groups, top_groups, group_best, score, renormalise, scale).
+    `bias` (a buffer) only takes part in the choice; it moves with balance()."""
+
+    def __init__(self, d_model: int, experts: int, top_k: int, **config):
+        super().__init__()
+        self.cfg = M.moara_route_default_config(experts=experts, top_k=top_k, **config)
+        self.weight = torch.nn.Parameter(torch.randn(experts, d_model) * d_model ** -0.5)
+        self.register_buffer("bias", torch.zeros(experts, dtype=torch.float32))
+        self.register_buffer("counts", torch.zeros(experts, dtype=torch.int64))
+
+    def forward(self, x: torch.Tensor, mask: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """x: tokens x d_model; mask: tokens, False where a token is not routed. An index is -1 (weight 0)
+        where there is no expert."""
+        logits = torch.nn.functional.linear(x.float(), self.weight.float())
+        return route(logits, self.cfg, self.bias, mask, self.counts)
+
+    def load(self) -> np.ndarray:
+        """Tokens of each expert since the last balance() (waits for the GPU)."""
+        return self.counts.cpu().numpy()
+
+    def balance(self, rate: float) -> None:
+        """Moves the bias by `rate` towards an even load and sets the counts to zero."""
+        M.moara_route_balance(self.counts, self.bias, rate)

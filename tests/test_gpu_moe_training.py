@@ -1,0 +1,175 @@
+"""The operators of a training step together: MoARa with the library's AdamW and clipping, the router
+module, and the example that trains with all of them."""
+import importlib.util
+import math
+import os
+
+import numpy as np
+import pytest
+import torch
+
+from tests.conftest import ROOT
+from tests.harness import have_gpu
+
+pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not have_gpu(), reason="needs an MI355X GPU")]
+
+
+class Net(torch.nn.Module):
+    def __init__(self, seed):
+        super().__init__()
+        torch.manual_seed(seed)
+        self.embed = torch.nn.Embedding(96, 64)
+        self.q_proj = torch.nn.Linear(64, 64, bias=False)
+        self.down_proj = torch.nn.Linear(64, 64, bias=False)
+        self.norm = torch.nn.LayerNorm(64)
+        self.head = torch.nn.Linear(64, 96)
+
+    def forward(self, x):
+        h = self.embed(x)
+        h = h + self.down_proj(torch.relu(self.q_proj(h)))
+        return self.head(self.norm(h))
+
+
+def _opt(net, **kw):
+    from paper_2609_15037_amd.optim import MoARa, moara_targets
+    targets, others = moara_targets(net)
+    assert len(targets) == 2 and len(others) == 5
+    return MoARa(targets, others, lr=1e-2, rank_table=[16] * 10, block_size=32, refresh_interval=5, **kw)
+
+
+def _backward(net, step, seed=0):
+    x = torch.randint(0, 96, (32,), generator=torch.Generator().manual_seed(seed + step)).cuda()
+    loss = torch.nn.functional.cross_entropy(net(x).float(), (x + 1) % 96)
+    loss.backward()
+    return loss
+
+
+def _same_grads(a, b):
+    for p, q in zip(a.parameters(), b.parameters()):
+        q.grad = None if p.grad is None else p.grad.detach().clone()
+
+
+def test_library_adamw_follows_torch_adamw_in_the_optimizer():
+    a, b = Net(1).cuda(), Net(1).cuda()
+    oa, ob = _opt(a), _opt(b, adamw_bits=32)
+    for step in range(6):
+        _backward(a, step)
+        _same_grads(a, b)
+        for o in (oa, ob):
+            o.step()
+            o.zero_grad()
+    for (n, p), q in zip(a.named_parameters(), b.parameters()):   # six updates of about 1e-2, a few roundings each
+        torch.testing.assert_close(q, p, rtol=4e-6, atol=4e-6, msg=n)
+
+
+@pytest.mark.parametrize("bits", [None, 8, 32])
+@pytest.mark.parametrize("limit", [0.05, 1e6])
+def test_clipping_in_step_equals_clipping_before_it(limit, bits):
+    a, b = Net(2).cuda(), Net(2).cuda()
+    oa, ob = _opt(a, adamw_bits=bits), _opt(b, adamw_bits=bits, max_grad_norm=limit)
+    for step in range(3):
+        _backward(a, step)
+        _same_grads(a, b)
+        norm = torch.nn.utils.clip_grad_norm_(a.parameters(), limit)
+        oa.step()
+        ob.step()
+        assert abs(float(ob.grad_norm) / float(norm) - 1) < 1e-6
+        for o in (oa, ob):
+            o.zero_grad()
+    for (n, p), q in zip(a.named_parameters(), b.parameters()):
+        if bits == 8 and "proj" not in n:       # a code may round the other way: a sixteenth of an update
+            torch.testing.assert_close(q, p, rtol=0, atol=3e-2 / 16, msg=n)
+        else:   # Adam's first steps are near sign(g): an element of G near zero may move either way
+            assert float((q - p).abs().max()) <= 6e-2 and float((q - p).norm() / p.norm()) < 2e-3, n
+
+
+def test_a_norm_that_is_not_finite_skips_the_other_parameters():
+    net = Net(3).cuda()
+    opt = _opt(net, adamw_bits=8, max_grad_norm=1.0)
+    _backward(net, 0)
+    opt.step()
+    opt.zero_grad()
+    before = [p.detach().clone() for p in net.parameters()]
+    saved = opt.state_dict()["adamw_own"]["state"]
+    _backward(net, 1)
+    net.head.bias.grad[3] = math.inf
+    opt.step()
+    after = opt.state_dict()["adamw_own"]["state"]
+    for (n, p), q in zip(net.named_parameters(), before):
+        assert torch.isfinite(p).all()
+        assert ("proj" in n) or torch.equal(p.detach(), q), n
+    assert all(torch.equal(x, y) for s, t in zip(saved, after) for x, y in zip(s, t))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_checkpoint_of_the_library_adamw(bits):
+    a = Net(4).cuda()
+    oa = _opt(a, adamw_bits=bits, adamw_seed=7)
+    for step in range(3):
+        _backward(a, step)
+        if step == 1:
+            a.norm.bias.grad = None         # a parameter that misses a step
+        oa.step()
+        oa.zero_grad()
+    b = Net(5).cuda()
+    b.load_state_dict(a.state_dict())
+    ob = _opt(b, adamw_bits=bits)
+    ob.load_state_dict(oa.state_dict())
+    assert sorted(oa.state_dict()["adamw_own"]["steps"]) == [2, 3, 3, 3, 3]
+    _backward(a, 9)
+    _same_grads(a, b)
+    oa.step()
+    ob.step()
+    assert all(torch.equal(p, q) for p, q in zip(a.parameters(), b.parameters()))
+    with pytest.raises(ValueError):
+        _opt(b, adamw_bits=40 - bits).load_state_dict(oa.state_dict())
+
+
+def test_parameters_replaced_and_transposed_between_steps():
+    net = Net(6).cuda()
+    net.head.weight = torch.nn.Parameter(net.head.weight.detach().t().contiguous().t())
+    opt = _opt(net, adamw_bits=32)
+    for step in range(2):
+        _backward(net, step)
+        before = net.head.weight.detach().clone()
+        opt.step()
+        opt.zero_grad()
+        assert not torch.equal(net.head.weight.detach(), before)
+        net.embed.weight.data = net.embed.weight.data.clone()     # other storage
+    assert opt._own.steps.tolist() == [2] * 5
+
+
+def test_router_module_gradients_and_load():
+    from paper_2609_15037_amd import moara as M
+    from paper_2609_15037_amd.route import ExpertRouter
+    torch.manual_seed(7)
+    r = ExpertRouter(32, 16, 3, score=M.MOARA_SIGMOID, renormalise=1).cuda()
+    x = torch.randn(50, 32, device="cuda", requires_grad=True)
+    index, weight = r(x)
+    c = torch.randn(50, 3, device="cuda")
+    (weight * c).sum().backward()
+    w64 = r.weight.detach().double().requires_grad_(True)
+    x64 = x.detach().double().requires_grad_(True)
+    s = torch.sigmoid(x64 @ w64.t()).gather(1, index.long())
+    ((s / s.sum(1, keepdim=True)) * c).sum().backward()
+    torch.testing.assert_close(r.weight.grad.double(), w64.grad, rtol=1e-4, atol=1e-5)
+    torch.testing.assert_close(x.grad.double(), x64.grad, rtol=1e-4, atol=1e-5)
+    assert r.load().sum() == 150
+    weight2 = r(x)[1]
+    weight2.sum().backward()                # a gradient that is an expanded scalar
+    assert r.load().sum() == 300
+    load = r.load().copy()
+    r.balance(0.25)
+    assert not r.load().any()
+    assert np.array_equal(r.bias.cpu().numpy(), 0.25 * np.sign(load.mean() - load))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_example_trains(bits):
+    spec = importlib.util.spec_from_file_location("train_moe", os.path.join(ROOT, "examples", "train_moe.py"))
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    losses, share = ex.train(steps=40, bits=bits, say=lambda s: print("[moe]", s, flush=True))
+    assert np.isfinite(losses).all()
+    assert losses[-1] < 0.8 * losses[0], losses
+    assert max(share) <= 0.5        # top-2 of 8 experts: an even share is an eighth, one expert always chosen a half
