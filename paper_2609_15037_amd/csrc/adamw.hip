@@ -134,7 +134,7 @@ __global__ __launch_bounds__(256) void k_grad_scale(GradList L, const float* __r
 }
 
 // ---------------------------------------------------------------- AdamW
-constexpr int ADAMW_TILE = 2048;
+constexpr int CHUNK = 8 * 256;        // elements a workgroup takes at a time, eight a thread
 
 // Moments of one element. The products and sums are rounded one by one (no fused multiply-adds): the
 // 8-bit codes, whose rounding is a comparison, must not depend on which products are fused.
@@ -143,18 +143,17 @@ __device__ __forceinline__ void moments(float g, float& m, float& v, const Adamw
   m = m * L.b1 + g * L.c1;
   v = v * L.b2 + (g * g) * L.c2;
 }
+// The hardware's root and reciprocal (1 ulp each) for the update: it is rounded into a parameter many
+// times its size. The smallest normal number under the root keeps its argument out of the subnormals,
+// which the instruction takes for zero (1e-19 beside eps).
 __device__ __forceinline__ float updated(float p, float m, float v, const AdamwTensor& T, float eps) {
-  return p * T.decay - T.lr * (m / (sqrtf(v * T.rbc2) + eps));
+  const float root = __builtin_amdgcn_sqrtf(fmaf(v, T.rbc2, 0x1p-126f)) + eps;
+  return fmaf(-T.lr, m * __builtin_amdgcn_rcpf(root), p * T.decay);
 }
 
 template <typename PT, typename GT>
-__global__ __launch_bounds__(256) void k_adamw32(AdamwList L) {
-  const uint32_t t = blockIdx.x;
-  const int i = find_tensor(L.n, t, [&](int j) { return L.t[j].start; });
-  const AdamwTensor& T = L.t[i];
-  const float clip = L.clip ? *L.clip : 1.f;
-  const int64_t e = (int64_t)(t - T.start) * ADAMW_TILE + 8 * threadIdx.x, left = T.count - e;
-  if (left <= 0 || !(clip == clip)) return;
+__device__ __forceinline__ void chunk32(const AdamwTensor& T, const AdamwList& L, float clip, int64_t e, int64_t left) {
+  if (left <= 0) return;
   float p[8], g[8], m[8], v[8];
   load8((const PT*)T.p + e, left, p);
   load8((const GT*)T.g + e, left, g);
@@ -170,12 +169,25 @@ __global__ __launch_bounds__(256) void k_adamw32(AdamwList L) {
   store8((float*)T.v + e, left, v);
 }
 
+template <typename PT, typename GT>
+__global__ __launch_bounds__(256) void k_adamw32(AdamwList L) {
+  const uint32_t t = blockIdx.x;
+  const int i = find_tensor(L.n, t, [&](int j) { return L.t[j].start; });
+  const AdamwTensor& T = L.t[i];
+  const float clip = L.clip ? *L.clip : 1.f;
+  if (!(clip == clip)) return;
+  const int64_t e0 = (int64_t)(t - T.start) * CHUNK;
+  const int64_t e = e0 + 8 * threadIdx.x;
+  if (T.count - e0 >= CHUNK) chunk32<PT, GT>(T, L, clip, e, CHUNK);
+  else chunk32<PT, GT>(T, L, clip, e, T.count - e);
+}
+
 // ---- 8-bit moments: blocks of 32 elements (four lanes of eight), a biased exponent for each moment.
 constexpr uint32_t MIX_A = 0x9E3779B1u, MIX_B = 0x6A09E667u, MIX_C = 0xB7E15163u;
 
-// 32 random bits for the elements 2c and 2c + 1 of a tensor.
-__device__ __forceinline__ uint32_t random32(uint64_t c, uint32_t k0, uint32_t k1) {
-  uint32_t x = (uint32_t)c + (uint32_t)(c >> 32) * MIX_C + k0;
+// 32 random bits for the elements 2c and 2c + 1 of a tensor. base: key0 and the index's upper half mixed.
+__device__ __forceinline__ uint32_t random32(uint32_t c, uint32_t base, uint32_t k1) {
+  uint32_t x = c + base;
   x = ((x ^ (x >> 16)) * MIX_A) ^ k1;
   x = (x ^ (x >> 15)) * MIX_B;
   return x ^ (x >> 16);
@@ -188,31 +200,42 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t x) {
 }
 
 constexpr uint32_t INF_BITS = 0x7F800000u;
+constexpr uint32_t TOP_BITS = 0x7F600000u;     // 1.75 2^127: larger values do not fit the largest exponent
 
-// Bits of the largest finite magnitude of a block.
-__device__ __forceinline__ uint32_t block_top(const float (&x)[8]) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const uint32_t b = __float_as_uint(x[j]) & 0x7FFFFFFFu;
-    top = max(top, b < INF_BITS ? b : 0u);
-  }
-  return quad_max(top);
-}
-// Its exponent, one more where the significand is over 1.75: the codes' largest value is 1.75 2^e.
+// The exponent of a block's largest magnitude, one more where the significand is over 1.75: the codes'
+// largest value is 1.75 2^e.
 __device__ __forceinline__ int block_exponent(uint32_t top, int least) {
-  return min(max((int)((top + 0x1FFFFFu) >> 23), least), 254);
+  return max((int)((top + 0x1FFFFFu) >> 23), least);
 }
 __device__ __forceinline__ float two_to(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
+// Codes of blocks with values that are not finite, or too large for the largest exponent: the exponents
+// are those of the finite values.
+__device__ __forceinline__ void encode_any(const float (&m)[8], const float (&v)[8], const uint32_t (&r)[4],
+                                           uint32_t (&co)[2], uint32_t (&cv)[2], int& em, int& ev) {
+  uint32_t tm = 0, tv = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t a = __float_as_uint(m[j]) & 0x7FFFFFFFu, b = __float_as_uint(v[j]) & 0x7FFFFFFFu;
+    tm = max(tm, a < INF_BITS ? a : 0u);
+    tv = max(tv, b < INF_BITS ? b : 0u);
+  }
+  em = min(block_exponent(quad_max(tm), 18), 254);
+  ev = min(block_exponent(quad_max(tv), 35), 254);
+  co[0] = co[1] = cv[0] = cv[1] = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float y = fminf(fmaxf(m[j] * two_to(135 - em), -448.f), 448.f);
+    const uint32_t a = isfinite(m[j]) ? (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false) & 255u : 0x7Fu;
+    const uint32_t y20 = __float_as_uint(__builtin_amdgcn_ldexpf(v[j], 31 - ev)) + (((r[j >> 1] >> (16 * (j & 1))) & 0xFFFFu) << 4);
+    const uint32_t b = isfinite(v[j]) ? min(max(y20 >> 20, v[j] > 0.f ? 1u : 0u), 254u) : 255u;
+    co[j >> 2] |= a << (8 * (j & 3));
+    cv[j >> 2] |= b << (8 * (j & 3));
+  }
+}
+
 template <typename PT, typename GT>
-__global__ __launch_bounds__(256) void k_adamw8(AdamwList L) {
-  const uint32_t t = blockIdx.x;
-  const int i = find_tensor(L.n, t, [&](int j) { return L.t[j].start; });
-  const AdamwTensor& T = L.t[i];
-  const float clip = L.clip ? *L.clip : 1.f;
-  if (!(clip == clip)) return;
-  const int64_t e = (int64_t)(t - T.start) * ADAMW_TILE + 8 * threadIdx.x, left = T.count - e;
+__device__ __forceinline__ void chunk8(const AdamwTensor& T, const AdamwList& L, float clip, int64_t e, int64_t left) {
   float p[8], g[8], m[8], v[8];
   uint8_t* const mq = (uint8_t*)T.m + e;
   uint8_t* const vq = (uint8_t*)T.v + e;
@@ -228,6 +251,7 @@ __global__ __launch_bounds__(256) void k_adamw8(AdamwList L) {
       mc = *reinterpret_cast<const u32x2u*>(mq);
       vc = *reinterpret_cast<const u32x2u*>(vq);
     } else {
+#pragma unroll
       for (int j = 0; j < 8; ++j)
         if (j < left) {
           mc[j >> 2] |= (uint32_t)mq[j] << (8 * (j & 3));
@@ -237,64 +261,91 @@ __global__ __launch_bounds__(256) void k_adamw8(AdamwList L) {
     em = sq[0];
     ev = sq[1];
   }
-  {
-    const float s = two_to(em - 135);
+  const float s = two_to(max(em, 18) - 135);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)mc[h], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)mc[h], true);
-      m[4 * h] = a[0] * s; m[4 * h + 1] = a[1] * s; m[4 * h + 2] = b[0] * s; m[4 * h + 3] = b[1] * s;
-    }
+  for (int h = 0; h < 2; ++h) {
+    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)mc[h], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)mc[h], true);
+    m[4 * h] = a[0] * s; m[4 * h + 1] = a[1] * s; m[4 * h + 2] = b[0] * s; m[4 * h + 3] = b[1] * s;
   }
+  uint32_t tc = 0, tv = 0;
+  float tm = 0.f;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const uint32_t c = (vc[j >> 2] >> (8 * (j & 3))) & 255u;
-    // a code's bits at the top of a 32-bit float's exponent and fraction are its value times 2^(31 - ev)
-    v[j] = c == 255u ? __builtin_nanf("") : __builtin_amdgcn_ldexpf(__uint_as_float(c << 20), ev - 31);
+    // a code's bits below the sign and three bits of a 32-bit float are its value times 2^(31 - ev)
+    const int sh = 20 - 8 * (j & 3);
+    const uint32_t c = (sh >= 0 ? vc[j >> 2] << (sh & 31) : vc[j >> 2] >> (-sh & 31)) & 0x0FF00000u;
+    tc = max(tc, c);
+    v[j] = __builtin_amdgcn_ldexpf(__uint_as_float(c), ev - 31);
     moments(g[j] * clip, m[j], v[j], L);
     p[j] = updated(p[j], m[j], v[j], T, L.eps);
+    tm = fmaxf(tm, fabsf(m[j]));
+    tv = max(tv, __float_as_uint(v[j]));
   }
-  em = block_exponent(block_top(m), 18);
-  ev = block_exponent(block_top(v), 35);
-  if (left <= 0) return;
-  store8((PT*)T.p + e, left, p);
-  uint32_t co[8], cv[8];
-  const float sm = two_to(135 - em);
+  const uint32_t qm = quad_max(__float_as_uint(tm));
+  const uint32_t qv = quad_max(tc == 0x0FF00000u ? 0xFFFFFFFFu : tv);
+  uint32_t r[4];
+  const uint64_t c0 = (uint64_t)e >> 1;
+  const uint32_t base = (uint32_t)(c0 >> 32) * MIX_C + T.key0;
 #pragma unroll
-  for (int j = 0; j < 8; j += 2) {
-    const float a = fminf(fmaxf(m[j] * sm, -448.f), 448.f), b = fminf(fmaxf(m[j + 1] * sm, -448.f), 448.f);
-    const uint32_t w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-    co[j] = isfinite(m[j]) ? w & 255u : 0x7Fu;
-    co[j + 1] = isfinite(m[j + 1]) ? (w >> 8) & 255u : 0x7Fu;
-    const uint32_t r = random32((uint64_t)(e + j) >> 1, T.key0, T.key1);
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const float x = v[j + q];
-      const uint32_t b20 = __float_as_uint(__builtin_amdgcn_ldexpf(x, 31 - ev)) + ((q ? r >> 16 : r & 0xFFFFu) << 4);
-      const uint32_t c = min(max(b20 >> 20, x > 0.f ? 1u : 0u), 254u);
-      cv[j + q] = isfinite(x) ? c : 255u;
-    }
-  }
-  if (left >= 8) {
-    u32x2u a, b;
+  for (int j = 0; j < 4; ++j) r[j] = random32((uint32_t)c0 + j, base, T.key1);
+  uint32_t co[2], cv[2];
+  if (max(qm, qv) <= TOP_BITS) {
+    em = block_exponent(qm, 18);
+    ev = block_exponent(qv, 35);
+    const float sm = two_to(135 - em);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      a[h] = co[4 * h] | co[4 * h + 1] << 8 | co[4 * h + 2] << 16 | co[4 * h + 3] << 24;
-      b[h] = cv[4 * h] | cv[4 * h + 1] << 8 | cv[4 * h + 2] << 16 | cv[4 * h + 3] << 24;
+      co[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(m[4 * h] * sm, m[4 * h + 1] * sm, 0, false);
+      co[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(m[4 * h + 2] * sm, m[4 * h + 3] * sm, (int)co[h], true);
+      uint32_t c[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float x = v[4 * h + j];
+        const uint32_t rr = r[2 * h + (j >> 1)], r16 = j & 1 ? rr >> 16 : rr & 0xFFFFu;
+        const uint32_t y = __float_as_uint(__builtin_amdgcn_ldexpf(x, 31 - ev)) + (r16 << 4);
+        c[j] = max(y >> 20, min(__float_as_uint(x), 1u));      // not 0 where x is above 0
+      }
+      cv[h] = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
     }
-    *reinterpret_cast<u32x2u*>(mq) = a;
-    *reinterpret_cast<u32x2u*>(vq) = b;
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      if (j < left) { mq[j] = (uint8_t)co[j]; vq[j] = (uint8_t)cv[j]; }
+      if (((vc[j >> 2] >> (8 * (j & 3))) & 255u) == 255u) v[j] = p[j] = __builtin_nanf("");
+    encode_any(m, v, r, co, cv, em, ev);
+  }
+  if (left <= 0) return;
+  store8((PT*)T.p + e, left, p);
+  if (left >= 8) {
+    *reinterpret_cast<u32x2u*>(mq) = u32x2u{co[0], co[1]};
+    *reinterpret_cast<u32x2u*>(vq) = u32x2u{cv[0], cv[1]};
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < left) {
+        mq[j] = (uint8_t)(co[j >> 2] >> (8 * (j & 3)));
+        vq[j] = (uint8_t)(cv[j >> 2] >> (8 * (j & 3)));
+      }
   }
   if ((threadIdx.x & 3) == 0) { sq[0] = (uint8_t)em; sq[1] = (uint8_t)ev; }
+}
+
+template <typename PT, typename GT>
+__global__ __launch_bounds__(256) void k_adamw8(AdamwList L) {
+  const uint32_t t = blockIdx.x;
+  const int i = find_tensor(L.n, t, [&](int j) { return L.t[j].start; });
+  const AdamwTensor& T = L.t[i];
+  const float clip = L.clip ? *L.clip : 1.f;
+  if (!(clip == clip)) return;
+  const int64_t e0 = (int64_t)(t - T.start) * CHUNK;
+  const int64_t e = e0 + 8 * threadIdx.x;
+  if (T.count - e0 >= CHUNK) chunk8<PT, GT>(T, L, clip, e, CHUNK);
+  else chunk8<PT, GT>(T, L, clip, e, T.count - e);
 }
 
 }  // namespace
 
 uint32_t grad_tiles(int64_t count) { return (uint32_t)((count + GRAD_TILE - 1) / GRAD_TILE); }
-uint32_t adamw_tiles(int64_t count) { return (uint32_t)((count + ADAMW_TILE - 1) / ADAMW_TILE); }
+uint32_t adamw_tiles(int64_t count) { return (uint32_t)((count + CHUNK - 1) / CHUNK); }
 
 hipError_t launch_grad_norm(const GradList& l, double* partial, bool first, hipStream_t st) {
   hipLaunchKernelGGL(k_grad_norm, dim3(NORM_WGS), dim3(256), 0, st, l, partial, (int)first);

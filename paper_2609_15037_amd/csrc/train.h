@@ -45,6 +45,7 @@ struct AdamwList {
   float b1, c1, b2, c2, eps;    // c = 1 - b
   int n;
 };
+static_assert(sizeof(GradList) <= 4096 && sizeof(AdamwList) <= 4096, "lists travel in the kernels' arguments");
 uint32_t adamw_tiles(int64_t count);
 hipError_t launch_adamw(const AdamwList& l, bool p_bf16, bool g_bf16, int bits, uint32_t total, hipStream_t st);
 

@@ -469,16 +469,20 @@ def _vector(t, device, dtype, count, what: str) -> int:
     return t.data_ptr()
 
 
-def _call(device: Optional[int], stream, fn, *args):
+def _call(device: int, stream, fn, *args):
     """fn(*args, stream) with the tensors' device current; stream None: the device's current torch stream."""
     import torch
-    if device is None or device == torch.cuda.current_device():
-        s = _stream_ptr(torch.cuda.current_stream() if stream is None else stream)
-        _check(fn(*args, s))
+    if stream is None:
+        s = torch._C._cuda_getCurrentRawStream(device)      # a third of a small call's time is the stream object's
+    else:
+        s = _stream_ptr(stream)
+    if device == torch._C._cuda_getDevice():
+        rc = fn(*args, s)
     else:
         with torch.cuda.device(device):
-            s = _stream_ptr(torch.cuda.current_stream() if stream is None else stream)
-            _check(fn(*args, s))
+            rc = fn(*args, s)
+    if rc != MOARA_OK:
+        _check(rc)
 
 
 class GradArgs:
@@ -610,7 +614,8 @@ def moara_adamw_step(args: AdamWArgs, cfg: moara_adamw_config, lr, step, clip=No
     args.rec["lr"] = lr
     args.rec["step"] = step
     c = None if clip is None else _vector(clip, args.device, torch.float32, 1, "clip")
-    _call(args.device, stream, lib().moara_adamw_step, ctypes.byref(cfg), args.ptr, args.n, c, seed & (2 ** 64 - 1))
+    if args.n:
+        _call(args.device, stream, lib().moara_adamw_step, ctypes.byref(cfg), args.ptr, args.n, c, seed & (2 ** 64 - 1))
 
 
 def moara_route_default_config(**overrides) -> moara_route_config:
