@@ -365,7 +365,8 @@ typedef struct {
   int32_t reserved;
 } moara_grad_tensor;
 
-/* Bytes of the workspace of moara_grad_norm (device memory, 8-byte aligned). */
+/* Bytes of the workspace of moara_grad_norm: device memory, 8-byte aligned, of any contents, for
+ * one call at a time. */
 #define MOARA_GRAD_NORM_WORKSPACE 16384
 
 /* out[0] = the 2-norm over all elements of all tensors, out[1] = min(1, max_norm /

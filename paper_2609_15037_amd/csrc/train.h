@@ -19,10 +19,10 @@ struct GradList {
 };
 constexpr int NORM_WGS = 2048;  // partial sums; the workspace of moara_grad_norm holds them
 uint32_t grad_tiles(int64_t count);
-// first: the partial sums are stored, else added to
-hipError_t launch_grad_norm(const GradList& l, double* partial, bool first, hipStream_t st);
+// first: the partial sums are stored, else added to. once: the list is read past the caches.
+hipError_t launch_grad_norm(const GradList& l, bool once, double* partial, bool first, hipStream_t st);
 hipError_t launch_grad_norm_end(const double* partial, float max_norm, float* out, hipStream_t st);
-hipError_t launch_grad_scale(const GradList& l, const float* coef, hipStream_t st);
+hipError_t launch_grad_scale(const GradList& l, bool once, const float* coef, hipStream_t st);
 
 // ---------------------------------------------------------------- AdamW
 constexpr int ADAMW_MAX = 48;

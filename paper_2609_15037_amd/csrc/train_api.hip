@@ -30,21 +30,17 @@ int check_grads(const moara_grad_tensor* t, int32_t n) {
   return MOARA_OK;
 }
 
-// The list in launches of at most GRAD_MAX tensors; launch(list) for each.
+// The list in launches of at most GRAD_MAX tensors: launch(list, first) for each, once at least.
 template <typename F> int each_grad_list(const moara_grad_tensor* t, int32_t n, F launch) {
-  GradList l;
-  auto clear = [&] {
-    l.n = 0;
-    l.tiles = 0;
-    for (uint32_t& b : l.bf16) b = 0;
-  };
-  clear();
+  GradList l{};
+  bool first = true;
   for (int i = 0; i < n; ++i) {
     if (!t[i].grad || t[i].count == 0) continue;
     const uint32_t tiles = grad_tiles(t[i].count);
     if (l.n == GRAD_MAX || (l.n && l.tiles + tiles > MAX_TILES)) {
-      TRAIN_TRY(launch(l));
-      clear();
+      TRAIN_TRY(launch(l, first));
+      first = false;
+      l = GradList{};
     }
     l.g[l.n] = t[i].grad;
     l.count[l.n] = t[i].count;
@@ -53,8 +49,16 @@ template <typename F> int each_grad_list(const moara_grad_tensor* t, int32_t n, 
     l.tiles += tiles;
     ++l.n;
   }
-  if (l.n) TRAIN_TRY(launch(l));
+  TRAIN_TRY(launch(l, first));
   return MOARA_OK;
+}
+
+// Whether the gradients take more than the memory-side cache holds.
+bool over_cache(const moara_grad_tensor* t, int32_t n) {
+  int64_t bytes = 0;
+  for (int i = 0; i < n; ++i)
+    if (t[i].grad) bytes += t[i].count * (t[i].dtype == MOARA_BF16 ? 2 : 4);
+  return bytes > (int64_t)256 << 20;
 }
 
 uint32_t mix(uint32_t x) {
@@ -117,20 +121,14 @@ int moara_grad_norm(const moara_grad_tensor* tensors, int32_t n, float max_norm,
   if (!out || !workspace) return moara_fail(MOARA_E_ARG, "null out or workspace");
   if (misaligned(out, 4) || misaligned(workspace, 8)) return moara_fail(MOARA_E_ARG, "out or workspace not aligned");
   if (!(max_norm > 0)) return moara_fail(MOARA_E_ARG, "max_norm must be positive");
-  const hipStream_t st = (hipStream_t)stream;
-  double* partial = (double*)workspace;
-  bool first = true;
-  const int rl = each_grad_list(tensors, n, [&](const GradList& l) {
-    const hipError_t e = launch_grad_norm(l, partial, first, st);
-    first = false;
-    return e;
+  static_assert(sizeof(double) * NORM_WGS <= MOARA_GRAD_NORM_WORKSPACE, "workspace of moara_grad_norm");
+  double* const partial = (double*)workspace;
+  const bool once = over_cache(tensors, n);
+  const int rl = each_grad_list(tensors, n, [&](const GradList& l, bool first) {
+    return launch_grad_norm(l, once, partial, first, (hipStream_t)stream);
   });
   if (rl != MOARA_OK) return rl;
-  if (first) {      // no elements: the partial sums are zero
-    GradList l{};
-    TRAIN_TRY(launch_grad_norm(l, partial, true, st));
-  }
-  TRAIN_TRY(launch_grad_norm_end(partial, max_norm, out, st));
+  TRAIN_TRY(launch_grad_norm_end(partial, max_norm, out, (hipStream_t)stream));
   return MOARA_OK;
 }
 
@@ -138,7 +136,10 @@ int moara_grad_scale(const moara_grad_tensor* tensors, int32_t n, const float* c
   const int rc = check_grads(tensors, n);
   if (rc != MOARA_OK) return rc;
   if (!coef || misaligned(coef, 4)) return moara_fail(MOARA_E_ARG, "null or misaligned coefficient");
-  return each_grad_list(tensors, n, [&](const GradList& l) { return launch_grad_scale(l, coef, (hipStream_t)stream); });
+  const bool once = over_cache(tensors, n);
+  return each_grad_list(tensors, n, [&](const GradList& l, bool) {
+    return l.n ? launch_grad_scale(l, once, coef, (hipStream_t)stream) : hipSuccess;
+  });
 }
 
 int moara_adamw_default_config(moara_adamw_config* out) {

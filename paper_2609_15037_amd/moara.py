@@ -488,24 +488,27 @@ def _call(device: int, stream, fn, *args):
 class GradArgs:
     """The marshalled list of gradient tensors for moara_grad_norm and moara_grad_scale, checked once:
     float32 or bfloat16 without gaps; None where a parameter has no gradient. Holds the tensors and
-    the norm's workspace. Calls that share it run on one stream, or in an order the caller keeps."""
+    the norm's workspace: calls that share a GradArgs run on one stream, or in an order the caller keeps."""
 
     def __init__(self, grads):
         import torch
-        self.keep = [g for g in grads if g is not None]
         self.device = None
-        self.rec = np.zeros(len(self.keep), dtype=_RECORDS[moara_grad_tensor])
+        self.set_grads(grads)
+        where = torch.cuda.current_device() if self.device is None else self.device
+        self.workspace = torch.empty(MOARA_GRAD_NORM_WORKSPACE, dtype=torch.uint8, device=f"cuda:{where}")
+        self.device = where
+
+    def set_grads(self, grads):
+        """Other gradient tensors (on the same GPU) for the same workspace."""
+        keep = [g for g in grads if g is not None]
         rows = []
-        for i, g in enumerate(self.keep):
+        for i, g in enumerate(keep):
             self.device = _on_gpu(g, self.device, f"grads[{i}]")
             if not _dense(g):
                 raise ValueError(f"grads[{i}]: strides {g.stride()} of shape {tuple(g.shape)} leave gaps")
             rows.append((g.data_ptr(), g.numel(), _dtype_id(g, f"grads[{i}]"), 0))
-        if rows:
-            self.rec[:] = rows
+        self.keep, self.rec = keep, np.array(rows, dtype=_RECORDS[moara_grad_tensor])
         self.ptr, self.n = self.rec.ctypes.data, len(rows)
-        where = torch.cuda.current_device() if self.device is None else self.device
-        self.workspace = torch.empty(MOARA_GRAD_NORM_WORKSPACE, dtype=torch.uint8, device=f"cuda:{where}")
 
 
 def moara_grad_norm(grads, max_norm: float, out=None, stream=None, args: Optional[GradArgs] = None):
@@ -516,8 +519,8 @@ def moara_grad_norm(grads, max_norm: float, out=None, stream=None, args: Optiona
     a = GradArgs(grads) if args is None else args
     if out is None:
         out = torch.empty(2, dtype=torch.float32, device=a.workspace.device)
-    _call(a.workspace.get_device(), stream, lib().moara_grad_norm, a.ptr, a.n, float(max_norm),
-          _vector(out, a.workspace.get_device(), torch.float32, 2, "out"), a.workspace.data_ptr())
+    _call(a.device, stream, lib().moara_grad_norm, a.ptr, a.n, float(max_norm),
+          _vector(out, a.device, torch.float32, 2, "out"), a.workspace.data_ptr())
     return out
 
 
@@ -526,8 +529,7 @@ def moara_grad_scale(grads, coef, stream=None, args: Optional[GradArgs] = None):
     GPU), in place."""
     import torch
     a = GradArgs(grads) if args is None else args
-    _call(a.workspace.get_device(), stream, lib().moara_grad_scale, a.ptr, a.n,
-          _vector(coef, a.workspace.get_device(), torch.float32, 1, "coef"))
+    _call(a.device, stream, lib().moara_grad_scale, a.ptr, a.n, _vector(coef, a.device, torch.float32, 1, "coef"))
 
 
 def moara_adamw_default_config(**overrides) -> moara_adamw_config:

@@ -196,6 +196,7 @@ class MoARa(torch.optim.Optimizer):
                                                                    eps=float(eps), bits=adamw_bits),
                                adamw_weight_decay, adamw_seed)
         self._max_norm = max_grad_norm
+        self._norm_args: Optional[M.GradArgs] = None
         self.grad_norm: Optional[torch.Tensor] = None
 
     def _device(self):
@@ -263,10 +264,14 @@ class MoARa(torch.optim.Optimizer):
             if p.grad is not None and (p.grad.layout != torch.strided or not p.grad.is_contiguous()):
                 p.grad = (p.grad.to_dense() if p.grad.layout != torch.strided else p.grad).contiguous()
         with self._device():
-            norm = M.moara_grad_norm([p.grad for p in params], self._max_norm)
-            scaled = self.param_groups[0]["params"] if self._own is not None else params
-            M.moara_grad_scale([p.grad for p in scaled], norm[1:])
             here = torch.cuda.current_stream()
+            if self._norm_args is None or here != self._norm_stream:    # its workspace is used by one stream at a time
+                self._norm_args, self._norm_stream = M.GradArgs([]), here
+            self._norm_args.set_grads([p.grad for p in params])
+            norm = M.moara_grad_norm(None, self._max_norm, args=self._norm_args)
+            if self._own is not None:
+                self._norm_args.set_grads([p.grad for p in self.param_groups[0]["params"]])
+            M.moara_grad_scale(None, norm[1:], args=self._norm_args)
             if here.cuda_stream != 0:
                 torch.cuda.default_stream().wait_stream(here)
         self.grad_norm = norm[0]
