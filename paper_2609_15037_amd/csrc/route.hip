@@ -21,14 +21,38 @@ template <int CTRL> __device__ __forceinline__ double dpp(double x) {
   const uint64_t b = __builtin_bit_cast(uint64_t, x);
   return __builtin_bit_cast(double, (uint64_t)dpp<CTRL>((uint32_t)(b >> 32)) << 32 | dpp<CTRL>((uint32_t)b));
 }
+// The two values, a lane's and that of the lane DIST (16 or 32) away, in the same order for both lanes.
+template <int DIST> __device__ __forceinline__ void rows_apart(uint32_t x, uint32_t& a, uint32_t& b) {
+  const auto r = DIST == 16 ? __builtin_amdgcn_permlane16_swap(x, x, false, false)
+                            : __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  a = r[0];
+  b = r[1];
+}
+template <int DIST> __device__ __forceinline__ void rows_apart(float x, float& a, float& b) {
+  uint32_t p, q;
+  rows_apart<DIST>(__float_as_uint(x), p, q);
+  a = __uint_as_float(p);
+  b = __uint_as_float(q);
+}
+template <int DIST> __device__ __forceinline__ void rows_apart(double x, double& a, double& b) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  uint32_t p0, q0, p1, q1;
+  rows_apart<DIST>((uint32_t)u, p0, q0);
+  rows_apart<DIST>((uint32_t)(u >> 32), p1, q1);
+  a = __builtin_bit_cast(double, (uint64_t)p1 << 32 | p0);
+  b = __builtin_bit_cast(double, (uint64_t)q1 << 32 | q0);
+}
 template <int LANES, typename T, typename F> __device__ __forceinline__ T reduce(T x, F f) {
   x = f(x, dpp<0xB1>(x));     // lane ^ 1
   x = f(x, dpp<0x4E>(x));     // lane ^ 2
   x = f(x, dpp<0x141>(x));    // mirrored within eight lanes
   x = f(x, dpp<0x140>(x));    // mirrored within sixteen
   if (LANES == 64) {
-    x = f(x, (T)__shfl_xor(x, 16, 64));
-    x = f(x, (T)__shfl_xor(x, 32, 64));
+    T a, b;
+    rows_apart<16>(x, a, b);
+    x = f(a, b);
+    rows_apart<32>(x, a, b);
+    x = f(a, b);
   }
   return x;
 }
@@ -38,57 +62,55 @@ template <int LANES> __device__ __forceinline__ float sum_of(float x) {
 template <int LANES> __device__ __forceinline__ double sum_of(double x) {
   return reduce<LANES>(x, [](double a, double b) { return a + b; });
 }
+template <int LANES> __device__ __forceinline__ double max_of(double x) {
+  return reduce<LANES>(x, [](double a, double b) { return fmax(a, b); });
+}
 template <int LANES> __device__ __forceinline__ float max_of(float x) {
   return reduce<LANES>(x, [](float a, float b) { return fmaxf(a, b); });
 }
 template <int LANES> __device__ __forceinline__ uint32_t max_of(uint32_t x) {
   return reduce<LANES>(x, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
-template <int LANES> __device__ __forceinline__ uint32_t min_of(uint32_t x) {
-  return reduce<LANES>(x, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
-}
 
-// Four lanes' worth of a row: experts e0 .. e0 + 3 of which those below E exist (the others read -inf).
-__device__ __forceinline__ void load4(const float* q, int n, float* x) {
-  if (n >= 4) {
-    const f32x4u a = *reinterpret_cast<const f32x4u*>(q);
+// Four experts of a row, from element i: fp32 or bf16, of any alignment; n of them exist, the others are
+// -inf and are not written.
+__device__ __forceinline__ void load4(const void* row, bool is_bf16, int64_t i, int n, float* x) {
+  const float* f = (const float*)row + i;
+  const bf16* h = (const bf16*)row + i;
+  if (n >= 4 && is_bf16) {
+    const u16x4u a = *reinterpret_cast<const u16x4u*>(h);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = __uint_as_float((uint32_t)a[j] << 16);
+  } else if (n >= 4) {
+    const f32x4u a = *reinterpret_cast<const f32x4u*>(f);
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[j] = a[j];
   } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = j < n ? q[j] : -__builtin_inff();
+    for (int j = 0; j < 4; ++j) x[j] = j >= n ? -__builtin_inff() : is_bf16 ? bf2f(h[j]) : f[j];
   }
 }
-__device__ __forceinline__ void load4(const bf16* q, int n, float* x) {
-  if (n >= 4) {
-    const u16x4u a = *reinterpret_cast<const u16x4u*>(q);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = __uint_as_float((uint32_t)a[j] << 16);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = j < n ? bf2f(q[j]) : -__builtin_inff();
-  }
-}
-__device__ __forceinline__ void store4(float* q, int n, const float* x) {
-  if (n >= 4) {
-    *reinterpret_cast<f32x4u*>(q) = f32x4u{x[0], x[1], x[2], x[3]};
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) if (j < n) q[j] = x[j];
-  }
-}
-__device__ __forceinline__ void store4(bf16* q, int n, const float* x) {
-  if (n >= 4) {
+__device__ __forceinline__ void store4(void* row, bool is_bf16, int64_t i, int n, const float* x) {
+  float* f = (float*)row + i;
+  bf16* h = (bf16*)row + i;
+  if (n >= 4 && is_bf16) {
     u16x4u a;
 #pragma unroll
     for (int j = 0; j < 4; ++j) a[j] = __builtin_bit_cast(uint16_t, f2bf(x[j]));
-    *reinterpret_cast<u16x4u*>(q) = a;
+    *reinterpret_cast<u16x4u*>(h) = a;
+  } else if (n >= 4) {
+    *reinterpret_cast<f32x4u*>(f) = f32x4u{x[0], x[1], x[2], x[3]};
   } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) if (j < n) q[j] = f2bf(x[j]);
+    for (int j = 0; j < 4; ++j)
+      if (j < n) {
+        if (is_bf16) h[j] = f2bf(x[j]); else f[j] = x[j];
+      }
   }
 }
-template <typename T> __device__ __forceinline__ float to_f32(T x) { return (float)x; }
+__device__ __forceinline__ float load1(const void* row, bool is_bf16, int64_t i) {
+  return is_bf16 ? bf2f(((const bf16*)row)[i]) : ((const float*)row)[i];
+}
 
 // Expert of a lane's value j: groups of four consecutive experts are dealt to the lanes in turn, so that
 // a load of the row is contiguous; a lane's experts ascend with j.
@@ -98,20 +120,16 @@ template <int LANES> __device__ __forceinline__ int expert_of(int j, int lane) {
 
 // Floats as unsigned integers of the same order; 0 is left for what cannot be chosen (-inf, NaN, none).
 __device__ __forceinline__ uint32_t order_key(float c) {
-  if (!(c > -__builtin_inff())) return 0;
-  const uint32_t b = __float_as_uint(c + 0.f);     // -0 counts as 0
-  return (int)b < 0 ? ~b : b | 0x80000000u;
+  const uint32_t b = __float_as_uint(c);           // no -0: a score, or a sum of one with a bias
+  return c > -__builtin_inff() ? b ^ ((uint32_t)((int)b >> 31) | 0x80000000u) : 0u;
 }
 __device__ __forceinline__ float key_value(uint32_t k) {
   return __uint_as_float((int)k < 0 ? k & 0x7FFFFFFFu : ~k);
 }
 
-// The score of a logit; top and total: the row's largest logit and its sum of exponentials (softmax). The
-// sum is taken in 64 bits: an expert's score must not depend on the order of the others.
+// A row's largest logit and its sum of exponentials (softmax). The sum is taken in 64 bits: an expert's
+// score must not depend on the order of the others.
 struct Row { float top, total; };
-__device__ __forceinline__ float score(float l, const Row& r, int sigmoid) {
-  return sigmoid ? 1.f / (1.f + expf(-l)) : expf(l - r.top) / r.total;
-}
 template <int LANES, int V> __device__ __forceinline__ Row softmax_row(const float (&l)[V]) {
   Row r;
   float top = l[0];
@@ -123,6 +141,51 @@ template <int LANES, int V> __device__ __forceinline__ Row softmax_row(const flo
   for (int j = 0; j < V; ++j) sum += (double)expf(l[j] - r.top);
   r.total = (float)sum_of<LANES>(sum);
   return r;
+}
+__device__ __forceinline__ float score(float l, const Row& r, int sigmoid) {
+  return sigmoid ? 1.f / (1.f + expf(-l)) : expf(l - r.top) / r.total;
+}
+// The same scores, to the bit, of all of a lane's logits. The quotients are rounded correctly without the
+// division's scaling. 1 / d with d from 1 to 2^100: one Newton step on the hardware's reciprocal (compared
+// for every such d). e / d with e from 2^-78: the correctly rounded reciprocal's product and one step on its
+// remainder (Markstein 1990). Lanes with other values divide.
+template <int V> __device__ __forceinline__ void scores(const float (&l)[V], const Row& r, int sigmoid, float (&s)[V]) {
+  if (sigmoid) {
+    float most = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      s[j] = expf(-l[j]);
+      most = fmaxf(most, s[j]);
+    }
+    if (most < 0x1p99f) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float d = 1.f + s[j], y = __builtin_amdgcn_rcpf(d);
+        s[j] = fmaf(fmaf(-d, y, 1.f), y, y);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) s[j] = 1.f / (1.f + s[j]);
+    }
+  } else {
+    uint32_t least = 0xFFFFFFFFu;       // of the exponentials that are not zero, their bits less 1
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      s[j] = expf(l[j] - r.top);
+      least = min(least, __float_as_uint(s[j]) - 1u);
+    }
+    if (least >= 0x18800000u - 1u) {    // 2^-78
+      const float y = 1.f / r.total;
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float q = s[j] * y;
+        s[j] = fmaf(fmaf(-q, r.total, s[j]), y, q);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) s[j] = s[j] / r.total;
+    }
+  }
 }
 
 // u_j of the chosen experts, one a lane (lanes without one: there = false): the score itself, or its share
@@ -138,80 +201,177 @@ template <int LANES> __device__ __forceinline__ float chosen_share(float l, bool
   return total > 0.f ? u / total : 0.f;
 }
 
-// LANES lanes take one token, V experts each. A workgroup walks over its tokens and counts the experts'
-// tokens in LDS; whole numbers, so the order of the atomic additions does not change them.
-template <typename T, int LANES, int V, bool GROUPS>
-__global__ __launch_bounds__(256) void k_route(RouteParams p) {
-  constexpr int TOK = 256 / LANES;      // tokens of a workgroup at a time
-  __shared__ uint32_t hist[LANES * V];
-  __shared__ uint32_t rowkey[GROUPS ? TOK * LANES * V : 1];
-  __shared__ uint32_t groupkey[GROUPS ? TOK * ROUTE_MAX_GROUPS : 1];
-  const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
-  if (p.counts)
-    for (int e = threadIdx.x; e < LANES * V; e += 256) hist[e] = 0;
-  __syncthreads();
-  for (int64_t t0 = (int64_t)blockIdx.x * TOK; t0 < p.tokens; t0 += (int64_t)gridDim.x * TOK) {
-    const int64_t t = t0 + slot;
-    const bool live = t < p.tokens && !(p.mask && !p.mask[t]);
-    const T* row = (const T*)p.logits + (t < p.tokens ? t : 0) * p.ld;
-    float l[V];
+// ---- selection. A candidate is a positive double that orders as (key, lowest index first): key / 2 above
+// 2^31 key - index - 1 below; the upper half is 0 for what cannot be chosen. (Keys of numbers and infinity
+// stay under the doubles' infinity.) One instruction then compares and moves key and index together.
+__device__ __forceinline__ double candidate(uint32_t key, int e) {
+  return __builtin_bit_cast(double, (uint64_t)(key >> 1) << 32 | (key << 31 | (0x7FFFFFFFu - (uint32_t)e)));
+}
+__device__ __forceinline__ int candidate_index(double d) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, d);
+  return b >> 32 ? (int)(0x7FFFFFFFu - ((uint32_t)b & 0x7FFFFFFFu)) : -1;
+}
+__device__ __forceinline__ void in_order(double& a, double& b) {
+  const double hi = fmax(a, b), lo = fmin(a, b);
+  a = hi;
+  b = lo;
+}
+// d[B .. B + N) in falling order: Batcher's odd-even merge sort.
+template <int B, int N, int V> __device__ __forceinline__ void sort_falling(double (&d)[V]) {
 #pragma unroll
-    for (int j = 0; j < V; j += 4) load4(row + expert_of<LANES>(j, lane), p.E - expert_of<LANES>(j, lane), l + j);
-    Row r = {0.f, 1.f};
-    if (!p.sigmoid) r = softmax_row<LANES, V>(l);
-    uint32_t key[V];
+  for (int p = 1; p < N; p *= 2)
+#pragma unroll
+    for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+      for (int j = k % p; j + k < N; j += 2 * k)
+#pragma unroll
+        for (int i = 0; i < k; ++i)
+          if (i + j + k < N && (i + j) / (2 * p) == (i + j + k) / (2 * p)) in_order(d[B + i + j], d[B + i + j + k]);
+}
+// The largest DEP of d, falling, in d[0 .. DEP).
+template <int DEP, int V> __device__ __forceinline__ void best_falling(double (&d)[V]) {
+  if (DEP == V) {
+    sort_falling<0, V>(d);
+  } else {              // two sorted halves: the larger of each and its mirror, a bitonic run, then merged
+    static_assert(DEP == V || 2 * DEP == V);
+    sort_falling<0, V / 2>(d);
+    sort_falling<V / 2, V / 2>(d);
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) d[j] = fmax(d[j], d[V - 1 - j]);
+#pragma unroll
+    for (int k = V / 4; k >= 1; k /= 2)
+#pragma unroll
+      for (int j = 0; j < V / 2; ++j)
+        if (!(j & k)) in_order(d[j], d[j + k]);
+  }
+}
+
+// Keys of experts outside the kept groups become 0. The two best keys of a group: where a group is 4, 8, .. 64
+// consecutive experts (EVEN) they are found across the lanes that hold it, else by one lane in LDS. A group
+// counts with its best, or the sum of the two best (what cannot be chosen adds nothing).
+template <int LANES, int V, bool EVEN>
+__device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const RouteParams& p, uint32_t* rk, uint64_t* gk, int lane) {
+  auto value = [&](uint32_t best, uint32_t next) {
+    return p.group_best == 2 && next ? order_key(key_value(best) + key_value(next)) : best;
+  };
+  uint64_t mine[V / 4];         // (key, lowest index first) of the group of each four of a lane's experts
+  if (EVEN) {
+    const int span = (int)p.group_size / 4;       // lanes of a group
+#pragma unroll
+    for (int c = 0; c < V / 4; ++c) {
+      const uint32_t* k = key + 4 * c;
+      const uint32_t b0 = max(k[0], k[1]), b1 = max(k[2], k[3]);
+      uint32_t best = max(b0, b1), next = max(min(b0, b1), max(min(k[0], k[1]), min(k[2], k[3])));
+      auto with = [&](uint32_t ob, uint32_t on) {
+        next = max(min(best, ob), max(next, on));
+        best = max(best, ob);
+      };
+      if (span > 1) with(dpp<0xB1>(best), dpp<0xB1>(next));
+      if (span > 2) with(dpp<0x4E>(best), dpp<0x4E>(next));
+      if (span > 4) with(dpp<0x141>(best), dpp<0x141>(next));
+      if (span > 8) with(dpp<0x140>(best), dpp<0x140>(next));
+      const int g = (c * 4 * LANES + lane * 4) / 4 / span;
+      mine[c] = (uint64_t)value(best, next) << 32 | (uint32_t)(ROUTE_MAX_GROUPS - 1 - g);
+      if (g < p.groups && lane % span == 0) gk[g] = mine[c];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < V / 4; ++c) {
+      int rank = 0;
+      for (int q = 0; q < p.groups; ++q) rank += gk[q] > mine[c];
+      if (rank >= p.top_groups)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) key[4 * c + j] = 0;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) rk[expert_of<LANES>(j, lane)] = key[j];
+    __syncthreads();
+    for (int g = lane; g < p.groups; g += LANES) {
+      uint32_t best = 0, next = 0;
+      for (uint32_t q = 0; q < p.group_size; ++q) {
+        const uint32_t k = rk[g * p.group_size + q];
+        next = max(next, min(best, k));
+        best = max(best, k);
+      }
+      gk[g] = (uint64_t)value(best, next) << 32 | (uint32_t)(ROUTE_MAX_GROUPS - 1 - g);
+    }
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const int e = expert_of<LANES>(j, lane);
-      float c = score(l[j], r, p.sigmoid);
-      if (p.bias && e < p.E) c += p.bias[e];
-      key[j] = live && e < p.E ? order_key(c) : 0u;
-    }
-    if (GROUPS) {
-      uint32_t* rk = rowkey + slot * (LANES * V);
-      uint32_t* gk = groupkey + slot * ROUTE_MAX_GROUPS;
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < V; ++j) rk[expert_of<LANES>(j, lane)] = key[j];
-      __syncthreads();
-      for (int g = lane; g < p.groups; g += LANES) {
-        uint32_t best = 0, next = 0;
-        for (uint32_t q = 0; q < p.group_size; ++q) {
-          const uint32_t k = rk[g * p.group_size + q];
-          next = max(next, min(best, k));
-          best = max(best, k);
-        }
-        // the sum of the two best (what cannot be chosen adds nothing), or the best
-        gk[g] = p.group_best == 2 && next ? order_key(key_value(best) + key_value(next)) : best;
-      }
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const int e = expert_of<LANES>(j, lane);
-        if (e < p.E && key[j]) {
-          const int g = (int)(((uint32_t)e * p.group_inv) >> 20);
-          const uint32_t mine = gk[g];
-          int rank = 0;
-          for (int q = 0; q < p.groups; ++q) rank += gk[q] > mine || (gk[q] == mine && q < g);
-          if (rank >= p.top_groups) key[j] = 0;
-        }
+      if (key[j]) {
+        const uint64_t own = gk[((uint32_t)e * p.group_inv) >> 20];
+        int rank = 0;
+        for (int q = 0; q < p.groups; ++q) rank += gk[q] > own;
+        if (rank >= p.top_groups) key[j] = 0;
       }
     }
-    int chosen = -1;      // of lane i < k: the token's i-th expert
+  }
+  __syncthreads();      // the keys in LDS are read before the next token's are written
+}
+
+// LANES lanes take one token, V experts each. Bound by its arithmetic: the exponentials (about 20
+// instructions each), then the choice. Every lane sorts its own candidates; the token's next expert is the
+// largest of the lanes' heads, whose lane moves up. (Scanning all candidates for each of the k experts
+// took 42 us of the 56 with 256 experts.) A workgroup of 64 or 16 tokens counts the experts' tokens in LDS
+// and adds them to the counts at its end: an address takes an addition in about 20 ns, so at most 256
+// workgroups walk over the tokens (with 1024 the counts cost 20 us of 26 for 16384 tokens, 64 experts).
+// They are whole numbers: the order of the additions does not change them.
+enum { NO_GROUPS, EVEN_GROUPS, ANY_GROUPS };
+constexpr int ROUTE_THREADS = 1024;
+template <int LANES, int V, int DEP, int GROUPS>
+__global__ __launch_bounds__(ROUTE_THREADS) void k_route(RouteParams p) {
+  constexpr int TOK = ROUTE_THREADS / LANES;      // tokens of a workgroup at a time
+  __shared__ uint32_t hist[LANES * V];
+  __shared__ uint32_t rowkey[GROUPS == ANY_GROUPS ? TOK * LANES * V : 1];
+  __shared__ uint64_t groupkey[GROUPS != NO_GROUPS ? TOK * ROUTE_MAX_GROUPS : 1];
+  const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
+  const bool half = p.bf16;
+  float bias[V];        // what a lane's experts' scores are raised by; -inf for those that do not exist
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int e = expert_of<LANES>(j, lane);
+    bias[j] = e >= p.E ? -__builtin_inff() : p.bias ? p.bias[e] : 0.f;
+  }
+  if (p.counts) {
+    for (int e = threadIdx.x; e < LANES * V; e += ROUTE_THREADS) hist[e] = 0;
+    __syncthreads();
+  }
+  for (int64_t t0 = (int64_t)blockIdx.x * TOK; t0 < p.tokens; t0 += (int64_t)gridDim.x * TOK) {
+    const int64_t t = t0 + slot, row = (t < p.tokens ? t : 0) * p.ld;
+    const bool live = t < p.tokens && !(p.mask && !p.mask[t]);
+    float l[V], s[V];
+#pragma unroll
+    for (int j = 0; j < V; j += 4) {
+      const int e = expert_of<LANES>(j, lane);
+      load4(p.logits, half, row + e, p.E - e, l + j);
+    }
+    Row r = {0.f, 1.f};
+    if (!p.sigmoid) r = softmax_row<LANES, V>(l);
+    scores<V>(l, r, p.sigmoid, s);
+    uint32_t key[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) key[j] = order_key(s[j] + bias[j]);
+    if (GROUPS != NO_GROUPS)
+      keep_groups<LANES, V, GROUPS == EVEN_GROUPS>(key, p, rowkey + (GROUPS == ANY_GROUPS ? slot * (LANES * V) : 0),
+                                                   groupkey + slot * ROUTE_MAX_GROUPS, lane);
+    double d[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) d[j] = candidate(key[j], expert_of<LANES>(j, lane));
+    best_falling<DEP>(d);
+    double own = 0;       // of lane i < k: the token's i-th expert
     for (int i = 0; i < p.k; ++i) {
-      uint32_t best = 0, at = 0xFFFFFFFFu;
+      const double top = max_of<LANES>(d[0]);
+      const bool up = d[0] == top;
 #pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (key[j] > best) { best = key[j]; at = (uint32_t)expert_of<LANES>(j, lane); }
-      const uint32_t top = max_of<LANES>(best);
-      at = min_of<LANES>(top && best == top ? at : 0xFFFFFFFFu);
-#pragma unroll
-      for (int j = 0; j < V; ++j)
-        if ((uint32_t)expert_of<LANES>(j, lane) == at) key[j] = 0;
-      if (lane == i) chosen = (int)at;
+      for (int j = 0; j + 1 < DEP; ++j) d[j] = up ? d[j + 1] : d[j];
+      d[DEP - 1] = up ? 0.0 : d[DEP - 1];
+      own = lane == i ? top : own;
     }
+    const int chosen = live ? candidate_index(own) : -1;
     const bool there = chosen >= 0;
-    const float u = chosen_share<LANES>(there ? to_f32(row[chosen]) : 0.f, there, r, p);
+    const float u = chosen_share<LANES>(there ? load1(p.logits, half, row + chosen) : 0.f, there, r, p);
     if (lane < p.k && t < p.tokens) {
       p.index[t * p.k + lane] = chosen;
       p.weight[t * p.k + lane] = u * p.scale;
@@ -220,7 +380,7 @@ __global__ __launch_bounds__(256) void k_route(RouteParams p) {
   }
   if (!p.counts) return;
   __syncthreads();
-  for (int e = threadIdx.x; e < p.E; e += 256)
+  for (int e = threadIdx.x; e < p.E; e += ROUTE_THREADS)
     if (hist[e]) atomicAdd(&p.counts[e], (unsigned long long)hist[e]);
 }
 
@@ -228,26 +388,30 @@ __global__ __launch_bounds__(256) void k_route(RouteParams p) {
 // renormalised, t_j = u_j (dw_j - sum dw u) and d l_j = t_j, times 1 - s_j for the sigmoid (the softmax's own
 // sum vanishes); else t_j = dw_j s_j, times 1 - s_j for the sigmoid, and d l_e = t_e - s_e sum t for the softmax,
 // the only form that needs the whole row.
-template <typename T, int LANES, int V>
+template <int LANES, int V>
 __global__ __launch_bounds__(256) void k_route_backward(RouteParams p) {
   constexpr int TOK = 256 / LANES;
   __shared__ float out[TOK * LANES * V];
   const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
-  const bool whole = !p.sigmoid && !p.renorm;
+  const bool whole = !p.sigmoid && !p.renorm, half = p.bf16;
   for (int64_t t0 = (int64_t)blockIdx.x * TOK; t0 < p.tokens; t0 += (int64_t)gridDim.x * TOK) {
     const int64_t t = t0 + slot;
     const bool in = t < p.tokens;
-    const T* row = (const T*)p.logits + (in ? t : 0) * p.ld;
+    const int64_t row = (in ? t : 0) * p.ld;
     const int chosen = in && lane < p.k ? p.index[t * p.k + lane] : -1;
     const bool there = chosen >= 0 && chosen < p.E;
     const float dw = there ? p.weight[t * p.k + lane] : 0.f;
-    const float lc = there ? to_f32(row[chosen]) : 0.f;
-    float l[V];
+    const float lc = there ? load1(p.logits, half, row + chosen) : 0.f;
+    float l[V], s[V];
     Row r = {0.f, 1.f};
     if (whole) {
 #pragma unroll
-      for (int j = 0; j < V; j += 4) load4(row + expert_of<LANES>(j, lane), p.E - expert_of<LANES>(j, lane), l + j);
+      for (int j = 0; j < V; j += 4) {
+        const int e = expert_of<LANES>(j, lane);
+        load4(p.logits, half, row + e, p.E - e, l + j);
+      }
       r = softmax_row<LANES, V>(l);
+      scores<V>(l, r, 0, s);
     }
     const float u = chosen_share<LANES>(lc, there, r, p);
     const float mean = p.renorm ? sum_of<LANES>(dw * u) : 0.f;
@@ -258,17 +422,15 @@ __global__ __launch_bounds__(256) void k_route_backward(RouteParams p) {
     float* o = out + slot * (LANES * V);
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-      o[expert_of<LANES>(j, lane)] = whole && any ? -score(l[j], r, 0) * total : 0.f;
+    for (int j = 0; j < V; ++j) o[expert_of<LANES>(j, lane)] = whole && any ? -s[j] * total : 0.f;
     __syncthreads();
     if (there) o[chosen] += d;
     __syncthreads();
     if (in) {
-      T* q = (T*)p.grad + t * p.E;
 #pragma unroll
       for (int j = 0; j < V; j += 4) {
         const int e = expert_of<LANES>(j, lane);
-        store4(q + e, p.E - e, o + e);
+        store4(p.grad, half, t * p.E + e, p.E - e, o + e);
       }
     }
   }
@@ -291,35 +453,50 @@ __global__ __launch_bounds__(256) void k_route_balance(int E, long long* __restr
   }
 }
 
-template <typename T> hipError_t route(const RouteParams& p, bool backward, hipStream_t st) {
-  const bool wide = p.k > 16 || p.E > 256;
-  const int tok = wide ? 4 : 16;
-  const int64_t wgs = (p.tokens + tok - 1) / tok;
-  const dim3 g((uint32_t)(wgs < 1024 ? wgs : 1024)), b(256);
-#define ROUTE(LANES, V)                                                                               \
-  do {                                                                                                \
-    if (backward) hipLaunchKernelGGL((k_route_backward<T, LANES, V>), g, b, 0, st, p);                \
-    else if (p.groups > 1) hipLaunchKernelGGL((k_route<T, LANES, V, true>), g, b, 0, st, p);          \
-    else hipLaunchKernelGGL((k_route<T, LANES, V, false>), g, b, 0, st, p);                           \
-  } while (0)
-  if (!wide && p.E <= 64) ROUTE(16, 4);
-  else if (!wide && p.E <= 128) ROUTE(16, 8);
-  else if (!wide) ROUTE(16, 16);
-  else if (p.E <= 256) ROUTE(64, 4);
-  else if (p.E <= 512) ROUTE(64, 8);
-  else ROUTE(64, 16);
-#undef ROUTE
-  return hipGetLastError();
+// Sixteen lanes hold up to 256 experts and 16 choices of a token, a wave what is more.
+bool wide(const RouteParams& p) { return p.k > 16 || p.E > 256; }
+int64_t workgroups(const RouteParams& p, int threads, int64_t most) {
+  const int64_t tok = threads / (wide(p) ? 64 : 16), n = (p.tokens + tok - 1) / tok;
+  return n < most ? n : most;
 }
 
 }  // namespace
 
 hipError_t launch_route(const RouteParams& p, hipStream_t st) {
-  return p.bf16 ? route<bf16>(p, false, st) : route<float>(p, false, st);
+  const dim3 g((uint32_t)workgroups(p, ROUTE_THREADS, 256)), b(ROUTE_THREADS);
+  const int s = (int)p.group_size;
+  const int groups = p.groups == 1 ? NO_GROUPS : s >= 4 && s <= 64 && (s & (s - 1)) == 0 ? EVEN_GROUPS : ANY_GROUPS;
+#define ROUTE(LANES, V, DEP)                                                                                     \
+  do {                                                                                                           \
+    if (groups == NO_GROUPS) hipLaunchKernelGGL((k_route<LANES, V, DEP, NO_GROUPS>), g, b, 0, st, p);            \
+    else if (groups == EVEN_GROUPS) hipLaunchKernelGGL((k_route<LANES, V, DEP, EVEN_GROUPS>), g, b, 0, st, p);   \
+    else hipLaunchKernelGGL((k_route<LANES, V, DEP, ANY_GROUPS>), g, b, 0, st, p);                               \
+  } while (0)
+  const bool w = wide(p), few = p.k <= 8;       // few: a lane's best eight are enough
+  if (!w && p.E <= 64) ROUTE(16, 4, 4);
+  else if (!w && p.E <= 128) ROUTE(16, 8, 8);
+  else if (!w && few) ROUTE(16, 16, 8);
+  else if (!w) ROUTE(16, 16, 16);
+  else if (p.E <= 256) ROUTE(64, 4, 4);
+  else if (p.E <= 512) ROUTE(64, 8, 8);
+  else if (few) ROUTE(64, 16, 8);
+  else ROUTE(64, 16, 16);
+#undef ROUTE
+  return hipGetLastError();
 }
+
 hipError_t launch_route_backward(const RouteParams& p, hipStream_t st) {
-  return p.bf16 ? route<bf16>(p, true, st) : route<float>(p, true, st);
+  const dim3 g((uint32_t)workgroups(p, 256, 1024)), b(256);
+  const bool w = wide(p);
+  if (!w && p.E <= 64) hipLaunchKernelGGL((k_route_backward<16, 4>), g, b, 0, st, p);
+  else if (!w && p.E <= 128) hipLaunchKernelGGL((k_route_backward<16, 8>), g, b, 0, st, p);
+  else if (!w) hipLaunchKernelGGL((k_route_backward<16, 16>), g, b, 0, st, p);
+  else if (p.E <= 256) hipLaunchKernelGGL((k_route_backward<64, 4>), g, b, 0, st, p);
+  else if (p.E <= 512) hipLaunchKernelGGL((k_route_backward<64, 8>), g, b, 0, st, p);
+  else hipLaunchKernelGGL((k_route_backward<64, 16>), g, b, 0, st, p);
+  return hipGetLastError();
 }
+
 hipError_t launch_route_balance(int E, long long* counts, float* bias, float rate, hipStream_t st) {
   hipLaunchKernelGGL(k_route_balance, dim3(1), dim3(256), 0, st, E, counts, bias, rate);
   return hipGetLastError();

@@ -649,8 +649,8 @@ def moara_route(cfg: moara_route_config, logits, bias=None, mask=None, counts=No
     b = None if bias is None else _vector(bias, dev, torch.float32, cfg.experts, "bias")
     m = None if mask is None else _vector(mask, dev, torch.uint8, tokens, "mask")
     c = None if counts is None else _vector(counts, dev, torch.int64, cfg.experts, "counts")
-    index = torch.empty((tokens, cfg.top_k), dtype=torch.int32, device=logits.device)
-    weight = torch.empty((tokens, cfg.top_k), dtype=torch.float32, device=logits.device)
+    index = logits.new_empty((tokens, cfg.top_k), dtype=torch.int32)
+    weight = torch.empty_like(index, dtype=torch.float32)
     _call(dev, stream, lib().moara_route, ctypes.byref(cfg), logits.data_ptr(), tokens, ld, b, m, index.data_ptr(),
           weight.data_ptr(), c)
     return index, weight
@@ -663,7 +663,7 @@ def moara_route_backward(cfg: moara_route_config, logits, index, grad_weight, st
     dev, tokens, ld = _route_logits(cfg, logits)
     i = _vector(index, dev, torch.int32, tokens * cfg.top_k, "index")
     w = _vector(grad_weight, dev, torch.float32, tokens * cfg.top_k, "grad_weight")
-    grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    grad = torch.empty_like(logits, memory_format=torch.contiguous_format)
     _call(dev, stream, lib().moara_route_backward, ctypes.byref(cfg), logits.data_ptr(), tokens, ld, i, w, grad.data_ptr())
     return grad
 
