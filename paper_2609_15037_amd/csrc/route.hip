@@ -12,7 +12,7 @@ typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 // ---- reductions over the LANES (16 or 64) lanes of a token; every lane gets the result. Sixteen lanes are
 // one row of the cross-lane data path: neighbours, neighbouring pairs, mirrored halves and rows.
 template <int CTRL> __device__ __forceinline__ uint32_t dpp(uint32_t x) {
-  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false);
+  return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xF, 0xF, true);     // every lane has its source
 }
 template <int CTRL> __device__ __forceinline__ float dpp(float x) {
   return __uint_as_float(dpp<CTRL>(__float_as_uint(x)));
@@ -61,9 +61,6 @@ template <int LANES> __device__ __forceinline__ float sum_of(float x) {
 }
 template <int LANES> __device__ __forceinline__ double sum_of(double x) {
   return reduce<LANES>(x, [](double a, double b) { return a + b; });
-}
-template <int LANES> __device__ __forceinline__ double max_of(double x) {
-  return reduce<LANES>(x, [](double a, double b) { return fmax(a, b); });
 }
 template <int LANES> __device__ __forceinline__ float max_of(float x) {
   return reduce<LANES>(x, [](float a, float b) { return fmaxf(a, b); });
@@ -203,13 +200,10 @@ template <int LANES> __device__ __forceinline__ float chosen_share(float l, bool
 
 // ---- selection. A candidate is a positive double that orders as (key, lowest index first): key / 2 above
 // 2^31 key - index - 1 below; the upper half is 0 for what cannot be chosen. (Keys of numbers and infinity
-// stay under the doubles' infinity.) One instruction then compares and moves key and index together.
+// stay under the doubles' infinity.) One instruction then compares and moves key and index together. For the
+// lanes' heads, two rounds on 32 bits, whose moves and comparisons are one instruction, are shorter again.
 __device__ __forceinline__ double candidate(uint32_t key, int e) {
   return __builtin_bit_cast(double, (uint64_t)(key >> 1) << 32 | (key << 31 | (0x7FFFFFFFu - (uint32_t)e)));
-}
-__device__ __forceinline__ int candidate_index(double d) {
-  const uint64_t b = __builtin_bit_cast(uint64_t, d);
-  return b >> 32 ? (int)(0x7FFFFFFFu - ((uint32_t)b & 0x7FFFFFFFu)) : -1;
 }
 __device__ __forceinline__ void in_order(double& a, double& b) {
   const double hi = fmax(a, b), lo = fmin(a, b);
@@ -360,16 +354,27 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_route(RouteParams p) {
 #pragma unroll
     for (int j = 0; j < V; ++j) d[j] = candidate(key[j], expert_of<LANES>(j, lane));
     best_falling<DEP>(d);
-    double own = 0;       // of lane i < k: the token's i-th expert
-    for (int i = 0; i < p.k; ++i) {
-      const double top = max_of<LANES>(d[0]);
-      const bool up = d[0] == top;
+    uint32_t hi[DEP], lo[DEP];
 #pragma unroll
-      for (int j = 0; j + 1 < DEP; ++j) d[j] = up ? d[j + 1] : d[j];
-      d[DEP - 1] = up ? 0.0 : d[DEP - 1];
-      own = lane == i ? top : own;
+    for (int j = 0; j < DEP; ++j) {
+      hi[j] = (uint32_t)(__builtin_bit_cast(uint64_t, d[j]) >> 32);
+      lo[j] = (uint32_t)__builtin_bit_cast(uint64_t, d[j]);
     }
-    const int chosen = live ? candidate_index(own) : -1;
+    uint32_t own = 0;     // of lane i < k: 2^31 - 1 less the token's i-th expert, in 31 bits; 0 where there is none
+    for (int i = 0; i < p.k; ++i) {
+      const uint32_t th = max_of<LANES>(hi[0]), head = hi[0] == th ? lo[0] : 0u, tl = max_of<LANES>(head);
+      const bool up = head == tl;
+      // the + makes values of the operands: of two elements of an array the choice would be an index
+#pragma unroll
+      for (int j = 0; j + 1 < DEP; ++j) {
+        hi[j] = up ? +hi[j + 1] : +hi[j];
+        lo[j] = up ? +lo[j + 1] : +lo[j];
+      }
+      hi[DEP - 1] = up ? 0u : +hi[DEP - 1];
+      lo[DEP - 1] = up ? 0u : +lo[DEP - 1];
+      if (lane == i) own = th ? tl & 0x7FFFFFFFu : 0u;
+    }
+    const int chosen = live && own ? (int)(0x7FFFFFFFu - own) : -1;
     const bool there = chosen >= 0;
     const float u = chosen_share<LANES>(there ? load1(p.logits, half, row + chosen) : 0.f, there, r, p);
     if (lane < p.k && t < p.tokens) {
