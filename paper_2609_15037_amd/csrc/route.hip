@@ -240,6 +240,12 @@ template <int DEP, int V> __device__ __forceinline__ void best_falling(double (&
   }
 }
 
+// Orders a wave's accesses to LDS: a token's lanes share a wave, what they exchange concerns no other.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // Keys of experts outside the kept groups become 0. The two best keys of a group: where a group is 4, 8, .. 64
 // consecutive experts (EVEN) they are found across the lanes that hold it, else by one lane in LDS. A group
 // counts with its best, or the sum of the two best (what cannot be chosen adds nothing).
@@ -250,7 +256,7 @@ __device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const RouteParam
   };
   uint64_t mine[V / 4];         // (key, lowest index first) of the group of each four of a lane's experts
   if (EVEN) {
-    const int span = (int)p.group_size / 4;       // lanes of a group
+    const int shift = __builtin_ctz(p.group_size) - 2, span = 1 << shift;       // lanes of a group
 #pragma unroll
     for (int c = 0; c < V / 4; ++c) {
       const uint32_t* k = key + 4 * c;
@@ -264,11 +270,11 @@ __device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const RouteParam
       if (span > 2) with(dpp<0x4E>(best), dpp<0x4E>(next));
       if (span > 4) with(dpp<0x141>(best), dpp<0x141>(next));
       if (span > 8) with(dpp<0x140>(best), dpp<0x140>(next));
-      const int g = (c * 4 * LANES + lane * 4) / 4 / span;
+      const int g = (c * LANES + lane) >> shift;
       mine[c] = (uint64_t)value(best, next) << 32 | (uint32_t)(ROUTE_MAX_GROUPS - 1 - g);
-      if (g < p.groups && lane % span == 0) gk[g] = mine[c];
+      if (g < p.groups && !(lane & (span - 1))) gk[g] = mine[c];
     }
-    __syncthreads();
+    wave_sync();
 #pragma unroll
     for (int c = 0; c < V / 4; ++c) {
       int rank = 0;
@@ -280,7 +286,7 @@ __device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const RouteParam
   } else {
 #pragma unroll
     for (int j = 0; j < V; ++j) rk[expert_of<LANES>(j, lane)] = key[j];
-    __syncthreads();
+    wave_sync();
     for (int g = lane; g < p.groups; g += LANES) {
       uint32_t best = 0, next = 0;
       for (uint32_t q = 0; q < p.group_size; ++q) {
@@ -290,7 +296,7 @@ __device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const RouteParam
       }
       gk[g] = (uint64_t)value(best, next) << 32 | (uint32_t)(ROUTE_MAX_GROUPS - 1 - g);
     }
-    __syncthreads();
+    wave_sync();
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const int e = expert_of<LANES>(j, lane);
@@ -302,7 +308,7 @@ __device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const RouteParam
       }
     }
   }
-  __syncthreads();      // the keys in LDS are read before the next token's are written
+  wave_sync();          // the keys in LDS are read before the next token's are written
 }
 
 // LANES lanes take one token, V experts each. Bound by its arithmetic: the exponentials (about 20
@@ -318,35 +324,38 @@ template <int LANES, int V, int DEP, int GROUPS>
 __global__ __launch_bounds__(ROUTE_THREADS) void k_route(RouteParams p) {
   constexpr int TOK = ROUTE_THREADS / LANES;      // tokens of a workgroup at a time
   __shared__ uint32_t hist[LANES * V];
+  __shared__ float bias[LANES * V];     // what scores are raised by; -inf for experts that do not exist
   __shared__ uint32_t rowkey[GROUPS == ANY_GROUPS ? TOK * LANES * V : 1];
   __shared__ uint64_t groupkey[GROUPS != NO_GROUPS ? TOK * ROUTE_MAX_GROUPS : 1];
   const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
   const bool half = p.bf16;
-  float bias[V];        // what a lane's experts' scores are raised by; -inf for those that do not exist
-#pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const int e = expert_of<LANES>(j, lane);
-    bias[j] = e >= p.E ? -__builtin_inff() : p.bias ? p.bias[e] : 0.f;
+  for (int e = threadIdx.x; e < LANES * V; e += ROUTE_THREADS) {
+    hist[e] = 0;
+    bias[e] = e >= p.E ? -__builtin_inff() : p.bias ? p.bias[e] : 0.f;
   }
-  if (p.counts) {
-    for (int e = threadIdx.x; e < LANES * V; e += ROUTE_THREADS) hist[e] = 0;
-    __syncthreads();
-  }
-  for (int64_t t0 = (int64_t)blockIdx.x * TOK; t0 < p.tokens; t0 += (int64_t)gridDim.x * TOK) {
-    const int64_t t = t0 + slot, row = (t < p.tokens ? t : 0) * p.ld;
-    const bool live = t < p.tokens && !(p.mask && !p.mask[t]);
-    float l[V], s[V];
+  __syncthreads();
+  float l[V];
+  auto fetch = [&](int64_t t) {         // a token's logits, past the end another's
+    const int64_t row = (t < p.tokens ? t : 0) * p.ld;
 #pragma unroll
     for (int j = 0; j < V; j += 4) {
       const int e = expert_of<LANES>(j, lane);
       load4(p.logits, half, row + e, p.E - e, l + j);
     }
+  };
+  const int64_t step = (int64_t)gridDim.x * TOK;
+  fetch((int64_t)blockIdx.x * TOK + slot);
+  for (int64_t t = (int64_t)blockIdx.x * TOK + slot; t - slot < p.tokens; t += step) {
+    const int64_t row = (t < p.tokens ? t : 0) * p.ld;
+    const bool live = t < p.tokens && !(p.mask && !p.mask[t]);
+    float s[V];
     Row r = {0.f, 1.f};
     if (!p.sigmoid) r = softmax_row<LANES, V>(l);
     scores<V>(l, r, p.sigmoid, s);
+    if (t - slot + step < p.tokens) fetch(t + step);        // arrives during the choice
     uint32_t key[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) key[j] = order_key(s[j] + bias[j]);
+    for (int j = 0; j < V; ++j) key[j] = order_key(s[j] + bias[expert_of<LANES>(j, lane)]);
     if (GROUPS != NO_GROUPS)
       keep_groups<LANES, V, GROUPS == EVEN_GROUPS>(key, p, rowkey + (GROUPS == ANY_GROUPS ? slot * (LANES * V) : 0),
                                                    groupkey + slot * ROUTE_MAX_GROUPS, lane);
