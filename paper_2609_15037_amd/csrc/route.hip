@@ -9,7 +9,7 @@ namespace {
 typedef uint16_t u16x4u __attribute__((ext_vector_type(4), aligned(2)));
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 
-// ---- reductions over the LANES (16 or 64) lanes of a token; every lane gets the result. Sixteen lanes are
+// ---- reductions over the LANES (8, 16 or 64) lanes of a token; every lane gets the result. Sixteen lanes are
 // one row of the cross-lane data path: neighbours, neighbouring pairs, mirrored halves and rows.
 template <int CTRL> __device__ __forceinline__ uint32_t dpp(uint32_t x) {
   return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xF, 0xF, true);     // every lane has its source
@@ -46,7 +46,7 @@ template <int LANES, typename T, typename F> __device__ __forceinline__ T reduce
   x = f(x, dpp<0xB1>(x));     // lane ^ 1
   x = f(x, dpp<0x4E>(x));     // lane ^ 2
   x = f(x, dpp<0x141>(x));    // mirrored within eight lanes
-  x = f(x, dpp<0x140>(x));    // mirrored within sixteen
+  if (LANES >= 16) x = f(x, dpp<0x140>(x));     // mirrored within sixteen
   if (LANES == 64) {
     T a, b;
     rows_apart<16>(x, a, b);
@@ -269,7 +269,7 @@ __device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const RouteParam
       if (span > 1) with(dpp<0xB1>(best), dpp<0xB1>(next));
       if (span > 2) with(dpp<0x4E>(best), dpp<0x4E>(next));
       if (span > 4) with(dpp<0x141>(best), dpp<0x141>(next));
-      if (span > 8) with(dpp<0x140>(best), dpp<0x140>(next));
+      if (LANES >= 16 && span > 8) with(dpp<0x140>(best), dpp<0x140>(next));
       const int g = (c * LANES + lane) >> shift;
       mine[c] = (uint64_t)value(best, next) << 32 | (uint32_t)(ROUTE_MAX_GROUPS - 1 - g);
       if (g < p.groups && !(lane & (span - 1))) gk[g] = mine[c];
@@ -467,10 +467,10 @@ __global__ __launch_bounds__(256) void k_route_balance(int E, long long* __restr
   }
 }
 
-// Sixteen lanes hold up to 256 experts and 16 choices of a token, a wave what is more.
-bool wide(const RouteParams& p) { return p.k > 16 || p.E > 256; }
+// Eight lanes hold up to 32 experts and 8 choices of a token, sixteen up to 256 and 16, a wave what is more.
+int lanes_of(const RouteParams& p) { return p.k > 16 || p.E > 256 ? 64 : p.k > 8 || p.E > 32 ? 16 : 8; }
 int64_t workgroups(const RouteParams& p, int threads, int64_t most) {
-  const int64_t tok = threads / (wide(p) ? 64 : 16), n = (p.tokens + tok - 1) / tok;
+  const int64_t tok = threads / lanes_of(p), n = (p.tokens + tok - 1) / tok;
   return n < most ? n : most;
 }
 
@@ -486,8 +486,10 @@ hipError_t launch_route(const RouteParams& p, hipStream_t st) {
     else if (groups == EVEN_GROUPS) hipLaunchKernelGGL((k_route<LANES, V, DEP, EVEN_GROUPS>), g, b, 0, st, p);   \
     else hipLaunchKernelGGL((k_route<LANES, V, DEP, ANY_GROUPS>), g, b, 0, st, p);                               \
   } while (0)
-  const bool w = wide(p), few = p.k <= 8;       // few: a lane's best eight are enough
-  if (!w && p.E <= 64) ROUTE(16, 4, 4);
+  const int lanes = lanes_of(p);
+  const bool w = lanes == 64, few = p.k <= 8;   // few: a lane's best eight are enough
+  if (lanes == 8) ROUTE(8, 4, 4);
+  else if (!w && p.E <= 64) ROUTE(16, 4, 4);
   else if (!w && p.E <= 128) ROUTE(16, 8, 8);
   else if (!w && few) ROUTE(16, 16, 8);
   else if (!w) ROUTE(16, 16, 16);
@@ -501,8 +503,10 @@ hipError_t launch_route(const RouteParams& p, hipStream_t st) {
 
 hipError_t launch_route_backward(const RouteParams& p, hipStream_t st) {
   const dim3 g((uint32_t)workgroups(p, 256, 1024)), b(256);
-  const bool w = wide(p);
-  if (!w && p.E <= 64) hipLaunchKernelGGL((k_route_backward<16, 4>), g, b, 0, st, p);
+  const int lanes = lanes_of(p);
+  const bool w = lanes == 64;
+  if (lanes == 8) hipLaunchKernelGGL((k_route_backward<8, 4>), g, b, 0, st, p);
+  else if (!w && p.E <= 64) hipLaunchKernelGGL((k_route_backward<16, 4>), g, b, 0, st, p);
   else if (!w && p.E <= 128) hipLaunchKernelGGL((k_route_backward<16, 8>), g, b, 0, st, p);
   else if (!w) hipLaunchKernelGGL((k_route_backward<16, 16>), g, b, 0, st, p);
   else if (p.E <= 256) hipLaunchKernelGGL((k_route_backward<64, 4>), g, b, 0, st, p);

@@ -434,13 +434,17 @@ def moara_matrix_info(st: State, mat: int):
 _RECORDS = {t: np.dtype(t) for t in (moara_grad_tensor, moara_adamw_tensor)}
 
 
+_IDS: dict = {}
+
+
 def _dtype_id(t, what: str) -> int:
-    import torch
-    if t.dtype == torch.float32:
-        return MOARA_F32
-    if t.dtype == torch.bfloat16:
-        return MOARA_BF16
-    raise ValueError(f"{what}: need float32 or bfloat16, got {t.dtype}")
+    if not _IDS:
+        import torch
+        _IDS.update({torch.float32: MOARA_F32, torch.bfloat16: MOARA_BF16})
+    i = _IDS.get(t.dtype)
+    if i is None:
+        raise ValueError(f"{what}: need float32 or bfloat16, got {t.dtype}")
+    return i
 
 
 def _dense(t) -> bool:
@@ -452,17 +456,20 @@ def _dense(t) -> bool:
 
 
 def _on_gpu(t, device: Optional[int], what: str) -> int:
+    """The index of the GPU a strided tensor is on (the same as `device`, if given)."""
     import torch
-    if t.layout != torch.strided or not t.is_cuda:
+    d = t.get_device()      # -1 on the CPU
+    if d < 0 or t.layout is not torch.strided or not t.is_cuda:
         raise ValueError(f"{what}: need a strided CUDA tensor, got {t.layout} on {t.device}")
-    if device is not None and t.get_device() != device:
+    if device is not None and d != device:
         raise ValueError(f"{what} is on {t.device}, the others are on cuda:{device}")
-    return t.get_device()
+    return d
 
 
 def _vector(t, device, dtype, count, what: str) -> int:
     """Address of a contiguous tensor of that type and element count."""
-    _on_gpu(t, device, what)
+    if t.get_device() != device:
+        _on_gpu(t, device, what)
     if t.dtype != dtype or t.numel() != count or not t.is_contiguous():
         raise ValueError(f"{what}: need {count} contiguous elements of {dtype}, got {tuple(t.shape)} {t.dtype} "
                          f"contiguous={t.is_contiguous()}")
@@ -502,11 +509,11 @@ class GradArgs:
         """Other gradient tensors (on the same GPU) for the same workspace."""
         keep = [g for g in grads if g is not None]
         rows = []
-        for i, g in enumerate(keep):
-            self.device = _on_gpu(g, self.device, f"grads[{i}]")
-            if not _dense(g):
-                raise ValueError(f"grads[{i}]: strides {g.stride()} of shape {tuple(g.shape)} leave gaps")
-            rows.append((g.data_ptr(), g.numel(), _dtype_id(g, f"grads[{i}]"), 0))
+        for i, g in enumerate(keep):    # a model may have thousands: a few attribute reads each
+            self.device = _on_gpu(g, self.device, "a gradient")
+            if not g.is_contiguous() and not _dense(g):
+                raise ValueError(f"gradient {i}: strides {g.stride()} of shape {tuple(g.shape)} leave gaps")
+            rows.append((g.data_ptr(), g.numel(), _dtype_id(g, "a gradient"), 0))
         self.keep, self.rec = keep, np.array(rows, dtype=_RECORDS[moara_grad_tensor])
         self.ptr, self.n = self.rec.ctypes.data, len(rows)
 
@@ -524,12 +531,13 @@ def moara_grad_norm(grads, max_norm: float, out=None, stream=None, args: Optiona
     return out
 
 
-def moara_grad_scale(grads, coef, stream=None, args: Optional[GradArgs] = None):
+def moara_grad_scale(grads, coef, stream=None, args: Optional[GradArgs] = None, first: Optional[int] = None):
     """moara_grad_scale of the C ABI: the gradients times coef (a float32 tensor of one element on the
-    GPU), in place."""
+    GPU), in place. first: only so many of the list's tensors (None entries do not count)."""
     import torch
     a = GradArgs(grads) if args is None else args
-    _call(a.device, stream, lib().moara_grad_scale, a.ptr, a.n, _vector(coef, a.device, torch.float32, 1, "coef"))
+    n = a.n if first is None else min(int(first), a.n)
+    _call(a.device, stream, lib().moara_grad_scale, a.ptr, n, _vector(coef, a.device, torch.float32, 1, "coef"))
 
 
 def moara_adamw_default_config(**overrides) -> moara_adamw_config:
@@ -617,7 +625,7 @@ def moara_adamw_step(args: AdamWArgs, cfg: moara_adamw_config, lr, step, clip=No
     args.rec["step"] = step
     c = None if clip is None else _vector(clip, args.device, torch.float32, 1, "clip")
     if args.n:
-        _call(args.device, stream, lib().moara_adamw_step, ctypes.byref(cfg), args.ptr, args.n, c, seed & (2 ** 64 - 1))
+        _call(args.device, stream, lib().moara_adamw_step, cfg, args.ptr, args.n, c, seed & (2 ** 64 - 1))
 
 
 def moara_route_default_config(**overrides) -> moara_route_config:
@@ -629,13 +637,14 @@ def moara_route_default_config(**overrides) -> moara_route_config:
 
 
 def _route_logits(cfg, logits):
-    dev = _on_gpu(logits, None, "logits")
-    if logits.dim() != 2 or logits.shape[1] != cfg.experts or (logits.shape[1] > 1 and logits.stride(1) != 1):
+    """(GPU, tokens, row stride) of the logits, checked; cfg.logits_dtype follows them."""
+    shape, strides = logits.shape, logits.stride()
+    if len(shape) != 2 or shape[1] != cfg.experts or (shape[1] > 1 and strides[1] != 1):
         raise ValueError(f"logits: need tokens x {cfg.experts} with unit stride along the experts, got "
-                         f"{tuple(logits.shape)}, strides {logits.stride()}")
+                         f"{tuple(shape)}, strides {strides}")
     cfg.logits_dtype = _dtype_id(logits, "logits")
-    tokens = logits.shape[0]
-    return dev, tokens, (logits.stride(0) if tokens > 1 else cfg.experts)
+    tokens = shape[0]
+    return _on_gpu(logits, None, "logits"), tokens, (strides[0] if tokens > 1 else shape[1])
 
 
 def moara_route(cfg: moara_route_config, logits, bias=None, mask=None, counts=None, stream=None):
@@ -644,15 +653,16 @@ def moara_route(cfg: moara_route_config, logits, bias=None, mask=None, counts=No
     expert; mask: bool or uint8, one for each token; counts: int64, one for each expert, added to."""
     import torch
     dev, tokens, ld = _route_logits(cfg, logits)
-    if mask is not None and mask.dtype != torch.uint8:
-        mask = mask.view(torch.uint8) if mask.dtype == torch.bool else mask
-    b = None if bias is None else _vector(bias, dev, torch.float32, cfg.experts, "bias")
-    m = None if mask is None else _vector(mask, dev, torch.uint8, tokens, "mask")
-    c = None if counts is None else _vector(counts, dev, torch.int64, cfg.experts, "counts")
+    if bias is not None:
+        bias = _vector(bias, dev, torch.float32, cfg.experts, "bias")
+    if mask is not None:
+        mask = _vector(mask, dev, torch.bool if mask.dtype == torch.bool else torch.uint8, tokens, "mask")
+    if counts is not None:
+        counts = _vector(counts, dev, torch.int64, cfg.experts, "counts")
     index = logits.new_empty((tokens, cfg.top_k), dtype=torch.int32)
     weight = torch.empty_like(index, dtype=torch.float32)
-    _call(dev, stream, lib().moara_route, ctypes.byref(cfg), logits.data_ptr(), tokens, ld, b, m, index.data_ptr(),
-          weight.data_ptr(), c)
+    _call(dev, stream, lib().moara_route, cfg, logits.data_ptr(), tokens, ld, bias, mask, index.data_ptr(),
+          weight.data_ptr(), counts)
     return index, weight
 
 
@@ -661,10 +671,11 @@ def moara_route_backward(cfg: moara_route_config, logits, index, grad_weight, st
     moara_route gave it; grad_weight: float32, tokens x top_k."""
     import torch
     dev, tokens, ld = _route_logits(cfg, logits)
-    i = _vector(index, dev, torch.int32, tokens * cfg.top_k, "index")
-    w = _vector(grad_weight, dev, torch.float32, tokens * cfg.top_k, "grad_weight")
+    n = tokens * cfg.top_k
+    i = _vector(index, dev, torch.int32, n, "index")
+    w = _vector(grad_weight, dev, torch.float32, n, "grad_weight")
     grad = torch.empty_like(logits, memory_format=torch.contiguous_format)
-    _call(dev, stream, lib().moara_route_backward, ctypes.byref(cfg), logits.data_ptr(), tokens, ld, i, w, grad.data_ptr())
+    _call(dev, stream, lib().moara_route_backward, cfg, logits.data_ptr(), tokens, ld, i, w, grad.data_ptr())
     return grad
 
 

@@ -260,18 +260,19 @@ class MoARa(torch.optim.Optimizer):
         """Norm of all gradients; the targets' (with torch's AdamW all) scaled to the limit in place. Returns the
         coefficient. Runs on the current stream; the library's step, on the default one, waits for it."""
         params = [p for g in self.param_groups for p in g["params"]]
-        for p in params:
-            if p.grad is not None and (p.grad.layout != torch.strided or not p.grad.is_contiguous()):
-                p.grad = (p.grad.to_dense() if p.grad.layout != torch.strided else p.grad).contiguous()
+        grads = [p.grad for p in params]
+        for i, g in enumerate(grads):
+            if g is not None and (g.layout != torch.strided or not g.is_contiguous()):
+                params[i].grad = grads[i] = (g.to_dense() if g.layout != torch.strided else g).contiguous()
         with self._device():
             here = torch.cuda.current_stream()
             if self._norm_args is None or here != self._norm_stream:    # its workspace is used by one stream at a time
                 self._norm_args, self._norm_stream = M.GradArgs([]), here
-            self._norm_args.set_grads([p.grad for p in params])
+            self._norm_args.set_grads(grads)
             norm = M.moara_grad_norm(None, self._max_norm, args=self._norm_args)
-            if self._own is not None:
-                self._norm_args.set_grads([p.grad for p in self.param_groups[0]["params"]])
-            M.moara_grad_scale(None, norm[1:], args=self._norm_args)
+            targets = len(self.param_groups[0]["params"])
+            M.moara_grad_scale(None, norm[1:], args=self._norm_args,
+                               first=None if self._own is None else sum(g is not None for g in grads[:targets]))
             if here.cuda_stream != 0:
                 torch.cuda.default_stream().wait_stream(here)
         self.grad_norm = norm[0]
