@@ -375,7 +375,7 @@ typedef struct {
  * which moara_adamw_step changes nothing and moara_grad_scale clears the gradients.
  * tensors: host array, read during the call. out: two floats of device memory.
  * max_norm > 0 (infinity: the coefficient is 1).
- * Errors: MOARA_E_ARG, MOARA_E_SHAPE (a count below 0 or over 2^40), MOARA_E_HIP. */
+ * Errors: MOARA_E_ARG, MOARA_E_SHAPE (a count below 0 or over 2^33), MOARA_E_HIP. */
 int moara_grad_norm(const moara_grad_tensor* tensors, int32_t n, float max_norm, float* out, void* workspace,
                     void* stream);
 
@@ -426,7 +426,7 @@ int moara_adamw_default_config(moara_adamw_config* out);
  *      leave it where it is. A v above zero never becomes 0, which would divide by eps.
  * The random bits of element i of tensor j are a function of (seed, j, i): give every step
  * another seed. The update of p uses the moments before their rounding.
- * Errors: MOARA_E_ARG, MOARA_E_SHAPE (a count below 0 or over 2^40), MOARA_E_HIP. */
+ * Errors: MOARA_E_ARG, MOARA_E_SHAPE (a count below 0 or over 2^33), MOARA_E_HIP. */
 int moara_adamw_step(const moara_adamw_config* cfg, const moara_adamw_tensor* tensors, int32_t n, const float* clip,
                      uint64_t seed, void* stream);
 

@@ -13,8 +13,9 @@ namespace {
     if (e_ != hipSuccess) return moara_fail(MOARA_E_HIP, "%s: %s", #expr, hipGetErrorString(e_));  \
   } while (0)
 
-constexpr int64_t MAX_COUNT = (int64_t)1 << 40;      // elements of one tensor
-constexpr uint32_t MAX_TILES = 1u << 30;             // workgroups of one launch (a tensor has at most 2^29)
+// A launch has fewer than 2^32 threads: 2^22 workgroups of 512, as many as the largest tensor takes.
+constexpr int64_t MAX_COUNT = (int64_t)1 << 33;      // elements of one tensor
+constexpr uint32_t MAX_TILES = 1u << 22;             // workgroups of one AdamW launch
 
 bool misaligned(const void* p, int size) { return ((uintptr_t)p & (uintptr_t)(size - 1)) != 0; }
 
@@ -37,7 +38,7 @@ template <typename F> int each_grad_list(const moara_grad_tensor* t, int32_t n, 
   for (int i = 0; i < n; ++i) {
     if (!t[i].grad || t[i].count == 0) continue;
     const uint32_t tiles = grad_tiles(t[i].count);
-    if (l.n == GRAD_MAX || (l.n && l.tiles + tiles > MAX_TILES)) {
+    if (l.n == GRAD_MAX) {
       TRAIN_TRY(launch(l, first));
       first = false;
       l = GradList{};
@@ -83,7 +84,7 @@ int check_route(const moara_route_config* c, const void* logits, int64_t tokens,
   if (c->experts > ROUTE_MAX_EXPERTS || c->top_k > ROUTE_MAX_K || c->groups > ROUTE_MAX_GROUPS)
     return moara_fail(MOARA_E_UNSUPPORTED, "at most %d experts, top_k %d and %d groups", ROUTE_MAX_EXPERTS, ROUTE_MAX_K,
                       ROUTE_MAX_GROUPS);
-  if (tokens < 0 || tokens > MAX_COUNT) return moara_fail(MOARA_E_SHAPE, "bad token count");
+  if (tokens < 0 || tokens > (int64_t)1 << 40) return moara_fail(MOARA_E_SHAPE, "bad token count");
   if (tokens > 0 && !logits) return moara_fail(MOARA_E_ARG, "null logits");
   if (row_stride < c->experts && tokens > 1) return moara_fail(MOARA_E_SHAPE, "rows overlap: stride %lld", (long long)row_stride);
   if (misaligned(logits, c->logits_dtype == MOARA_BF16 ? 2 : 4))

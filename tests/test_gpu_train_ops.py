@@ -413,6 +413,28 @@ def test_adamw_8_bits_past_2_to_the_31_elements():
     np.testing.assert_allclose(float(norm[0]), O.grad_norm([x], 1.0)[0], rtol=NORM_TOL)
 
 
+def test_adamw_8_bits_largest_tensor_and_one_after_it():
+    """2^33 elements fill a launch (2^31 threads), the next tensor takes another; pair indices pass 32 bits."""
+    M = _M()
+    n, k = 1 << 33, 5000
+    gt = np.float32(1e-3 * rng(32, 1).standard_normal(k))
+    p = [torch.zeros(n, dtype=BF16, device="cuda"), torch.zeros(k, dtype=BF16, device="cuda")]
+    g = [torch.zeros(n, dtype=BF16, device="cuda"), torch.from_numpy(gt).cuda().to(BF16)]
+    g[0][n - k:] = g[1]
+    st = [M.moara_adamw_state(x, 8) for x in p]
+    M.moara_adamw_step(M.AdamWArgs(p, g, *([s[j] for s in st] for j in range(3))),
+                       M.moara_adamw_default_config(bits=8, **HYPER), LR, 1, seed=78)
+    for i, first in ((0, n - k - (n - k) % 32), (1, 0)):
+        x = _np(g[i][first:])
+        m1, v1 = O.moments(x, 0.0, 0.0, HYPER["beta1"], HYPER["beta2"])
+        em, ev = O.block_exponents(m1, 18), O.block_exponents(v1, 35)
+        _codes_agree(st[i][0][first:].cpu().numpy(), O.encode_m(m1, em), k, "m")
+        _codes_agree(st[i][1][first:].cpu().numpy(), O.encode_v(v1, ev, O.random16(first, x.size, 78, i)), k, "v")
+        assert np.array_equal(st[i][2][first // 16:].cpu().numpy().reshape(-1, 2), np.stack([em, ev], 1))
+    assert not p[0][:n - k].any()
+    assert float(M.moara_grad_norm(g, 1.0)[0]) == pytest.approx(O.grad_norm([_np(g[1])] * 2, 1.0)[0], rel=NORM_TOL)
+
+
 # ---------------------------------------------------------------- routing
 
 ROUTES = [

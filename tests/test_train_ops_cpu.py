@@ -26,6 +26,7 @@ def _grads(**kw):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(dtype=7), M.MOARA_E_ARG), (dict(count=-1), M.MOARA_E_SHAPE), (dict(count=(1 << 40) + 1), M.MOARA_E_SHAPE),
+    (dict(count=(1 << 33) + 1), M.MOARA_E_SHAPE),
     (dict(grad=P + 2), M.MOARA_E_ARG), (dict(grad=P + 1, dtype=M.MOARA_BF16), M.MOARA_E_ARG)])
 def test_gradient_lists_are_refused(kw, status):
     L, t = M.lib(), _grads(**kw)
@@ -48,6 +49,7 @@ def test_scale_without_a_coefficient_is_refused():
 
 @pytest.mark.parametrize("kw,status", [
     (dict(param_dtype=2), M.MOARA_E_ARG), (dict(grad_dtype=-1), M.MOARA_E_ARG), (dict(count=-5), M.MOARA_E_SHAPE),
+    (dict(count=(1 << 33) + 1), M.MOARA_E_SHAPE),
     (dict(param=None), M.MOARA_E_ARG), (dict(exp_avg=None), M.MOARA_E_ARG), (dict(exp_avg_sq=None), M.MOARA_E_ARG),
     (dict(scales=None), M.MOARA_E_ARG), (dict(param=P + 2), M.MOARA_E_ARG), (dict(grad=P + 1), M.MOARA_E_ARG),
     (dict(step=0), M.MOARA_E_ARG), (dict(lr=math.nan), M.MOARA_E_ARG), (dict(weight_decay=math.inf), M.MOARA_E_ARG)])
