@@ -6,7 +6,7 @@ namespace {
 
 // Vectors of any alignment (the hardware takes unaligned vector accesses). A lane's 16 bytes and the next
 // lane's are neighbours in every access: lanes that took 32 consecutive bytes of fp32 in two halves
-// touched each line twice (32-bit AdamW over 66 M elements 254 us instead of 227).
+// touched each line twice (32-bit AdamW over 66 M elements 254 us instead of 227 side by side).
 typedef uint16_t u16x4u __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint16_t u16x8u __attribute__((ext_vector_type(8), aligned(2)));
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
@@ -341,7 +341,7 @@ __device__ __forceinline__ void chunk8(const AdamwTensor& T, const AdamwList& L,
 // faster on aligned bf16 and 5 % slower elsewhere, 256 threads 2 % slower. Reads and writes are
 // non-temporal: the next reader of a line is the next step or the next forward pass (32 bits, 66 M
 // elements 275 -> 254 us; 8 bits, 262 M elements 485 -> 419 us). Measured, bf16 parameters and gradients:
-// 32 bits 227 us for 66 M elements, 6.4 TB/s; 8 bits 427 us for 262 M elements, 6.2 TB/s (its arithmetic
+// 32 bits 237 us for 66 M elements, 6.1 TB/s; 8 bits 433 us for 262 M elements, 6.1 TB/s (its arithmetic
 // alone, about 50 issue slots an element, would take 340). fp32 parameters that start on odd elements:
 // 8 bits, 66 M elements, 169 us, 5.5 TB/s.
 template <typename PT, typename GT, int BITS>

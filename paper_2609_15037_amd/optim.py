@@ -110,7 +110,7 @@ class _AdamW:
         if self.args is None or where != self.where:
             self.args = M.AdamWArgs([p.detach() for p in self.params], grads, *([s[k] for s in self.state] for k in (0, 1)),
                                     scales=[s[2] for s in self.state] if self.cfg.bits == 8 else None,
-                                    weight_decay=self.weight_decay)
+                                    weight_decay=[self.weight_decay if p.dim() > 1 else 0.0 for p in self.params])
             self.where = where
         else:
             self.args.set_grads(grads)
@@ -146,7 +146,8 @@ class MoARa(torch.optim.Optimizer):
     others:  the remaining parameters (AdamW).
     adamw_bits: None: torch.optim.AdamW steps the others; 32 or 8: the library's AdamW, its
              moments of that many bits (parameters fp32 or bf16).
-    adamw_weight_decay, adamw_seed: of the library's AdamW (the seed of the 8-bit moments' rounding).
+    adamw_weight_decay: of the library's AdamW, on parameters of two axes or more (not on norms and biases).
+    adamw_seed: of the random rounding of its 8-bit moments.
     max_grad_norm: None, or the norm that step() clips the gradients of all parameters to. Gradients
              of the targets are scaled in place, so are the others' with torch's AdamW. A norm that is
              not finite clears the targets' gradients (their moments decay) and leaves the others alone.

@@ -7,7 +7,8 @@ balancing bias's step).
     loss.backward(); opt.step()
     router.balance(1e-3)                    # moves the bias, starts the counts again
 
-An expert without tokens has no gradient: the MoARa optimizer skips its matrices.
+An expert without tokens has no gradient: the MoARa optimizer skips its matrices. Data-parallel ranks add up
+`router.counts` (int64) before balance().
 """
 from __future__ import annotations
 
@@ -29,6 +30,7 @@ class _Route(torch.autograd.Function):
         return index, weight
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, _, grad_weight):
         logits, index = ctx.saved_tensors
         grad = M.moara_route_backward(ctx.cfg, logits, index, grad_weight.float().contiguous())
@@ -57,7 +59,8 @@ class ExpertRouter(torch.nn.Module):
     def forward(self, x: torch.Tensor, mask: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
         """x: tokens x d_model; mask: tokens, False where a token is not routed. An index is -1 (weight 0)
         where there is no expert."""
-        logits = torch.nn.functional.linear(x.float(), self.weight.float())
+        with torch.autocast(x.device.type, enabled=False):      # the choice is sensitive to the logits' rounding
+            logits = torch.nn.functional.linear(x.float(), self.weight.float())
         return route(logits, self.cfg, self.bias, mask, self.counts)
 
     def load(self) -> np.ndarray:

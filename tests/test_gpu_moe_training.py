@@ -102,6 +102,21 @@ def test_a_norm_that_is_not_finite_skips_the_other_parameters():
 
 
 @pytest.mark.parametrize("bits", [8, 32])
+def test_weight_decay_is_for_matrices(bits):
+    """With gradients of zero and fresh moments the update is the decay alone, one rounding of the product."""
+    net = Net(8).cuda()
+    opt = _opt(net, adamw_bits=bits, adamw_weight_decay=0.5)
+    before = {n: p.detach().clone() for n, p in net.named_parameters()}
+    for p in net.parameters():
+        p.grad = torch.zeros_like(p)
+    opt.step()
+    for n, p in net.named_parameters():
+        if "proj" not in n:
+            want = before[n] * (1 - 1e-2 * 0.5) if p.dim() > 1 else before[n]
+            torch.testing.assert_close(p.detach(), want, rtol=2.0 ** -22, atol=0, msg=n)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
 def test_checkpoint_of_the_library_adamw(bits):
     a = Net(4).cuda()
     oa = _opt(a, adamw_bits=bits, adamw_seed=7)
@@ -158,6 +173,10 @@ def test_router_module_gradients_and_load():
     weight2 = r(x)[1]
     weight2.sum().backward()                # a gradient that is an expanded scalar
     assert r.load().sum() == 300
+    load = r.load().copy()
+    with torch.autocast("cuda", dtype=torch.bfloat16):
+        again = r(x)
+    assert torch.equal(again[0], index) and torch.equal(again[1], weight)
     load = r.load().copy()
     r.balance(0.25)
     assert not r.load().any()
