@@ -382,7 +382,9 @@ hipError_t launch_grad_norm_end(const double* partial, float max_norm, float* ou
 }
 
 hipError_t launch_grad_scale(const GradList& l, bool once, const float* coef, hipStream_t st) {
-  const dim3 g(l.tiles < 2048 ? l.tiles : 2048), b(256);
+  // 2.3 GB of fp32: 834 us with 16384 workgroups, 855 with 2048, 800 with one for each tile, which take 8 us
+  // more to find that the coefficient is 1
+  const dim3 g(l.tiles < 16384 ? l.tiles : 16384), b(256);
   if (once) hipLaunchKernelGGL((k_grad_scale<true>), g, b, 0, st, l, coef);
   else hipLaunchKernelGGL((k_grad_scale<false>), g, b, 0, st, l, coef);
   return hipGetLastError();
