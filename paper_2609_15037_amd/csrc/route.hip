@@ -127,26 +127,14 @@ __device__ __forceinline__ float key_value(uint32_t k) {
 // A row's largest logit and its sum of exponentials (softmax). The sum is taken in 64 bits: an expert's
 // score must not depend on the order of the others.
 struct Row { float top, total; };
-template <int LANES, int V> __device__ __forceinline__ Row softmax_row(const float (&l)[V]) {
-  Row r;
-  float top = l[0];
-#pragma unroll
-  for (int j = 1; j < V; ++j) top = fmaxf(top, l[j]);
-  r.top = max_of<LANES>(top);
-  double sum = 0;
-#pragma unroll
-  for (int j = 0; j < V; ++j) sum += (double)expf(l[j] - r.top);
-  r.total = (float)sum_of<LANES>(sum);
-  return r;
-}
 __device__ __forceinline__ float score(float l, const Row& r, int sigmoid) {
   return sigmoid ? 1.f / (1.f + expf(-l)) : expf(l - r.top) / r.total;
 }
-// The same scores, to the bit, of all of a lane's logits. The quotients are rounded correctly without the
-// division's scaling. 1 / d with d from 1 to 2^100: one Newton step on the hardware's reciprocal (compared
-// for every such d). e / d with e from 2^-78: the correctly rounded reciprocal's product and one step on its
-// remainder (Markstein 1990). Lanes with other values divide.
-template <int V> __device__ __forceinline__ void scores(const float (&l)[V], const Row& r, int sigmoid, float (&s)[V]) {
+// The same scores, to the bit, of all of a lane's logits, and the row. The quotients are rounded correctly
+// without the division's scaling. 1 / d with d from 1 to 2^100: one Newton step on the hardware's reciprocal
+// (compared for every such d). e / d with e from 2^-78: the correctly rounded reciprocal's product and one step
+// on its remainder (Markstein 1990). Lanes with other values divide.
+template <int LANES, int V> __device__ __forceinline__ Row scores(const float (&l)[V], int sigmoid, float (&s)[V]) {
   if (sigmoid) {
     float most = 0.f;
 #pragma unroll
@@ -164,25 +152,33 @@ template <int V> __device__ __forceinline__ void scores(const float (&l)[V], con
 #pragma unroll
       for (int j = 0; j < V; ++j) s[j] = 1.f / (1.f + s[j]);
     }
-  } else {
-    uint32_t least = 0xFFFFFFFFu;       // of the exponentials that are not zero, their bits less 1
+    return Row{0.f, 1.f};
+  }
+  float top = l[0];
+#pragma unroll
+  for (int j = 1; j < V; ++j) top = fmaxf(top, l[j]);
+  top = max_of<LANES>(top);
+  double sum = 0;
+  uint32_t least = 0xFFFFFFFFu;         // of the exponentials that are not zero, their bits less 1
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    s[j] = expf(l[j] - top);
+    sum += (double)s[j];
+    least = min(least, __float_as_uint(s[j]) - 1u);
+  }
+  const float total = (float)sum_of<LANES>(sum);
+  if (least >= 0x18800000u - 1u) {      // 2^-78
+    const float y = 1.f / total;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      s[j] = expf(l[j] - r.top);
-      least = min(least, __float_as_uint(s[j]) - 1u);
+      const float q = s[j] * y;
+      s[j] = fmaf(fmaf(-q, total, s[j]), y, q);
     }
-    if (least >= 0x18800000u - 1u) {    // 2^-78
-      const float y = 1.f / r.total;
+  } else {
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const float q = s[j] * y;
-        s[j] = fmaf(fmaf(-q, r.total, s[j]), y, q);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) s[j] = s[j] / r.total;
-    }
+    for (int j = 0; j < V; ++j) s[j] = s[j] / total;
   }
+  return Row{top, total};
 }
 
 // u_j of the chosen experts, one a lane (lanes without one: there = false): the score itself, or its share
@@ -352,9 +348,7 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_route(RouteParams p) {
     const int64_t row = (t < p.tokens ? t : 0) * p.ld;
     const bool live = t < p.tokens && !(p.mask && !p.mask[t]);
     float s[V];
-    Row r = {0.f, 1.f};
-    if (!p.sigmoid) r = softmax_row<LANES, V>(l);
-    scores<V>(l, r, p.sigmoid, s);
+    const Row r = scores<LANES, V>(l, p.sigmoid, s);
     if (t - slot + step < p.tokens) fetch(t + step);        // arrives during the choice
     uint32_t key[V];
 #pragma unroll
@@ -429,8 +423,7 @@ __global__ __launch_bounds__(256) void k_route_backward(RouteParams p) {
         const int e = expert_of<LANES>(j, lane);
         load4(p.logits, half, row + e, p.E - e, l + j);
       }
-      r = softmax_row<LANES, V>(l);
-      scores<V>(l, r, 0, s);
+      r = scores<LANES, V>(l, 0, s);
     }
     const float u = chosen_share<LANES>(lc, there, r, p);
     const float mean = p.renorm ? sum_of<LANES>(dw * u) : 0.f;
