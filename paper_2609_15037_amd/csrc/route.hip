@@ -9,7 +9,7 @@ namespace {
 typedef uint16_t u16x4u __attribute__((ext_vector_type(4), aligned(2)));
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 
-// ---- reductions over the LANES (8, 16 or 64) lanes of a token; every lane gets the result. Sixteen lanes are
+// ---- reductions over the LANES (8 to 64) lanes of a token; every lane gets the result. Sixteen lanes are
 // one row of the cross-lane data path: neighbours, neighbouring pairs, mirrored halves and rows.
 template <int CTRL> __device__ __forceinline__ uint32_t dpp(uint32_t x) {
   return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xF, 0xF, true);     // every lane has its source
@@ -47,10 +47,12 @@ template <int LANES, typename T, typename F> __device__ __forceinline__ T reduce
   x = f(x, dpp<0x4E>(x));     // lane ^ 2
   x = f(x, dpp<0x141>(x));    // mirrored within eight lanes
   if (LANES >= 16) x = f(x, dpp<0x140>(x));     // mirrored within sixteen
-  if (LANES == 64) {
-    T a, b;
+  T a, b;
+  if (LANES >= 32) {
     rows_apart<16>(x, a, b);
     x = f(a, b);
+  }
+  if (LANES == 64) {
     rows_apart<32>(x, a, b);
     x = f(a, b);
   }
@@ -314,9 +316,9 @@ __device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const RouteParam
 // addition in about 20 ns, so at most 256 workgroups walk over the tokens (with 1024 the counts cost 20 us of
 // 26 for 16384 tokens of 64 experts, with 128 the rest takes as much longer). They are whole numbers: the
 // order of the additions does not change them.
-// fp32 logits, with bias and counts: 8 tokens, 64 experts, top 6: 4.7 us; 16384 tokens of the same 10.8 us (5.5
+// fp32 logits, with bias and counts: 8 tokens, 64 experts, top 6: 4.2 us; 16384 tokens of the same 10.3 us (5.0
 // without counts); 32768 tokens, 256 experts in 8 groups, top 8: 24 us (20; a scan of all candidates for each
-// choice, with divisions and one lane for a group, took 41); 16384 tokens, 512 experts, top 12: 37 us.
+// choice, with divisions and one lane for a group, took 41); 16384 tokens, 512 experts, top 12: 28 us.
 enum { NO_GROUPS, EVEN_GROUPS, ANY_GROUPS };
 constexpr int ROUTE_THREADS = 1024;
 template <int LANES, int V, int DEP, int GROUPS>
@@ -465,9 +467,13 @@ __global__ __launch_bounds__(256) void k_route_balance(int E, long long* __restr
   }
 }
 
-// Eight lanes hold up to 32 experts and 8 choices of a token (65536 tokens of 8 experts, top 2: 7.4 us, on
-// sixteen lanes 12.5), sixteen up to 256 and 16, a wave what is more.
-int lanes_of(const RouteParams& p) { return p.k > 16 || p.E > 256 ? 64 : p.k > 8 || p.E > 32 ? 16 : 8; }
+// Lanes of a token: as few as hold its choices, and its experts at sixteen a lane (four a lane of eight).
+// Fewer lanes share a wave's instructions among more tokens: 65536 tokens of 8 experts, top 2, take 7 us on
+// eight lanes and 12 on sixteen; 16384 of 512 experts, top 12, with counts 28 us on 32
+// lanes and 34 on a wave.
+int lanes_of(const RouteParams& p) {
+  return p.k <= 8 && p.E <= 32 ? 8 : p.k <= 16 && p.E <= 256 ? 16 : p.k <= 32 && p.E <= 512 ? 32 : 64;
+}
 int64_t workgroups(const RouteParams& p, int threads, int64_t most) {
   const int64_t tok = threads / lanes_of(p), n = (p.tokens + tok - 1) / tok;
   return n < most ? n : most;
@@ -486,16 +492,19 @@ hipError_t launch_route(const RouteParams& p, hipStream_t st) {
     else hipLaunchKernelGGL((k_route<LANES, V, DEP, ANY_GROUPS>), g, b, 0, st, p);                               \
   } while (0)
   const int lanes = lanes_of(p);
-  const bool w = lanes == 64, few = p.k <= 8;   // few: a lane's best eight are enough
+  const bool few = p.k <= 8;    // a lane's best eight are enough
+#define ROUTE_ON(LANES)                                   \
+  do {                                                    \
+    if (p.E <= 4 * LANES) ROUTE(LANES, 4, 4);             \
+    else if (p.E <= 8 * LANES) ROUTE(LANES, 8, 8);        \
+    else if (few) ROUTE(LANES, 16, 8);                    \
+    else ROUTE(LANES, 16, 16);                            \
+  } while (0)
   if (lanes == 8) ROUTE(8, 4, 4);
-  else if (!w && p.E <= 64) ROUTE(16, 4, 4);
-  else if (!w && p.E <= 128) ROUTE(16, 8, 8);
-  else if (!w && few) ROUTE(16, 16, 8);
-  else if (!w) ROUTE(16, 16, 16);
-  else if (p.E <= 256) ROUTE(64, 4, 4);
-  else if (p.E <= 512) ROUTE(64, 8, 8);
-  else if (few) ROUTE(64, 16, 8);
-  else ROUTE(64, 16, 16);
+  else if (lanes == 16) ROUTE_ON(16);
+  else if (lanes == 32) ROUTE_ON(32);
+  else ROUTE_ON(64);
+#undef ROUTE_ON
 #undef ROUTE
   return hipGetLastError();
 }
@@ -503,14 +512,19 @@ hipError_t launch_route(const RouteParams& p, hipStream_t st) {
 hipError_t launch_route_backward(const RouteParams& p, hipStream_t st) {
   const dim3 g((uint32_t)workgroups(p, 256, 1024)), b(256);
   const int lanes = lanes_of(p);
-  const bool w = lanes == 64;
-  if (lanes == 8) hipLaunchKernelGGL((k_route_backward<8, 4>), g, b, 0, st, p);
-  else if (!w && p.E <= 64) hipLaunchKernelGGL((k_route_backward<16, 4>), g, b, 0, st, p);
-  else if (!w && p.E <= 128) hipLaunchKernelGGL((k_route_backward<16, 8>), g, b, 0, st, p);
-  else if (!w) hipLaunchKernelGGL((k_route_backward<16, 16>), g, b, 0, st, p);
-  else if (p.E <= 256) hipLaunchKernelGGL((k_route_backward<64, 4>), g, b, 0, st, p);
-  else if (p.E <= 512) hipLaunchKernelGGL((k_route_backward<64, 8>), g, b, 0, st, p);
-  else hipLaunchKernelGGL((k_route_backward<64, 16>), g, b, 0, st, p);
+#define BACKWARD(LANES, V) hipLaunchKernelGGL((k_route_backward<LANES, V>), g, b, 0, st, p)
+#define BACKWARD_ON(LANES)                                \
+  do {                                                    \
+    if (p.E <= 4 * LANES) BACKWARD(LANES, 4);             \
+    else if (p.E <= 8 * LANES) BACKWARD(LANES, 8);        \
+    else BACKWARD(LANES, 16);                             \
+  } while (0)
+  if (lanes == 8) BACKWARD(8, 4);
+  else if (lanes == 16) BACKWARD_ON(16);
+  else if (lanes == 32) BACKWARD_ON(32);
+  else BACKWARD_ON(64);
+#undef BACKWARD_ON
+#undef BACKWARD
   return hipGetLastError();
 }
 

@@ -451,59 +451,85 @@ def _logits(T, E, seed, dtype):
     return torch.from_numpy(np.float32(1.5 * g.standard_normal((T, E)))).cuda().to(dtype), g
 
 
+def _check_route(T, E, k, groups, top_groups, best, sigmoid, renorm, biased, dtype):
+    """Indices, weights, counts and the gradient of one call against the oracle, the formula and differences."""
+    M = _M()
+    x, g = _logits(T, E, 41, dtype)
+    bias = np.float32(0.1 * g.standard_normal(E)) if biased else None
+    mask = g.random(T) < 0.8 if biased else None
+    counts = torch.full((E,), 5, dtype=torch.int64, device="cuda")
+    cfg = M.moara_route_default_config(experts=E, top_k=k, groups=groups, top_groups=top_groups, group_best=best,
+                                       score=sigmoid, renormalise=renorm, scale=1.5)
+    index, weight = M.moara_route(cfg, x, bias=None if bias is None else torch.from_numpy(bias).cuda(),
+                                  mask=None if mask is None else torch.from_numpy(mask).cuda(), counts=counts)
+    L = _np(x)
+    ri, rw, c = O.route(L, k, bool(sigmoid), None if bias is None else bias.astype(np.float64), mask, groups, top_groups, best,
+                        bool(renorm), 1.5)
+    got = index.cpu().numpy()
+    # scores are at most 1 (and the bias 0.5): experts whose c differ by less than 1e-6 may change places
+    differ = got != ri
+    if differ.any():
+        a = np.take_along_axis(c, np.maximum(got, 0), 1)[differ]
+        b = np.take_along_axis(c, np.maximum(ri, 0), 1)[differ]
+        assert np.all(np.abs(a - b) <= 1e-6), (T, E)
+    assert np.array_equal(got < 0, ri < 0)
+    want = O.weights(L, got, bool(sigmoid), bool(renorm), 1.5)
+    np.testing.assert_allclose(_np(weight), want, rtol=16 * EPS32 * max(1, math.log2(E)), atol=1e-12)
+    n = np.bincount(got[got >= 0], minlength=E)
+    assert np.array_equal(counts.cpu().numpy(), 5 + n)
+    # gradient: the formula's by torch in 64 bits, and differences of the weights
+    dw = torch.from_numpy(np.float32(g.standard_normal((T, k)))).cuda()
+    grad = M.moara_route_backward(cfg, x, index, dw)
+    leaf = torch.from_numpy(L).requires_grad_(True)
+    s = torch.sigmoid(leaf) if sigmoid else torch.softmax(leaf, 1)
+    there = torch.from_numpy(got >= 0)
+    at = torch.where(there, s.gather(1, torch.from_numpy(np.maximum(got, 0)).long()), 0.0)
+    if renorm:
+        total = at.sum(1, keepdim=True)
+        at = at / torch.where(total > 0, total, 1.0)
+    (1.5 * at * dw.double().cpu()).sum().backward()
+    ref = leaf.grad.numpy()
+    size = np.abs(ref).max(axis=1, keepdims=True) + np.abs(_np(dw)).max(axis=1, keepdims=True) * want.max(axis=1, keepdims=True)
+    tol = 32 * EPS32 * size + 1e-12
+    if dtype == BF16:
+        tol = tol + 2.0 ** -8 * np.abs(ref)
+    assert np.all(np.abs(_np(grad) - ref) <= tol), (T, E, float((np.abs(_np(grad) - ref) / tol).max()))
+    h, e = 2.0 ** -12, int(g.integers(E))
+    up, down = L.copy(), L.copy()
+    up[:, e] += h
+    down[:, e] -= h
+    slope = ((O.weights(up, got, bool(sigmoid), bool(renorm), 1.5) - O.weights(down, got, bool(sigmoid), bool(renorm), 1.5))
+             * _np(dw)).sum(axis=1) / (2 * h)
+    np.testing.assert_allclose(_np(grad)[:, e], slope, atol=float(size.max()) * (1e-6 + (2.0 ** -8 if dtype == BF16 else 0)),
+                               rtol=0)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("sigmoid,renorm,biased", [(0, 0, 0), (0, 1, 1), (1, 0, 0), (1, 1, 1), (0, 0, 1)])
 def test_route_and_its_gradient(sigmoid, renorm, biased, dtype):
-    M = _M()
-    for T, E, k, groups, top_groups, best in ROUTES:
-        x, g = _logits(T, E, 41, dtype)
-        bias = np.float32(0.1 * g.standard_normal(E)) if biased else None
-        mask = g.random(T) < 0.8 if biased else None
-        counts = torch.full((E,), 5, dtype=torch.int64, device="cuda")
-        cfg = M.moara_route_default_config(experts=E, top_k=k, groups=groups, top_groups=top_groups, group_best=best,
-                                           score=sigmoid, renormalise=renorm, scale=1.5)
-        index, weight = M.moara_route(cfg, x, bias=None if bias is None else torch.from_numpy(bias).cuda(),
-                                      mask=None if mask is None else torch.from_numpy(mask).cuda(), counts=counts)
-        L = _np(x)
-        ri, rw, c = O.route(L, k, bool(sigmoid), None if bias is None else bias.astype(np.float64), mask, groups, top_groups, best,
-                            bool(renorm), 1.5)
-        got = index.cpu().numpy()
-        # scores are at most 1 (and the bias 0.5): experts whose c differ by less than 1e-6 may change places
-        differ = got != ri
-        if differ.any():
-            a = np.take_along_axis(c, np.maximum(got, 0), 1)[differ]
-            b = np.take_along_axis(c, np.maximum(ri, 0), 1)[differ]
-            assert np.all(np.abs(a - b) <= 1e-6), (T, E)
-        assert np.array_equal(got < 0, ri < 0)
-        want = O.weights(L, got, bool(sigmoid), bool(renorm), 1.5)
-        np.testing.assert_allclose(_np(weight), want, rtol=16 * EPS32 * max(1, math.log2(E)), atol=1e-12)
-        n = np.bincount(got[got >= 0], minlength=E)
-        assert np.array_equal(counts.cpu().numpy(), 5 + n)
-        # gradient: the formula's by torch in 64 bits, and differences of the weights
-        dw = torch.from_numpy(np.float32(g.standard_normal((T, k)))).cuda()
-        grad = M.moara_route_backward(cfg, x, index, dw)
-        leaf = torch.from_numpy(L).requires_grad_(True)
-        s = torch.sigmoid(leaf) if sigmoid else torch.softmax(leaf, 1)
-        there = torch.from_numpy(got >= 0)
-        at = torch.where(there, s.gather(1, torch.from_numpy(np.maximum(got, 0)).long()), 0.0)
-        if renorm:
-            total = at.sum(1, keepdim=True)
-            at = at / torch.where(total > 0, total, 1.0)
-        (1.5 * at * dw.double().cpu()).sum().backward()
-        ref = leaf.grad.numpy()
-        size = np.abs(ref).max(axis=1, keepdims=True) + np.abs(_np(dw)).max(axis=1, keepdims=True) * want.max(axis=1, keepdims=True)
-        tol = 32 * EPS32 * size + 1e-12
-        if dtype == BF16:
-            tol = tol + 2.0 ** -8 * np.abs(ref)
-        assert np.all(np.abs(_np(grad) - ref) <= tol), (T, E, float((np.abs(_np(grad) - ref) / tol).max()))
-        h, e = 2.0 ** -12, int(g.integers(E))
-        up, down = L.copy(), L.copy()
-        up[:, e] += h
-        down[:, e] -= h
-        slope = ((O.weights(up, got, bool(sigmoid), bool(renorm), 1.5) - O.weights(down, got, bool(sigmoid), bool(renorm), 1.5))
-                 * _np(dw)).sum(axis=1) / (2 * h)
-        np.testing.assert_allclose(_np(grad)[:, e], slope, atol=float(size.max()) * (1e-6 + (2.0 ** -8 if dtype == BF16 else 0)),
-                                   rtol=0)
+    for shape in ROUTES:
+        _check_route(*shape, sigmoid, renorm, biased, dtype)
+
+
+# every number of lanes for a token, of experts for a lane, and of candidates kept
+LAYOUTS = [(32, 8), (31, 3), (64, 6), (128, 8), (256, 8), (256, 16), (128, 32), (256, 20), (512, 8), (512, 30),
+           (256, 64), (512, 40), (1024, 8), (1024, 50)]
+
+
+@pytest.mark.parametrize("E,k", LAYOUTS)
+def test_route_in_every_layout(E, k):
+    """Without groups, with groups of 2^n experts that lanes share, and with groups of any size."""
+    shapes = [(37, E, k, 1, 1, 1)]
+    if E == 31:
+        shapes += [(37, 30, k, 5, 2, 2), (37, 28, k, 7, 3, 1)]
+    else:
+        even = 2 if k > E // 4 else 8 if E > 64 else 4
+        shapes += [(37, E, k, even, even // 2 if k <= E // 2 else even, 2), (37, E, k, even, even // 2, 1)]
+        shapes += [(37, E // 10 * 10, k, 5, 4, 2), (37, E // 10 * 10, k, 10, 7, 1)]
+    for s in shapes:
+        if s[2] <= s[1] // s[3] * s[4]:
+            _check_route(*s, 1, 1, 1, F32)
+            _check_route(*s, 0, 0, 0, BF16)
 
 
 @pytest.mark.parametrize("E,k,groups,top", [(64, 6, 1, 1), (256, 8, 8, 4), (300, 20, 1, 1), (512, 8, 64, 8)])
