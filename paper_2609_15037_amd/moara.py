@@ -576,23 +576,23 @@ class AdamWArgs:
         if any(len(x) != n for x in (grads, exp_avgs, exp_avg_sqs)) or (scales is not None and len(scales) != n):
             raise ValueError("one gradient, one pair of moments and one scales tensor for each parameter")
         self.bits = 32 if scales is None else 8
-        self.keep = (list(params), list(exp_avgs), list(exp_avg_sqs), None if scales is None else list(scales))
+        self.params, self.keep = list(params), (list(exp_avgs), list(exp_avg_sqs), None if scales is None else list(scales))
         self.device = None
-        self.rec = np.zeros(n, dtype=_RECORDS[moara_adamw_tensor])
         mdt = torch.float32 if scales is None else torch.uint8
-        for i, p in enumerate(params):
-            self.device = dev = _on_gpu(p, self.device, f"params[{i}]")
-            if not _dense(p):
+        rows, seen = [], set()
+        for i, p in enumerate(self.params):     # an optimizer makes these on every step: a few attribute reads each
+            self.device = dev = _on_gpu(p, self.device, "a parameter")
+            if not p.is_contiguous() and not _dense(p):
                 raise ValueError(f"params[{i}]: strides {p.stride()} of shape {tuple(p.shape)} leave gaps")
-            k = p.numel()
-            r = self.rec[i]
-            r["param"], r["count"], r["param_dtype"] = p.data_ptr(), k, _dtype_id(p, f"params[{i}]")
-            r["exp_avg"] = _vector(exp_avgs[i], dev, mdt, k, f"exp_avgs[{i}]")
-            r["exp_avg_sq"] = _vector(exp_avg_sqs[i], dev, mdt, k, f"exp_avg_sqs[{i}]")
-            if scales is not None:
-                r["scales"] = _vector(scales[i], dev, mdt, 2 * -(-k // MOARA_ADAMW_BLOCK), f"scales[{i}]")
-        if len({int(a) for a, k in zip(self.rec["param"], self.rec["count"]) if k}) < sum(self.rec["count"] > 0):
-            raise ValueError("a parameter occurs twice")
+            k, at = p.numel(), p.data_ptr()
+            if k and at in seen:
+                raise ValueError("a parameter occurs twice")
+            seen.add(at)
+            rows.append((at, 0, _vector(exp_avgs[i], dev, mdt, k, "a first moment"),
+                         _vector(exp_avg_sqs[i], dev, mdt, k, "a second moment"),
+                         0 if scales is None else _vector(scales[i], dev, mdt, 2 * -(-k // MOARA_ADAMW_BLOCK), "scales"),
+                         k, 1, 0.0, 0.0, _dtype_id(p, "a parameter"), MOARA_F32))
+        self.rec = np.array(rows, dtype=_RECORDS[moara_adamw_tensor])
         self.rec["weight_decay"] = weight_decay
         self.set_grads(grads)
         self.ptr, self.n = self.rec.ctypes.data, n
@@ -600,17 +600,17 @@ class AdamWArgs:
     def set_grads(self, grads):
         """Other gradient tensors for the same parameters."""
         ptrs, types = [], []
-        for i, (p, g) in enumerate(zip(self.keep[0], grads)):
+        for i, (p, g) in enumerate(zip(self.params, grads)):
             if g is None:
                 ptrs.append(0)
                 types.append(MOARA_F32)
                 continue
-            _on_gpu(g, self.device, f"grads[{i}]")
+            _on_gpu(g, self.device, "a gradient")
             if g.shape != p.shape or (g.stride() != p.stride() and not (g.is_contiguous() and p.is_contiguous())):
                 raise ValueError(f"grads[{i}]: shape {tuple(g.shape)}, strides {g.stride()}; the parameter's are "
                                  f"{tuple(p.shape)}, {p.stride()}")
             ptrs.append(g.data_ptr())
-            types.append(_dtype_id(g, f"grads[{i}]"))
+            types.append(_dtype_id(g, "a gradient"))
         self.grads = list(grads)
         self.rec["grad"], self.rec["grad_dtype"] = ptrs, types
 

@@ -91,7 +91,6 @@ class _AdamW:
         self.steps = np.zeros(len(self.params), dtype=np.int64)
         self.calls = 0
         self.state = None
-        self.args: Optional[M.AdamWArgs] = None
 
     def _make(self) -> None:
         if self.state is None:
@@ -106,17 +105,12 @@ class _AdamW:
     def step(self, lr: float, clip: Optional[torch.Tensor]) -> None:
         self._make()
         grads = [self._grad(p) for p in self.params]
-        where = tuple(p.data_ptr() for p in self.params)    # a parameter's storage may have been replaced
-        if self.args is None or where != self.where:
-            self.args = M.AdamWArgs([p.detach() for p in self.params], grads, *([s[k] for s in self.state] for k in (0, 1)),
-                                    scales=[s[2] for s in self.state] if self.cfg.bits == 8 else None,
-                                    weight_decay=[self.weight_decay if p.dim() > 1 else 0.0 for p in self.params])
-            self.where = where
-        else:
-            self.args.set_grads(grads)
+        args = M.AdamWArgs(self.params, grads, *([s[k] for s in self.state] for k in (0, 1)),
+                           scales=[s[2] for s in self.state] if self.cfg.bits == 8 else None,
+                           weight_decay=[self.weight_decay if p.dim() > 1 else 0.0 for p in self.params])
         self.steps += np.array([g is not None for g in grads])
         self.calls += 1
-        M.moara_adamw_step(self.args, self.cfg, lr, np.maximum(self.steps, 1), clip=clip,
+        M.moara_adamw_step(args, self.cfg, lr, np.maximum(self.steps, 1), clip=clip,
                            seed=(self.seed << 32) + self.calls)
 
     def state_dict(self) -> Dict:
@@ -306,6 +300,8 @@ class MoARa(torch.optim.Optimizer):
         return out
 
     def load_state_dict(self, sd: Dict) -> None:
+        if (self._own is not None and sd.get("adamw") is not None) or (self._adamw is not None and "adamw_own" in sd):
+            raise ValueError("the state is of the other AdamW (adamw_bits) than this optimizer's")
         for g, lr in zip(self.param_groups, sd["lr"]):
             g["lr"] = lr
         if self._adamw is not None and sd["adamw"] is not None:

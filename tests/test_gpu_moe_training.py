@@ -136,8 +136,11 @@ def test_checkpoint_of_the_library_adamw(bits):
     oa.step()
     ob.step()
     assert all(torch.equal(p, q) for p, q in zip(a.parameters(), b.parameters()))
+    for other in (40 - bits, None):
+        with pytest.raises(ValueError):
+            _opt(b, adamw_bits=other).load_state_dict(oa.state_dict())
     with pytest.raises(ValueError):
-        _opt(b, adamw_bits=40 - bits).load_state_dict(oa.state_dict())
+        _opt(b, adamw_bits=bits).load_state_dict(_opt(b).state_dict())
 
 
 def test_parameters_replaced_and_transposed_between_steps():
