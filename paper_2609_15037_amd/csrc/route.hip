@@ -244,17 +244,21 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
+// What a token's lanes exchange about its groups.
+template <int LANES, int V> struct Groups {
+  static constexpr int MOST = LANES * V < ROUTE_MAX_GROUPS ? LANES * V : ROUTE_MAX_GROUPS;
+  uint64_t value[MOST];         // the two best keys, then (key of the group, lowest index first)
+  uint32_t kept[MOST];
+};
+
 // Keys of experts outside the kept groups become 0. The two best keys of a group: where a group is 4, 8, .. 64
 // consecutive experts (EVEN) they are found across the lanes that hold it, else by one lane in LDS. A group
-// counts with its best, or the sum of the two best (what cannot be chosen adds nothing).
+// counts with its best, or the sum of the two best (what cannot be chosen adds nothing); a lane ranks it.
 template <int LANES, int V, bool EVEN>
-__device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const RouteParams& p, uint32_t* rk, uint64_t* gk, int lane) {
-  auto value = [&](uint32_t best, uint32_t next) {
-    return p.group_best == 2 && next ? order_key(key_value(best) + key_value(next)) : best;
-  };
-  uint64_t mine[V / 4];         // (key, lowest index first) of the group of each four of a lane's experts
+__device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const RouteParams& p, uint32_t* rk, Groups<LANES, V>& x,
+                                            int lane) {
+  const int shift = EVEN ? __builtin_ctz(p.group_size) - 2 : 0, span = 1 << shift;      // EVEN: lanes of a group
   if (EVEN) {
-    const int shift = __builtin_ctz(p.group_size) - 2, span = 1 << shift;       // lanes of a group
 #pragma unroll
     for (int c = 0; c < V / 4; ++c) {
       const uint32_t* k = key + 4 * c;
@@ -269,17 +273,7 @@ __device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const RouteParam
       if (span > 4) with(dpp<0x141>(best), dpp<0x141>(next));
       if (LANES >= 16 && span > 8) with(dpp<0x140>(best), dpp<0x140>(next));
       const int g = (c * LANES + lane) >> shift;
-      mine[c] = (uint64_t)value(best, next) << 32 | (uint32_t)(ROUTE_MAX_GROUPS - 1 - g);
-      if (g < p.groups && !(lane & (span - 1))) gk[g] = mine[c];
-    }
-    wave_sync();
-#pragma unroll
-    for (int c = 0; c < V / 4; ++c) {
-      int rank = 0;
-      for (int q = 0; q < p.groups; ++q) rank += gk[q] > mine[c];
-      if (rank >= p.top_groups)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) key[4 * c + j] = 0;
+      if (g < p.groups && !(lane & (span - 1))) x.value[g] = (uint64_t)best << 32 | next;
     }
   } else {
 #pragma unroll
@@ -292,21 +286,32 @@ __device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const RouteParam
         next = max(next, min(best, k));
         best = max(best, k);
       }
-      gk[g] = (uint64_t)value(best, next) << 32 | (uint32_t)(ROUTE_MAX_GROUPS - 1 - g);
-    }
-    wave_sync();
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int e = expert_of<LANES>(j, lane);
-      if (key[j]) {
-        const uint64_t own = gk[((uint32_t)e * p.group_inv) >> 20];
-        int rank = 0;
-        for (int q = 0; q < p.groups; ++q) rank += gk[q] > own;
-        if (rank >= p.top_groups) key[j] = 0;
-      }
+      x.value[g] = (uint64_t)best << 32 | next;
     }
   }
-  wave_sync();          // the keys in LDS are read before the next token's are written
+  wave_sync();
+  for (int g = lane; g < p.groups; g += LANES) {
+    const uint32_t best = (uint32_t)(x.value[g] >> 32), next = (uint32_t)x.value[g];
+    const uint32_t v = p.group_best == 2 && next ? order_key(key_value(best) + key_value(next)) : best;
+    x.value[g] = (uint64_t)v << 32 | (uint32_t)(ROUTE_MAX_GROUPS - 1 - g);
+  }
+  wave_sync();
+  for (int g = lane; g < p.groups; g += LANES) {
+    const uint64_t own = x.value[g];
+    int rank = 0;
+    for (int q = 0; q < p.groups; ++q) rank += x.value[q] > own;
+    x.kept[g] = rank < p.top_groups;
+  }
+  wave_sync();
+#pragma unroll
+  for (int j = 0; j < V; j += EVEN ? 4 : 1) {
+    const int e = expert_of<LANES>(j, lane);
+    const int g = EVEN ? e >> (shift + 2) : (int)(((uint32_t)e * p.group_inv) >> 20);
+    const bool out = g >= p.groups || !x.kept[g];
+#pragma unroll
+    for (int i = 0; i < (EVEN ? 4 : 1); ++i) key[j + i] = out ? 0u : +key[j + i];
+  }
+  wave_sync();          // what is in LDS is read before the next token's is written
 }
 
 // LANES lanes take one token, V experts each. Bound by its arithmetic: the exponentials (about 20
@@ -317,7 +322,7 @@ __device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const RouteParam
 // 26 for 16384 tokens of 64 experts, with 128 the rest takes as much longer). They are whole numbers: the
 // order of the additions does not change them.
 // fp32 logits, with bias and counts: 8 tokens, 64 experts, top 6: 4.2 us; 16384 tokens of the same 10.3 us (5.0
-// without counts); 32768 tokens, 256 experts in 8 groups, top 8: 24 us (20; a scan of all candidates for each
+// without counts); 32768 tokens, 256 experts in 8 groups, top 8: 23 us (18; a scan of all candidates for each
 // choice, with divisions and one lane for a group, took 41); 16384 tokens, 512 experts, top 12: 28 us.
 enum { NO_GROUPS, EVEN_GROUPS, ANY_GROUPS };
 constexpr int ROUTE_THREADS = 1024;
@@ -327,7 +332,7 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_route(RouteParams p) {
   __shared__ uint32_t hist[LANES * V];
   __shared__ float bias[LANES * V];     // what scores are raised by; -inf for experts that do not exist
   __shared__ uint32_t rowkey[GROUPS == ANY_GROUPS ? TOK * LANES * V : 1];
-  __shared__ uint64_t groupkey[GROUPS != NO_GROUPS ? TOK * ROUTE_MAX_GROUPS : 1];
+  __shared__ Groups<LANES, V> grouped[GROUPS != NO_GROUPS ? TOK : 1];
   const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
   const bool half = p.bf16;
   for (int e = threadIdx.x; e < LANES * V; e += ROUTE_THREADS) {
@@ -357,7 +362,7 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_route(RouteParams p) {
     for (int j = 0; j < V; ++j) key[j] = order_key(s[j] + bias[expert_of<LANES>(j, lane)]);
     if (GROUPS != NO_GROUPS)
       keep_groups<LANES, V, GROUPS == EVEN_GROUPS>(key, p, rowkey + (GROUPS == ANY_GROUPS ? slot * (LANES * V) : 0),
-                                                   groupkey + slot * ROUTE_MAX_GROUPS, lane);
+                                                   grouped[slot], lane);
     double d[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) d[j] = candidate(key[j], expert_of<LANES>(j, lane));
@@ -369,18 +374,29 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_route(RouteParams p) {
       lo[j] = (uint32_t)__builtin_bit_cast(uint64_t, d[j]);
     }
     uint32_t own = 0;     // of lane i < k: 2^31 - 1 less the token's i-th expert, in 31 bits; 0 where there is none
-    for (int i = 0; i < p.k; ++i) {
+    // keep: how much of the list later choices may still ask for
+    auto choose = [&](int i, int keep) {
       const uint32_t th = max_of<LANES>(hi[0]), head = hi[0] == th ? lo[0] : 0u, tl = max_of<LANES>(head);
       const bool up = head == tl;
       // the + makes values of the operands: of two elements of an array the choice would be an index
 #pragma unroll
-      for (int j = 0; j + 1 < DEP; ++j) {
-        hi[j] = up ? +hi[j + 1] : +hi[j];
-        lo[j] = up ? +lo[j + 1] : +lo[j];
+      for (int j = 0; j + 1 < DEP; ++j)
+        if (j < keep) {
+          hi[j] = up ? +hi[j + 1] : +hi[j];
+          lo[j] = up ? +lo[j + 1] : +lo[j];
+        }
+      if (DEP <= keep) {
+        hi[DEP - 1] = up ? 0u : +hi[DEP - 1];
+        lo[DEP - 1] = up ? 0u : +lo[DEP - 1];
       }
-      hi[DEP - 1] = up ? 0u : +hi[DEP - 1];
-      lo[DEP - 1] = up ? 0u : +lo[DEP - 1];
       if (lane == i) own = th ? tl & 0x7FFFFFFFu : 0u;
+    };
+    if (DEP < V) {        // at most DEP choices
+#pragma unroll
+      for (int i = 0; i < DEP; ++i)
+        if (i < p.k) choose(i, DEP - 1 - i);
+    } else {
+      for (int i = 0; i < p.k; ++i) choose(i, DEP);
     }
     const int chosen = live && own ? (int)(0x7FFFFFFFu - own) : -1;
     const bool there = chosen >= 0;
