@@ -449,13 +449,13 @@ __global__ __launch_bounds__(256) void k_route_backward(RouteParams p) {
     if (p.sigmoid) d *= 1.f / (1.f + expf(lc));
     const float total = whole ? sum_of<LANES>(d) : 0.f;
     const bool any = max_of<LANES>((uint32_t)there) != 0;
-    float* o = out + slot * (LANES * V);
-    __syncthreads();
+    float* o = out + slot * (LANES * V);        // the lanes of a token share a wave
+    wave_sync();
 #pragma unroll
     for (int j = 0; j < V; ++j) o[expert_of<LANES>(j, lane)] = whole && any ? -s[j] * total : 0.f;
-    __syncthreads();
+    wave_sync();
     if (there) o[chosen] += d;
-    __syncthreads();
+    wave_sync();
     if (in) {
 #pragma unroll
       for (int j = 0; j < V; j += 4) {
@@ -485,8 +485,7 @@ __global__ __launch_bounds__(256) void k_route_balance(int E, long long* __restr
 
 // Lanes of a token: as few as hold its choices, and its experts at sixteen a lane (four a lane of eight).
 // Fewer lanes share a wave's instructions among more tokens: 65536 tokens of 8 experts, top 2, take 7 us on
-// eight lanes and 12 on sixteen; 16384 of 512 experts, top 12, with counts 28 us on 32
-// lanes and 34 on a wave.
+// eight lanes and 12 on sixteen; 16384 of 512 experts, top 12, with counts 28 us on 32 lanes and 34 on a wave.
 int lanes_of(const RouteParams& p) {
   return p.k <= 8 && p.E <= 32 ? 8 : p.k <= 16 && p.E <= 256 ? 16 : p.k <= 32 && p.E <= 512 ? 32 : 64;
 }
