@@ -321,7 +321,7 @@ __device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const RouteParam
 // addition in about 20 ns, so at most 256 workgroups walk over the tokens (with 1024 the counts cost 20 us of
 // 26 for 16384 tokens of 64 experts, with 128 the rest takes as much longer). They are whole numbers: the
 // order of the additions does not change them.
-// fp32 logits, with bias and counts: 8 tokens, 64 experts, top 6: 4.2 us; 16384 tokens of the same 10.3 us (5.0
+// fp32 logits, with bias and counts: 8 tokens, 64 experts, top 6: 4.2 us; 16384 tokens of the same 8.7 us (6.5
 // without counts); 32768 tokens, 256 experts in 8 groups, top 8: 23 us (18; a scan of all candidates for each
 // choice, with divisions and one lane for a group, took 41); 16384 tokens, 512 experts, top 12: 28 us.
 enum { NO_GROUPS, EVEN_GROUPS, ANY_GROUPS };
@@ -483,11 +483,14 @@ __global__ __launch_bounds__(256) void k_route_balance(int E, long long* __restr
   }
 }
 
-// Lanes of a token: as few as hold its choices, and its experts at sixteen a lane (four a lane of eight).
-// Fewer lanes share a wave's instructions among more tokens: 65536 tokens of 8 experts, top 2, take 7 us on
-// eight lanes and 12 on sixteen; 16384 of 512 experts, top 12, with counts 28 us on 32 lanes and 34 on a wave.
+// Lanes of a token: as few as hold its choices, and its experts at sixteen a lane (eight lanes: at four, or at
+// eight where there are tokens for half of the CUs). Fewer lanes share a wave's instructions among more
+// tokens: 65536 tokens of 8 experts, top 2, take 6 us on eight lanes and 12 on sixteen; 16384 of 512 experts, top
+// 12, with counts 28 us on 32 lanes and 34 on a wave. Top 6 of 64 experts with counts, on eight and on sixteen
+// lanes: 4096 tokens 6.6 and 6.1 us, 8192 7.3 and 7.5, 16384 8.7 and 10.4, 65536 15.5 and 18.5.
 int lanes_of(const RouteParams& p) {
-  return p.k <= 8 && p.E <= 32 ? 8 : p.k <= 16 && p.E <= 256 ? 16 : p.k <= 32 && p.E <= 512 ? 32 : 64;
+  const int most8 = p.tokens >= 128 * (ROUTE_THREADS / 8) ? 64 : 32;
+  return p.k <= 8 && p.E <= most8 ? 8 : p.k <= 16 && p.E <= 256 ? 16 : p.k <= 32 && p.E <= 512 ? 32 : 64;
 }
 int64_t workgroups(const RouteParams& p, int threads, int64_t most) {
   const int64_t tok = threads / lanes_of(p), n = (p.tokens + tok - 1) / tok;
@@ -515,7 +518,8 @@ hipError_t launch_route(const RouteParams& p, hipStream_t st) {
     else if (few) ROUTE(LANES, 16, 8);                    \
     else ROUTE(LANES, 16, 16);                            \
   } while (0)
-  if (lanes == 8) ROUTE(8, 4, 4);
+  if (lanes == 8 && p.E <= 32) ROUTE(8, 4, 4);
+  else if (lanes == 8) ROUTE(8, 8, 8);
   else if (lanes == 16) ROUTE_ON(16);
   else if (lanes == 32) ROUTE_ON(32);
   else ROUTE_ON(64);
@@ -534,7 +538,8 @@ hipError_t launch_route_backward(const RouteParams& p, hipStream_t st) {
     else if (p.E <= 8 * LANES) BACKWARD(LANES, 8);        \
     else BACKWARD(LANES, 16);                             \
   } while (0)
-  if (lanes == 8) BACKWARD(8, 4);
+  if (lanes == 8 && p.E <= 32) BACKWARD(8, 4);
+  else if (lanes == 8) BACKWARD(8, 8);
   else if (lanes == 16) BACKWARD_ON(16);
   else if (lanes == 32) BACKWARD_ON(32);
   else BACKWARD_ON(64);

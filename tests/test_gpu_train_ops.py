@@ -532,6 +532,29 @@ def test_route_in_every_layout(E, k):
             _check_route(*s, 0, 0, 0, BF16)
 
 
+@pytest.mark.parametrize("E,groups,top", [(64, 1, 1), (64, 8, 4), (40, 5, 3), (60, 10, 7)])
+def test_route_many_tokens_equals_few_at_a_time(E, groups, top):
+    """From 16384 tokens on the layout is another: its choices are those of the parts."""
+    M = _M()
+    T = 16384 + 77
+    x, g = _logits(T, E, 71, F32)
+    bias = torch.from_numpy(np.float32(0.1 * g.standard_normal(E))).cuda()
+    for sigmoid, renorm in ((0, 0), (0, 1), (1, 1)):
+        cfg = M.moara_route_default_config(experts=E, top_k=7, groups=groups, top_groups=top, group_best=2, score=sigmoid,
+                                           renormalise=renorm)
+        counts, part = (torch.zeros(E, dtype=torch.int64, device="cuda") for _ in range(2))
+        index, weight = M.moara_route(cfg, x, bias=bias, counts=counts)
+        dw = torch.randn(T, 7, device="cuda")
+        grad = M.moara_route_backward(cfg, x, index, dw)
+        for a in range(0, T, 5000):
+            i, w = M.moara_route(cfg, x[a:a + 5000], bias=bias, counts=part)
+            assert torch.equal(i, index[a:a + 5000])
+            torch.testing.assert_close(w, weight[a:a + 5000], rtol=4 * EPS32 * 7, atol=1e-30)     # sums of 7 in other orders
+            d = M.moara_route_backward(cfg, x[a:a + 5000], i, dw[a:a + 5000].contiguous())
+            torch.testing.assert_close(d, grad[a:a + 5000], rtol=0, atol=32 * EPS32 * float(dw.abs().max()))
+        assert torch.equal(counts, part)
+
+
 @pytest.mark.parametrize("E,k,groups,top", [(64, 6, 1, 1), (256, 8, 8, 4), (300, 20, 1, 1), (512, 8, 64, 8)])
 @pytest.mark.parametrize("sigmoid", [0, 1])
 def test_route_ties_go_to_the_lowest_index(E, k, groups, top, sigmoid):
