@@ -125,22 +125,25 @@ __device__ __forceinline__ double block_sum(double x) {
 // of 97 as long as the second launch.)
 // 1.62 GB of bf16 gradients: 237 us, 6.8 TB/s (the copy rate of this card is 5.4, a library sum's 5.6).
 template <bool ONCE>
-__global__ __launch_bounds__(256) void k_grad_norm(GradList L, double* __restrict__ partial, int first) {
+__global__ __launch_bounds__(256) void k_grad_norm(GradList L, double* __restrict__ partial, uint32_t filled) {
   double sum = 0;
   each_tile<ONCE>(L, [&](const auto& x, const void*, int64_t) {
 #pragma unroll
     for (float v : x) sum = fma((double)v, (double)v, sum);
   });
   sum = block_sum(sum);
-  if (threadIdx.x == 0) partial[blockIdx.x] = first ? sum : partial[blockIdx.x] + sum;
+  if (threadIdx.x == 0) partial[blockIdx.x] = blockIdx.x < filled ? partial[blockIdx.x] + sum : sum;
 }
 
 // The norm and the coefficient that clips it to max_norm; NaN where the norm is not finite.
-__global__ __launch_bounds__(256) void k_grad_norm_end(const double* __restrict__ partial, float max_norm,
+__global__ __launch_bounds__(256) void k_grad_norm_end(const double* __restrict__ partial, uint32_t filled, float max_norm,
                                                        float* __restrict__ out) {
   double sum = 0;
 #pragma unroll
-  for (int j = 0; j < NORM_WGS / 256; ++j) sum += partial[j * 256 + threadIdx.x];
+  for (int j = 0; j < NORM_WGS / 256; ++j) {
+    const uint32_t b = j * 256 + threadIdx.x;
+    sum += b < filled ? partial[b] : 0.0;
+  }
   sum = block_sum(sum);
   if (threadIdx.x) return;
   const float norm = (float)sqrt(sum);
@@ -369,15 +372,17 @@ uint32_t adamw_tiles(int64_t count) { return (uint32_t)((count + CHUNK - 1) / CH
 // Lists over the 256 MB of the memory-side cache leave nothing there for the next reader of the
 // gradients: they are read past it (1.62 GB 263 -> 237 us); smaller ones stay (norm and clipping of 132 MB
 // 71 us, past the cache 77).
-hipError_t launch_grad_norm(const GradList& l, bool once, double* partial, bool first, hipStream_t st) {
-  const dim3 g(NORM_WGS), b(256);
-  if (once) hipLaunchKernelGGL((k_grad_norm<true>), g, b, 0, st, l, partial, (int)first);
-  else hipLaunchKernelGGL((k_grad_norm<false>), g, b, 0, st, l, partial, (int)first);
+hipError_t launch_grad_norm(const GradList& l, bool once, double* partial, uint32_t& filled, hipStream_t st) {
+  const uint32_t wgs = l.tiles < NORM_WGS ? l.tiles : NORM_WGS;
+  const dim3 g(wgs), b(256);
+  if (once) hipLaunchKernelGGL((k_grad_norm<true>), g, b, 0, st, l, partial, filled);
+  else hipLaunchKernelGGL((k_grad_norm<false>), g, b, 0, st, l, partial, filled);
+  if (wgs > filled) filled = wgs;
   return hipGetLastError();
 }
 
-hipError_t launch_grad_norm_end(const double* partial, float max_norm, float* out, hipStream_t st) {
-  hipLaunchKernelGGL(k_grad_norm_end, dim3(1), dim3(256), 0, st, partial, max_norm, out);
+hipError_t launch_grad_norm_end(const double* partial, uint32_t filled, float max_norm, float* out, hipStream_t st) {
+  hipLaunchKernelGGL(k_grad_norm_end, dim3(1), dim3(256), 0, st, partial, filled, max_norm, out);
   return hipGetLastError();
 }
 

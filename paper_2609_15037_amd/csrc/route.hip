@@ -251,8 +251,21 @@ template <int LANES, int V> struct Groups {
   uint32_t kept[MOST];
 };
 
+// The two best keys over `span` neighbouring lanes, a power of two.
+template <int LANES> __device__ __forceinline__ void two_best(uint32_t& best, uint32_t& next, int span) {
+  auto with = [&](uint32_t ob, uint32_t on) {
+    next = max(min(best, ob), max(next, on));
+    best = max(best, ob);
+  };
+  if (span > 1) with(dpp<0xB1>(best), dpp<0xB1>(next));
+  if (span > 2) with(dpp<0x4E>(best), dpp<0x4E>(next));
+  if (span > 4) with(dpp<0x141>(best), dpp<0x141>(next));
+  if (LANES >= 16 && span > 8) with(dpp<0x140>(best), dpp<0x140>(next));
+  if (LANES >= 32 && span > 16) with((uint32_t)__shfl_xor(best, 16, 64), (uint32_t)__shfl_xor(next, 16, 64));
+}
+
 // Keys of experts outside the kept groups become 0. The two best keys of a group: where a group is 4, 8, .. 64
-// consecutive experts (EVEN) they are found across the lanes that hold it, else by one lane in LDS. A group
+// consecutive experts (EVEN) they are found across the lanes that hold it, else by lanes that share it in LDS. A group
 // counts with its best, or the sum of the two best (what cannot be chosen adds nothing); a lane ranks it.
 template <int LANES, int V, bool EVEN>
 __device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const RouteParams& p, uint32_t* rk, Groups<LANES, V>& x,
@@ -264,14 +277,7 @@ __device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const RouteParam
       const uint32_t* k = key + 4 * c;
       const uint32_t b0 = max(k[0], k[1]), b1 = max(k[2], k[3]);
       uint32_t best = max(b0, b1), next = max(min(b0, b1), max(min(k[0], k[1]), min(k[2], k[3])));
-      auto with = [&](uint32_t ob, uint32_t on) {
-        next = max(min(best, ob), max(next, on));
-        best = max(best, ob);
-      };
-      if (span > 1) with(dpp<0xB1>(best), dpp<0xB1>(next));
-      if (span > 2) with(dpp<0x4E>(best), dpp<0x4E>(next));
-      if (span > 4) with(dpp<0x141>(best), dpp<0x141>(next));
-      if (LANES >= 16 && span > 8) with(dpp<0x140>(best), dpp<0x140>(next));
+      two_best<LANES>(best, next, span);
       const int g = (c * LANES + lane) >> shift;
       if (g < p.groups && !(lane & (span - 1))) x.value[g] = (uint64_t)best << 32 | next;
     }
@@ -279,14 +285,17 @@ __device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const RouteParam
 #pragma unroll
     for (int j = 0; j < V; ++j) rk[expert_of<LANES>(j, lane)] = key[j];
     wave_sync();
-    for (int g = lane; g < p.groups; g += LANES) {
+    // lanes of a group: as many as there are for each, a power of two
+    const int share = p.groups >= LANES ? 0 : 31 - __builtin_clz(LANES) - (32 - __builtin_clz(p.groups - 1)), span = 1 << share;
+    for (int g = lane >> share; g < p.groups; g += LANES >> share) {
       uint32_t best = 0, next = 0;
-      for (uint32_t q = 0; q < p.group_size; ++q) {
+      for (uint32_t q = lane & (span - 1); q < p.group_size; q += span) {
         const uint32_t k = rk[g * p.group_size + q];
         next = max(next, min(best, k));
         best = max(best, k);
       }
-      x.value[g] = (uint64_t)best << 32 | next;
+      two_best<LANES>(best, next, span);
+      if (!(lane & (span - 1))) x.value[g] = (uint64_t)best << 32 | next;
     }
   }
   wave_sync();
@@ -488,9 +497,13 @@ __global__ __launch_bounds__(256) void k_route_balance(int E, long long* __restr
 // tokens: 65536 tokens of 8 experts, top 2, take 6 us on eight lanes and 12 on sixteen; 16384 of 512 experts, top
 // 12, with counts 28 us on 32 lanes and 34 on a wave. Top 6 of 64 experts with counts, on eight and on sixteen
 // lanes: 4096 tokens 6.6 and 6.1 us, 8192 7.3 and 7.5, 16384 8.7 and 10.4, 65536 15.5 and 18.5.
+// Few tokens take more lanes, as long as one round of workgroups holds them: a lane's experts are straight
+// code that such a call runs once (113 tokens of 138 experts 9.4 us on sixteen lanes, 4.5 on a wave).
 int lanes_of(const RouteParams& p) {
   const int most8 = p.tokens >= 128 * (ROUTE_THREADS / 8) ? 64 : 32;
-  return p.k <= 8 && p.E <= most8 ? 8 : p.k <= 16 && p.E <= 256 ? 16 : p.k <= 32 && p.E <= 512 ? 32 : 64;
+  int lanes = p.k <= 8 && p.E <= most8 ? 8 : p.k <= 16 && p.E <= 256 ? 16 : p.k <= 32 && p.E <= 512 ? 32 : 64;
+  while (lanes >= 16 && lanes < 64 && p.E > 4 * lanes && p.tokens <= 256 * (ROUTE_THREADS / (2 * lanes))) lanes *= 2;
+  return lanes;
 }
 int64_t workgroups(const RouteParams& p, int threads, int64_t most) {
   const int64_t tok = threads / lanes_of(p), n = (p.tokens + tok - 1) / tok;

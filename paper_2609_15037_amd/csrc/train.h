@@ -19,9 +19,10 @@ struct GradList {
 };
 constexpr int NORM_WGS = 2048;  // partial sums; the workspace of moara_grad_norm holds them
 uint32_t grad_tiles(int64_t count);
-// first: the partial sums are stored, else added to. once: the list is read past the caches.
-hipError_t launch_grad_norm(const GradList& l, bool once, double* partial, bool first, hipStream_t st);
-hipError_t launch_grad_norm_end(const double* partial, float max_norm, float* out, hipStream_t st);
+// filled: how many partial sums the launches before this one have stored, raised to what there is after
+// it (a launch adds to those, and stores the others). once: the list is read past the caches.
+hipError_t launch_grad_norm(const GradList& l, bool once, double* partial, uint32_t& filled, hipStream_t st);
+hipError_t launch_grad_norm_end(const double* partial, uint32_t filled, float max_norm, float* out, hipStream_t st);
 hipError_t launch_grad_scale(const GradList& l, bool once, const float* coef, hipStream_t st);
 
 // ---------------------------------------------------------------- AdamW

@@ -31,26 +31,23 @@ int check_grads(const moara_grad_tensor* t, int32_t n) {
   return MOARA_OK;
 }
 
-// The list in launches of at most GRAD_MAX tensors: launch(list, first) for each, once at least.
+// The list in launches of at most GRAD_MAX tensors: launch(list) for each.
 template <typename F> int each_grad_list(const moara_grad_tensor* t, int32_t n, F launch) {
   GradList l{};
-  bool first = true;
   for (int i = 0; i < n; ++i) {
     if (!t[i].grad || t[i].count == 0) continue;
-    const uint32_t tiles = grad_tiles(t[i].count);
     if (l.n == GRAD_MAX) {
-      TRAIN_TRY(launch(l, first));
-      first = false;
+      TRAIN_TRY(launch(l));
       l = GradList{};
     }
     l.g[l.n] = t[i].grad;
     l.count[l.n] = t[i].count;
     l.start[l.n] = l.tiles;
     if (t[i].dtype == MOARA_BF16) l.bf16[l.n >> 5] |= 1u << (l.n & 31);
-    l.tiles += tiles;
+    l.tiles += grad_tiles(t[i].count);
     ++l.n;
   }
-  TRAIN_TRY(launch(l, first));
+  if (l.n) TRAIN_TRY(launch(l));
   return MOARA_OK;
 }
 
@@ -125,11 +122,12 @@ int moara_grad_norm(const moara_grad_tensor* tensors, int32_t n, float max_norm,
   static_assert(sizeof(double) * NORM_WGS <= MOARA_GRAD_NORM_WORKSPACE, "workspace of moara_grad_norm");
   double* const partial = (double*)workspace;
   const bool once = over_cache(tensors, n);
-  const int rl = each_grad_list(tensors, n, [&](const GradList& l, bool first) {
-    return launch_grad_norm(l, once, partial, first, (hipStream_t)stream);
+  uint32_t filled = 0;
+  const int rl = each_grad_list(tensors, n, [&](const GradList& l) {
+    return launch_grad_norm(l, once, partial, filled, (hipStream_t)stream);
   });
   if (rl != MOARA_OK) return rl;
-  TRAIN_TRY(launch_grad_norm_end(partial, max_norm, out, (hipStream_t)stream));
+  TRAIN_TRY(launch_grad_norm_end(partial, filled, max_norm, out, (hipStream_t)stream));
   return MOARA_OK;
 }
 
@@ -138,9 +136,7 @@ int moara_grad_scale(const moara_grad_tensor* tensors, int32_t n, const float* c
   if (rc != MOARA_OK) return rc;
   if (!coef || misaligned(coef, 4)) return moara_fail(MOARA_E_ARG, "null or misaligned coefficient");
   const bool once = over_cache(tensors, n);
-  return each_grad_list(tensors, n, [&](const GradList& l, bool) {
-    return l.n ? launch_grad_scale(l, once, coef, (hipStream_t)stream) : hipSuccess;
-  });
+  return each_grad_list(tensors, n, [&](const GradList& l) { return launch_grad_scale(l, once, coef, (hipStream_t)stream); });
 }
 
 int moara_adamw_default_config(moara_adamw_config* out) {
