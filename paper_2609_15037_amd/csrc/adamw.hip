@@ -166,6 +166,28 @@ __global__ __launch_bounds__(256) void k_grad_scale(GradList L, const float* __r
 constexpr int THREADS = 512;
 constexpr int CHUNK = 4 * THREADS;      // elements of a workgroup, four a thread
 
+// One tensor of a list, and its random bits' keys.
+struct AdamwTensor : AdamwSet {
+  void* p;
+  const void* g;
+  void* m;
+  void* v;
+  uint8_t* scales;
+  int64_t count;
+  uint32_t start, key0, key1;
+  __device__ __forceinline__ AdamwTensor(const AdamwList& L, int i) : AdamwSet(L.set[(L.about[i] >> ADAMW_SET_BIT) & 7]) {
+    p = L.p[i];
+    g = L.g[i];
+    m = L.m[i];
+    v = L.v[i];
+    scales = L.scales[i];
+    count = (int64_t)(L.about[i] & (((uint64_t)1 << ADAMW_SET_BIT) - 1));
+    start = L.start[i];
+    key0 = mix32((uint32_t)L.seed ^ mix32((uint32_t)(L.seed >> 32) ^ mix32((uint32_t)(L.about[i] >> ADAMW_PLACE_BIT))));
+    key1 = mix32(key0 ^ MIX_C);
+  }
+};
+
 // Moments of one element. The products and sums are rounded one by one (no fused multiply-adds): the
 // 8-bit codes, whose rounding is a comparison, must not depend on which products are fused.
 __device__ __forceinline__ void moments(float g, float& m, float& v, const AdamwList& L) {
@@ -200,8 +222,6 @@ __device__ __forceinline__ void chunk32(const AdamwTensor& T, const AdamwList& L
 }
 
 // ---- 8-bit moments: blocks of 32 elements (eight lanes of four), a biased exponent for each moment.
-constexpr uint32_t MIX_A = 0x9E3779B1u, MIX_B = 0x6A09E667u, MIX_C = 0xB7E15163u;
-
 // 32 random bits for the elements 2c and 2c + 1 of a tensor. base: key0 and the index's upper half mixed.
 __device__ __forceinline__ uint32_t random32(uint32_t c, uint32_t base, uint32_t k1) {
   uint32_t x = c + base;
@@ -350,8 +370,7 @@ __device__ __forceinline__ void chunk8(const AdamwTensor& T, const AdamwList& L,
 template <typename PT, typename GT, int BITS>
 __global__ __launch_bounds__(THREADS) void k_adamw(AdamwList L) {
   const uint32_t t = blockIdx.x;
-  const int i = find_tensor(L.n, t, [&](int j) { return L.t[j].start; });
-  const AdamwTensor& T = L.t[i];
+  const AdamwTensor T(L, find_tensor(L.n, t, [&](int j) { return L.start[j]; }));
   const float clip = L.clip ? *L.clip : 1.f;
   if (!(clip == clip)) return;
   const int64_t e0 = (int64_t)(t - T.start) * CHUNK, e = e0 + 4 * threadIdx.x;

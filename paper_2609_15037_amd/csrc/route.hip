@@ -497,12 +497,15 @@ __global__ __launch_bounds__(256) void k_route_balance(int E, long long* __restr
 // tokens: 65536 tokens of 8 experts, top 2, take 6 us on eight lanes and 12 on sixteen; 16384 of 512 experts, top
 // 12, with counts 28 us on 32 lanes and 34 on a wave. Top 6 of 64 experts with counts, on eight and on sixteen
 // lanes: 4096 tokens 6.6 and 6.1 us, 8192 7.3 and 7.5, 16384 8.7 and 10.4, 65536 15.5 and 18.5.
-// Few tokens take more lanes, as long as one round of workgroups holds them: a lane's experts are straight
+// Few tokens take more lanes, as long as one round of workgroups holds them (of 64 where each adds to the
+// counts: 8192 tokens of 256 experts 10.8 us with 128 workgroups, 12.5 with 256): a lane's experts are straight
 // code that such a call runs once (113 tokens of 138 experts 9.4 us on sixteen lanes, 4.5 on a wave).
 int lanes_of(const RouteParams& p) {
   const int most8 = p.tokens >= 128 * (ROUTE_THREADS / 8) ? 64 : 32;
   int lanes = p.k <= 8 && p.E <= most8 ? 8 : p.k <= 16 && p.E <= 256 ? 16 : p.k <= 32 && p.E <= 512 ? 32 : 64;
-  while (lanes >= 16 && lanes < 64 && p.E > 4 * lanes && p.tokens <= 256 * (ROUTE_THREADS / (2 * lanes))) lanes *= 2;
+  while (lanes >= 16 && lanes < 64 && p.E > 4 * lanes &&
+         p.tokens <= (p.counts ? 64 : 256) * (ROUTE_THREADS / (2 * lanes)))
+    lanes *= 2;
   return lanes;
 }
 int64_t workgroups(const RouteParams& p, int threads, int64_t most) {

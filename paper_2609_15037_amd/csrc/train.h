@@ -26,26 +26,34 @@ hipError_t launch_grad_norm_end(const double* partial, uint32_t filled, float ma
 hipError_t launch_grad_scale(const GradList& l, bool once, const float* coef, hipStream_t st);
 
 // ---------------------------------------------------------------- AdamW
-constexpr int ADAMW_MAX = 48;
-struct AdamwTensor {
-  void* p;
-  const void* g;
-  void* m;
-  void* v;
-  uint8_t* scales;              // 8 bits: two exponents for each block of 32
-  int64_t count;
+constexpr int ADAMW_MAX = 75, ADAMW_SETS = 8;
+struct AdamwSet {               // numbers that tensors of a launch share
   float decay;                  // 1 - lr weight_decay
   float lr;                     // lr / (1 - beta1^t)
   float rbc2;                   // 1 / (1 - beta2^t)
-  uint32_t start;               // first workgroup
-  uint32_t key0, key1;          // random bits of the 8-bit second moment
 };
 struct AdamwList {
-  AdamwTensor t[ADAMW_MAX];
+  void* p[ADAMW_MAX];
+  const void* g[ADAMW_MAX];
+  void* m[ADAMW_MAX];
+  void* v[ADAMW_MAX];
+  uint8_t* scales[ADAMW_MAX];   // 8 bits: two exponents for each block of 32
+  uint64_t about[ADAMW_MAX];    // elements (34 bits), set (3), place in the caller's list (27)
+  uint32_t start[ADAMW_MAX];    // first workgroup
+  AdamwSet set[ADAMW_SETS];
   const float* clip;
+  uint64_t seed;
   float b1, c1, b2, c2, eps;    // c = 1 - b
   int n;
 };
+constexpr int ADAMW_SET_BIT = 34, ADAMW_PLACE_BIT = 37;
+// Mixes 32 bits; digits of the golden ratio, sqrt 2 and e (odd).
+constexpr uint32_t MIX_A = 0x9E3779B1u, MIX_B = 0x6A09E667u, MIX_C = 0xB7E15163u;
+__host__ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
+  x = (x ^ (x >> 16)) * MIX_A;
+  x = (x ^ (x >> 15)) * MIX_B;
+  return x ^ (x >> 16);
+}
 static_assert(sizeof(GradList) <= 4096 && sizeof(AdamwList) <= 4096, "lists travel in the kernels' arguments");
 uint32_t adamw_tiles(int64_t count);
 hipError_t launch_adamw(const AdamwList& l, bool p_bf16, bool g_bf16, int bits, uint32_t total, hipStream_t st);

@@ -59,12 +59,6 @@ bool over_cache(const moara_grad_tensor* t, int32_t n) {
   return bytes > (int64_t)256 << 20;
 }
 
-uint32_t mix(uint32_t x) {
-  x = (x ^ (x >> 16)) * 0x9E3779B1u;
-  x = (x ^ (x >> 15)) * 0x6A09E667u;
-  return x ^ (x >> 16);
-}
-
 int check_route(const moara_route_config* c, const void* logits, int64_t tokens, int64_t row_stride) {
   if (!c) return moara_fail(MOARA_E_ARG, "null config");
   if (c->experts < 1 || c->top_k < 1 || c->top_k > c->experts)
@@ -152,6 +146,7 @@ int moara_adamw_default_config(moara_adamw_config* out) {
 int moara_adamw_step(const moara_adamw_config* cfg, const moara_adamw_tensor* tensors, int32_t n, const float* clip,
                      uint64_t seed, void* stream) {
   if (!cfg || n < 0 || (n > 0 && !tensors)) return moara_fail(MOARA_E_ARG, "null config or tensor list");
+  if (n >= 1 << (64 - ADAMW_PLACE_BIT)) return moara_fail(MOARA_E_ARG, "%d tensors", n);
   if (cfg->bits != 8 && cfg->bits != 32) return moara_fail(MOARA_E_ARG, "moments of %d bits (8 or 32)", cfg->bits);
   if (!(cfg->beta1 >= 0 && cfg->beta1 < 1) || !(cfg->beta2 >= 0 && cfg->beta2 < 1))
     return moara_fail(MOARA_E_ARG, "beta outside [0, 1)");
@@ -176,39 +171,40 @@ int moara_adamw_step(const moara_adamw_config* cfg, const moara_adamw_tensor* te
   }
   AdamwList l;
   l.clip = clip;
+  l.seed = seed;
   l.b1 = (float)cfg->beta1;
   l.c1 = (float)(1 - cfg->beta1);
   l.b2 = (float)cfg->beta2;
   l.c2 = (float)(1 - cfg->beta2);
   l.eps = (float)cfg->eps;
-  // tensors of one pair of types share launches
+  // tensors of one pair of types share launches, those of one step, rate and decay a set of numbers
   for (int kind = 0; kind < 4; ++kind) {
     uint32_t total = 0;
+    int sets = 0;
     l.n = 0;
     auto launch = [&] { return launch_adamw(l, (kind & 1) != 0, (kind & 2) != 0, cfg->bits, total, (hipStream_t)stream); };
     for (int i = 0; i < n; ++i) {
       const moara_adamw_tensor& t = tensors[i];
       if (!t.grad || t.count == 0) continue;
       if ((t.param_dtype == MOARA_BF16 ? 1 : 0) + (t.grad_dtype == MOARA_BF16 ? 2 : 0) != kind) continue;
+      const AdamwSet set = {(float)(1 - t.lr * t.weight_decay), (float)(t.lr / (1 - pow(cfg->beta1, (double)t.step))),
+                            (float)(1 / (1 - pow(cfg->beta2, (double)t.step)))};
       const uint32_t tiles = adamw_tiles(t.count);
-      if (l.n == ADAMW_MAX || (l.n && total + tiles > MAX_TILES)) {
+      int at = 0;
+      while (at < sets && (l.set[at].decay != set.decay || l.set[at].lr != set.lr || l.set[at].rbc2 != set.rbc2)) ++at;
+      if (l.n == ADAMW_MAX || at == ADAMW_SETS || (l.n && total + tiles > MAX_TILES)) {
         TRAIN_TRY(launch());
         total = 0;
-        l.n = 0;
+        l.n = sets = at = 0;
       }
-      AdamwTensor& d = l.t[l.n++];
-      d.p = t.param;
-      d.g = t.grad;
-      d.m = t.exp_avg;
-      d.v = t.exp_avg_sq;
-      d.scales = (uint8_t*)t.scales;
-      d.count = t.count;
-      d.decay = (float)(1 - t.lr * t.weight_decay);
-      d.lr = (float)(t.lr / (1 - pow(cfg->beta1, (double)t.step)));
-      d.rbc2 = (float)(1 / (1 - pow(cfg->beta2, (double)t.step)));
-      d.start = total;
-      d.key0 = mix((uint32_t)seed ^ mix((uint32_t)(seed >> 32) ^ mix((uint32_t)i)));
-      d.key1 = mix(d.key0 ^ 0xB7E15163u);
+      if (at == sets) l.set[sets++] = set;
+      l.p[l.n] = t.param;
+      l.g[l.n] = t.grad;
+      l.m[l.n] = t.exp_avg;
+      l.v[l.n] = t.exp_avg_sq;
+      l.scales[l.n] = (uint8_t*)t.scales;
+      l.about[l.n] = (uint64_t)t.count | (uint64_t)at << ADAMW_SET_BIT | (uint64_t)i << ADAMW_PLACE_BIT;
+      l.start[l.n++] = total;
       total += tiles;
     }
     if (l.n) TRAIN_TRY(launch());

@@ -181,6 +181,24 @@ def test_adamw_32_bits_over_a_list_of_every_size(pt, gt, gap):
     assert all(b[2]() for b in bufs)
 
 
+def test_adamw_every_tensor_with_its_own_rate_step_and_decay():
+    """More sets of numbers and more tensors than a launch takes: the same bits as one call for each."""
+    M = _M()
+    g = torch.Generator(device="cuda").manual_seed(6)
+    n = 100
+    x = [torch.randn(50 + 3 * i, generator=g, device="cuda") for i in range(n)]
+    gr = [torch.randn(t.shape, generator=g, device="cuda") for t in x]
+    lr, step, decay = [1e-3 * (1 + i % 11) for i in range(n)], [1 + i % 7 for i in range(n)], [0.1 * (i % 3) for i in range(n)]
+    y = [t.clone() for t in x]
+    a, b = ([M.moara_adamw_state(t, 32) for t in x] for _ in range(2))
+    cfg = M.moara_adamw_default_config()
+    M.moara_adamw_step(M.AdamWArgs(x, gr, [s[0] for s in a], [s[1] for s in a], weight_decay=decay), cfg, lr, step)
+    for i in range(n):
+        M.moara_adamw_step(M.AdamWArgs([y[i]], [gr[i]], [b[i][0]], [b[i][1]], weight_decay=decay[i]), cfg, lr[i], step[i])
+    assert all(torch.equal(p, q) for p, q in zip(x, y))
+    assert all(torch.equal(p[k], q[k]) for p, q in zip(a, b) for k in (0, 1))
+
+
 def test_adamw_matches_torch_over_several_steps():
     M = _M()
     g = torch.Generator(device="cuda").manual_seed(5)
