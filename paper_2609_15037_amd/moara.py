@@ -10,6 +10,7 @@ instead of being read out of bounds on the GPU.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import List, Optional, Sequence
 
@@ -476,13 +477,10 @@ def _vector(t, device, dtype, count, what: str) -> int:
     return t.data_ptr()
 
 
-def _call(device: int, stream, fn, *args):
-    """fn(*args, stream) with the tensors' device current; stream None: the device's current torch stream."""
+def _call(device: int, fn, *args):
+    """fn(*args, stream) on the current torch stream of the tensors' device, that device current."""
     import torch
-    if stream is None:
-        s = torch._C._cuda_getCurrentRawStream(device)      # a third of a small call's time is the stream object's
-    else:
-        s = _stream_ptr(stream)
+    s = torch._C._cuda_getCurrentRawStream(device)      # a third of a small call's time is the stream object's
     if device == torch._C._cuda_getDevice():
         rc = fn(*args, s)
     else:
@@ -490,6 +488,21 @@ def _call(device: int, stream, fn, *args):
             rc = fn(*args, s)
     if rc != MOARA_OK:
         _check(rc)
+
+
+def _streamed(f):
+    """Adds the argument `stream` (a torch stream or a hipStream_t as an int; None: the current one): the call runs
+    with it as the current stream, so what it allocates belongs to that stream too."""
+    @functools.wraps(f)
+    def call(*args, stream=None, **kw):
+        if stream is None:
+            return f(*args, **kw)
+        import torch
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+        with torch.cuda.stream(stream):
+            return f(*args, **kw)
+    return call
 
 
 class GradArgs:
@@ -518,7 +531,8 @@ class GradArgs:
         self.ptr, self.n = self.rec.ctypes.data, len(rows)
 
 
-def moara_grad_norm(grads, max_norm: float, out=None, stream=None, args: Optional[GradArgs] = None):
+@_streamed
+def moara_grad_norm(grads, max_norm: float, out=None, args: Optional[GradArgs] = None):
     """moara_grad_norm of the C ABI: a float32 tensor of the norm over all gradients and of the
     coefficient that clips them to max_norm (nothing is copied to the host). With `args` (a GradArgs
     of the same tensors) `grads` is ignored."""
@@ -526,18 +540,19 @@ def moara_grad_norm(grads, max_norm: float, out=None, stream=None, args: Optiona
     a = GradArgs(grads) if args is None else args
     if out is None:
         out = torch.empty(2, dtype=torch.float32, device=a.workspace.device)
-    _call(a.device, stream, lib().moara_grad_norm, a.ptr, a.n, float(max_norm),
+    _call(a.device, lib().moara_grad_norm, a.ptr, a.n, float(max_norm),
           _vector(out, a.device, torch.float32, 2, "out"), a.workspace.data_ptr())
     return out
 
 
-def moara_grad_scale(grads, coef, stream=None, args: Optional[GradArgs] = None, first: Optional[int] = None):
+@_streamed
+def moara_grad_scale(grads, coef, args: Optional[GradArgs] = None, first: Optional[int] = None):
     """moara_grad_scale of the C ABI: the gradients times coef (a float32 tensor of one element on the
     GPU), in place. first: only so many of the list's tensors (None entries do not count)."""
     import torch
     a = GradArgs(grads) if args is None else args
     n = a.n if first is None else min(int(first), a.n)
-    _call(a.device, stream, lib().moara_grad_scale, a.ptr, n, _vector(coef, a.device, torch.float32, 1, "coef"))
+    _call(a.device, lib().moara_grad_scale, a.ptr, n, _vector(coef, a.device, torch.float32, 1, "coef"))
 
 
 def moara_adamw_default_config(**overrides) -> moara_adamw_config:
@@ -615,7 +630,8 @@ class AdamWArgs:
         self.rec["grad"], self.rec["grad_dtype"] = ptrs, types
 
 
-def moara_adamw_step(args: AdamWArgs, cfg: moara_adamw_config, lr, step, clip=None, seed: int = 0, stream=None):
+@_streamed
+def moara_adamw_step(args: AdamWArgs, cfg: moara_adamw_config, lr, step, clip=None, seed: int = 0):
     """moara_adamw_step of the C ABI on the tensors of `args`. lr and step (t >= 1): one number or one for
     each tensor. clip: a float32 tensor of one element on the GPU, e.g. moara_grad_norm(...)[1:]."""
     import torch
@@ -625,7 +641,7 @@ def moara_adamw_step(args: AdamWArgs, cfg: moara_adamw_config, lr, step, clip=No
     args.rec["step"] = step
     c = None if clip is None else _vector(clip, args.device, torch.float32, 1, "clip")
     if args.n:
-        _call(args.device, stream, lib().moara_adamw_step, cfg, args.ptr, args.n, c, seed & (2 ** 64 - 1))
+        _call(args.device, lib().moara_adamw_step, cfg, args.ptr, args.n, c, seed & (2 ** 64 - 1))
 
 
 def moara_route_default_config(**overrides) -> moara_route_config:
@@ -647,7 +663,8 @@ def _route_logits(cfg, logits):
     return _on_gpu(logits, None, "logits"), tokens, (strides[0] if tokens > 1 else shape[1])
 
 
-def moara_route(cfg: moara_route_config, logits, bias=None, mask=None, counts=None, stream=None):
+@_streamed
+def moara_route(cfg: moara_route_config, logits, bias=None, mask=None, counts=None):
     """moara_route of the C ABI: (index int32, weight float32), both tokens x top_k. logits: tokens x experts,
     float32 or bfloat16, rows any distance apart (cfg.logits_dtype follows). bias: float32, one for each
     expert; mask: bool or uint8, one for each token; counts: int64, one for each expert, added to."""
@@ -661,12 +678,13 @@ def moara_route(cfg: moara_route_config, logits, bias=None, mask=None, counts=No
         counts = _vector(counts, dev, torch.int64, cfg.experts, "counts")
     index = logits.new_empty((tokens, cfg.top_k), dtype=torch.int32)
     weight = torch.empty_like(index, dtype=torch.float32)
-    _call(dev, stream, lib().moara_route, cfg, logits.data_ptr(), tokens, ld, bias, mask, index.data_ptr(),
+    _call(dev, lib().moara_route, cfg, logits.data_ptr(), tokens, ld, bias, mask, index.data_ptr(),
           weight.data_ptr(), counts)
     return index, weight
 
 
-def moara_route_backward(cfg: moara_route_config, logits, index, grad_weight, stream=None):
+@_streamed
+def moara_route_backward(cfg: moara_route_config, logits, index, grad_weight):
     """moara_route_backward of the C ABI: the gradient of the logits, contiguous, of their type. index: as
     moara_route gave it; grad_weight: float32, tokens x top_k."""
     import torch
@@ -675,14 +693,15 @@ def moara_route_backward(cfg: moara_route_config, logits, index, grad_weight, st
     i = _vector(index, dev, torch.int32, n, "index")
     w = _vector(grad_weight, dev, torch.float32, n, "grad_weight")
     grad = torch.empty_like(logits, memory_format=torch.contiguous_format)
-    _call(dev, stream, lib().moara_route_backward, cfg, logits.data_ptr(), tokens, ld, i, w, grad.data_ptr())
+    _call(dev, lib().moara_route_backward, cfg, logits.data_ptr(), tokens, ld, i, w, grad.data_ptr())
     return grad
 
 
-def moara_route_balance(counts, bias, rate: float, stream=None):
+@_streamed
+def moara_route_balance(counts, bias, rate: float):
     """moara_route_balance of the C ABI: one step of the balancing bias, in place; the counts end at zero."""
     import torch
     dev = _on_gpu(counts, None, "counts")
     n = counts.numel()
     c = _vector(counts, dev, torch.int64, n, "counts")
-    _call(dev, stream, lib().moara_route_balance, n, c, _vector(bias, dev, torch.float32, n, "bias"), float(rate))
+    _call(dev, lib().moara_route_balance, n, c, _vector(bias, dev, torch.float32, n, "bias"), float(rate))

@@ -713,6 +713,34 @@ def test_calls_run_on_the_current_stream():
     assert torch.equal(p, q) and all(torch.equal(a, b) for a, b in zip(s, r))
 
 
+def test_calls_on_a_stream_that_is_given():
+    M = _M()
+    st = torch.cuda.Stream()
+    x, logits = torch.randn(5000, device="cuda"), torch.randn(300, 64, device="cuda")
+    cfg, acfg = M.moara_route_default_config(), M.moara_adamw_default_config()
+    want = [M.moara_grad_norm([x], 1.0), *M.moara_route(cfg, logits)]
+    y = torch.zeros_like(x)
+    p, q = torch.zeros_like(x), torch.zeros_like(x)
+    a, b = M.moara_adamw_state(x, 32), M.moara_adamw_state(x, 32)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        _busy(y)
+        y.copy_(x)
+    for s in (st, st.cuda_stream):
+        got = [M.moara_grad_norm([y], 1.0, stream=s), *M.moara_route(cfg, logits, stream=s)]
+        grad = M.moara_route_backward(cfg, logits, got[1], got[2], stream=s)
+        st.synchronize()
+        assert all(torch.equal(g, w) for g, w in zip(got, want))
+        assert torch.equal(grad, M.moara_route_backward(cfg, logits, want[1], want[2]))
+    M.moara_adamw_step(M.AdamWArgs([p], [y], [a[0]], [a[1]]), acfg, 0.1, 1, clip=got[0][1:], stream=st)
+    M.moara_grad_scale([y], got[0][1:], stream=st)
+    st.synchronize()
+    M.moara_adamw_step(M.AdamWArgs([q], [x], [b[0]], [b[1]]), acfg, 0.1, 1, clip=want[0][1:], stream=0)
+    M.moara_grad_scale([x], want[0][1:])
+    torch.cuda.synchronize()
+    assert torch.equal(p, q) and torch.equal(x, y)
+
+
 def test_calls_in_a_captured_graph():
     """Captured once, replayed on new inputs between eager work; every replay equals the eager calls."""
     M = _M()
