@@ -82,40 +82,68 @@ def warmup_cosine(total_steps: int, warmup_frac: float = 0.1, min_ratio: float =
     return f
 
 
+def _order(t_shape: Sequence[int], stride: Sequence[int]) -> List[int]:
+    """What says in which order the elements of a tensor without gaps lie: the strides of its axes, those of one
+    element aside."""
+    return [s for n, s in zip(t_shape, stride) if n != 1]
+
+
 class _AdamW:
     """The library's AdamW over a list of parameters: their moments, and each one's step count (parameters
-    without a gradient are not stepped)."""
+    without a gradient are not stepped).
+
+    Moments lie in the order that the parameter's elements had when they were made (`form`: its shape and strides;
+    saved with them). A parameter whose strides are others by now is stepped through a copy in that order: 8-bit
+    moments share a scale with their neighbours in memory and cannot be moved without rounding them again."""
 
     def __init__(self, params: Sequence[torch.nn.Parameter], cfg: M.moara_adamw_config, weight_decay: float, seed: int):
         self.params, self.cfg, self.weight_decay, self.seed = list(params), cfg, float(weight_decay), int(seed)
         self.steps = np.zeros(len(self.params), dtype=np.int64)
         self.calls = 0
         self.state = None
+        self.form: List[Tuple[Tuple[int, ...], Tuple[int, ...]]] = []
 
     def _make(self) -> None:
         if self.state is None:
-            self.state = [M.moara_adamw_state(p, self.cfg.bits) for p in self.params]
+            form = [(tuple(p.shape), p.stride()) for p in self.params]
+            for i, p in enumerate(self.params):
+                if not M._dense(p):
+                    raise ValueError(f"parameter {i}: strides {p.stride()} of shape {tuple(p.shape)} leave gaps")
+            self.state, self.form = [M.moara_adamw_state(p, self.cfg.bits) for p in self.params], form
 
-    def _grad(self, p: torch.nn.Parameter) -> Optional[torch.Tensor]:
-        g = p.grad
-        if g is None or (g.layout == torch.strided and g.stride() == p.stride()):
+    @staticmethod
+    def _grad(g: torch.Tensor, p: torch.Tensor) -> torch.Tensor:
+        if g.layout == torch.strided and g.stride() == p.stride():
             return g
         return torch.empty_like(p, dtype=g.dtype).copy_(g.to_dense() if g.layout != torch.strided else g)
 
     def step(self, lr: float, clip: Optional[torch.Tensor]) -> None:
         self._make()
-        grads = [self._grad(p) for p in self.params]
-        args = M.AdamWArgs(self.params, grads, *([s[k] for s in self.state] for k in (0, 1)),
+        params, grads, copies = list(self.params), [], []
+        for i, (p, (shape, stride)) in enumerate(zip(self.params, self.form)):
+            if p.shape != shape:
+                raise ValueError(f"parameter {i} has shape {tuple(p.shape)}, its moments {shape}")
+            g = p.grad
+            if g is not None:
+                if p.stride() != stride and _order(shape, p.stride()) != _order(shape, stride):
+                    params[i] = torch.empty_strided(shape, stride, dtype=p.dtype, device=p.device).copy_(p)
+                    copies.append(i)
+                g = self._grad(g, params[i])
+            grads.append(g)
+        args = M.AdamWArgs(params, grads, *([s[k] for s in self.state] for k in (0, 1)),
                            scales=[s[2] for s in self.state] if self.cfg.bits == 8 else None,
                            weight_decay=[self.weight_decay if p.dim() > 1 else 0.0 for p in self.params])
         self.steps += np.array([g is not None for g in grads])
         self.calls += 1
         M.moara_adamw_step(args, self.cfg, lr, np.maximum(self.steps, 1), clip=clip,
                            seed=(self.seed << 32) + self.calls)
+        for i in copies:
+            self.params[i].copy_(params[i])
 
     def state_dict(self) -> Dict:
         self._make()
         return {"bits": self.cfg.bits, "steps": self.steps.tolist(), "calls": self.calls, "seed": self.seed,
+                "form": [[list(shape), list(stride)] for shape, stride in self.form],
                 "state": [[None if t is None else t.cpu().clone() for t in s] for s in self.state]}
 
     def load_state_dict(self, sd: Dict) -> None:
@@ -127,6 +155,9 @@ class _AdamW:
             for t, x in zip(s, saved):
                 if t is not None:
                     t.copy_(x)
+        # a state without its form is in the order of the parameters' elements
+        form = sd.get("form") or [(p.shape, p.stride()) for p in self.params]
+        self.form = [(tuple(shape), tuple(stride)) for shape, stride in form]
         self.steps[:] = sd["steps"]
         self.calls, self.seed = int(sd["calls"]), int(sd["seed"])
 

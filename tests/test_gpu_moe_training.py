@@ -195,3 +195,69 @@ def test_example_trains(bits):
     assert np.isfinite(losses).all()
     assert losses[-1] < 0.8 * losses[0], losses
     assert max(share) <= 0.5        # top-2 of 8 experts: an even share is an eighth, one expert always chosen a half
+
+
+def _other_strides(p):
+    """The same elements, rows first or columns first in memory."""
+    p.data = p.data.t().contiguous().t() if p.data.is_contiguous() else p.data.contiguous()
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_moments_stay_with_their_elements_when_strides_change(bits):
+    """One copy's head changes its strides twice between steps; both take the same gradients: the same bits."""
+    a, b = Net(9).cuda(), Net(9).cuda()
+    oa, ob = _opt(a, adamw_bits=bits), _opt(b, adamw_bits=bits)
+    for step in range(4):
+        _backward(a, step)
+        _same_grads(a, b)
+        if step in (1, 3):
+            _other_strides(b.head.weight)
+        for o in (oa, ob):
+            o.step()
+            o.zero_grad()
+        assert b.head.weight.is_contiguous() == (step in (0, 3))
+        for (n, p), q in zip(a.named_parameters(), b.parameters()):
+            assert torch.equal(p, q), (step, n)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_checkpoint_of_a_transposed_parameter(bits):
+    """Saved with a transposed head, loaded for a contiguous one, and on from there: the same bits. A state that
+    does not say its strides is taken to be in the order of the parameters that it is loaded for."""
+    a, b = Net(9).cuda(), Net(9).cuda()
+    _other_strides(a.head.weight)
+    oa, ob = _opt(a, adamw_bits=bits), _opt(b, adamw_bits=bits)
+    for step in range(2):
+        _backward(a, step)
+        oa.step()
+        oa.zero_grad()
+    b.load_state_dict(a.state_dict())
+    ob.load_state_dict(oa.state_dict())
+    bare = oa.state_dict()
+    del bare["adamw_own"]["form"]
+    c = Net(9).cuda()
+    _other_strides(c.head.weight)
+    oc = _opt(c, adamw_bits=bits)
+    c.load_state_dict(a.state_dict())
+    oc.load_state_dict(bare)
+    for step in (9, 10):
+        _backward(a, step)
+        for net, opt in ((b, ob), (c, oc)):
+            _same_grads(a, net)
+            opt.step()
+        oa.step()
+        oa.zero_grad()
+        for (n, p), q, r in zip(a.named_parameters(), b.parameters(), c.parameters()):
+            assert torch.equal(p, q) and torch.equal(p, r), n
+
+
+def test_a_parameter_of_another_shape_than_its_moments_is_refused():
+    net = Net(9).cuda()
+    opt = _opt(net, adamw_bits=8)
+    _backward(net, 0)
+    opt.step()
+    opt.zero_grad()
+    net.head.weight.data = net.head.weight.data.t()
+    net.head.weight.grad = torch.zeros_like(net.head.weight)
+    with pytest.raises(ValueError):
+        opt.step()
