@@ -151,13 +151,23 @@ class _AdamW:
             raise ValueError(f"the state is of {len(sd['state'])} parameters with moments of {sd['bits']} bits, the optimizer "
                              f"has {len(self.params)} with {self.cfg.bits}")
         self._make()
+        # a state without its form is in the order of the parameters' elements
+        form = [(tuple(shape), tuple(stride)) for shape, stride in
+                sd.get("form") or [(p.shape, p.stride()) for p in self.params]]
+        # all of it is looked at before any of it is taken
+        if len(form) != len(self.params) or len(sd["steps"]) != len(self.params):
+            raise ValueError("the state's steps or shapes are not one for each parameter")
+        for i, (s, saved) in enumerate(zip(self.state, sd["state"])):
+            if form[i][0] != tuple(self.params[i].shape):
+                raise ValueError(f"the state of parameter {i} is of shape {form[i][0]}, the parameter of "
+                                 f"{tuple(self.params[i].shape)}")
+            if [None if t is None else t.shape for t in s] != [None if x is None else x.shape for x in saved]:
+                raise ValueError(f"the state of parameter {i} has not as many elements as its moments")
         for s, saved in zip(self.state, sd["state"]):
             for t, x in zip(s, saved):
                 if t is not None:
                     t.copy_(x)
-        # a state without its form is in the order of the parameters' elements
-        form = sd.get("form") or [(p.shape, p.stride()) for p in self.params]
-        self.form = [(tuple(shape), tuple(stride)) for shape, stride in form]
+        self.form = form
         self.steps[:] = sd["steps"]
         self.calls, self.seed = int(sd["calls"]), int(sd["seed"])
 

@@ -60,3 +60,38 @@ def test_expert_projections_take_the_expert_types():
     t, _ = moara_targets(Moe())
     assert [m for _, m in t] == [M.MOARA_EXP_GATE, M.MOARA_EXP_DOWN, M.MOARA_EXP_GATE, M.MOARA_EXP_DOWN,
                                  M.MOARA_UP]
+
+
+def _own_adamw(shapes, bits=32):
+    from paper_2609_15037_amd.optim import _AdamW
+    params = [torch.nn.Parameter(torch.zeros(s)) for s in shapes]
+    return _AdamW(params, M.moara_adamw_config(beta1=0.9, beta2=0.999, eps=1e-6, bits=bits), 0.0, 0)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("mine,theirs", [([(7,), (33,)], [(7,), (1,)]), ([(7,), (4, 6)], [(7,), (6, 4)]), ([(3,)], [(4,)])])
+def test_adamw_state_of_other_shapes_is_refused_whole(mine, theirs, bits):
+    """Moments of one element would fill a longer parameter's, those of a transposed matrix lie elsewhere."""
+    a, b = _own_adamw(mine, bits), _own_adamw(theirs, bits)
+    sd = b.state_dict()
+    for s in sd["state"]:
+        for t in s:
+            if t is not None:
+                t.fill_(5)
+    sd["steps"] = [9] * len(theirs)
+    before = a.state_dict()
+    for drop in ((), ("form",)):
+        bad = {k: v for k, v in sd.items() if k not in drop}
+        if drop and mine[-1] == (4, 6):     # as many elements: without the shapes there is nothing to compare
+            continue
+        with pytest.raises(ValueError):
+            a.load_state_dict(bad)
+        after = a.state_dict()
+        assert after["steps"] == before["steps"] and after["form"] == before["form"]
+        assert all(x is None or torch.equal(x, y) for s, t in zip(after["state"], before["state"]) for x, y in zip(s, t))
+    good = a.state_dict()
+    with pytest.raises(ValueError):
+        a.load_state_dict({**good, "steps": [3]} if len(mine) > 1 else {**good, "steps": [3, 3]})
+    good["steps"] = [4] * len(mine)
+    a.load_state_dict(good)
+    assert a.steps.tolist() == [4] * len(mine)
