@@ -309,6 +309,7 @@ class MoARa(torch.optim.Optimizer):
             targets = len(self.param_groups[0]["params"])
             M.moara_grad_scale(None, norm[1:], args=self._norm_args,
                                first=None if self._own is None else sum(g is not None for g in grads[:targets]))
+            self._norm_args.set_grads([])       # the gradients are the caller's: none outlives its zero_grad() here
             if here.cuda_stream != 0:
                 torch.cuda.default_stream().wait_stream(here)
         self.grad_norm = norm[0]

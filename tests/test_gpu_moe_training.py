@@ -3,6 +3,7 @@ module, and the example that trains with all of them."""
 import importlib.util
 import math
 import os
+import weakref
 
 import numpy as np
 import pytest
@@ -261,3 +262,16 @@ def test_a_parameter_of_another_shape_than_its_moments_is_refused():
     net.head.weight.grad = torch.zeros_like(net.head.weight)
     with pytest.raises(ValueError):
         opt.step()
+
+
+@pytest.mark.parametrize("bits", [None, 8, 32])
+def test_clipping_keeps_no_gradient(bits):
+    """After zero_grad() the gradients' memory is free again: nothing of the step holds one."""
+    net = Net(3).cuda()
+    opt = _opt(net, adamw_bits=bits, max_grad_norm=1.0)
+    for step in range(2):
+        _backward(net, step)
+        grads = [weakref.ref(p.grad) for p in net.parameters()]
+        opt.step()
+        opt.zero_grad()
+        assert all(g() is None for g in grads)
