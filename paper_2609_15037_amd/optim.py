@@ -281,8 +281,15 @@ class MoARa(torch.optim.Optimizer):
             grads = self._grads()
             active = [g is not None for g in grads]
             if any(active):
+                # torch's side streams and the default one do not wait for each other by themselves: gradients (and
+                # their copies) are made on the current stream, weights and gradients used or freed on it afterwards
+                here, default = torch.cuda.current_stream(), torch.cuda.default_stream()
+                if here != default:
+                    default.wait_stream(here)
                 M.moara_step_mixed(self._st, tg["params"], grads, self._g32, lr=float(tg["lr"]),
                                    active=None if all(active) else active)
+                if here != default:
+                    here.wait_stream(default)
         if self._adamw is not None:
             og = self.param_groups[1]
             for g in self._adamw.param_groups:   # the schedule drives both groups
@@ -294,7 +301,7 @@ class MoARa(torch.optim.Optimizer):
 
     def _clip(self) -> torch.Tensor:
         """Norm of all gradients; the targets' (with torch's AdamW all) scaled to the limit in place. Returns the
-        coefficient. Runs on the current stream; the library's step, on the default one, waits for it."""
+        coefficient. Runs on the current stream."""
         params = [p for g in self.param_groups for p in g["params"]]
         grads = [p.grad for p in params]
         for i, g in enumerate(grads):
@@ -310,8 +317,6 @@ class MoARa(torch.optim.Optimizer):
             M.moara_grad_scale(None, norm[1:], args=self._norm_args,
                                first=None if self._own is None else sum(g is not None for g in grads[:targets]))
             self._norm_args.set_grads([])       # the gradients are the caller's: none outlives its zero_grad() here
-            if here.cuda_stream != 0:
-                torch.cuda.default_stream().wait_stream(here)
         self.grad_norm = norm[0]
         return norm[1:]
 

@@ -275,3 +275,24 @@ def test_clipping_keeps_no_gradient(bits):
         opt.step()
         opt.zero_grad()
         assert all(g() is None for g in grads)
+
+
+@pytest.mark.parametrize("clip", [None, 0.05])
+def test_training_on_a_side_stream_equals_the_default_one(clip):
+    """Forward, backward, step and zero_grad on a side stream, nothing waited for between: the same bits."""
+    nets, opts = [Net(11).cuda() for _ in range(2)], []
+    opts = [_opt(n, adamw_bits=32, max_grad_norm=clip) for n in nets]
+    for step in range(8):
+        _backward(nets[0], step)
+        opts[0].step()
+        opts[0].zero_grad()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for step in range(8):
+            _backward(nets[1], step)
+            opts[1].step()
+            opts[1].zero_grad()
+    side.synchronize()
+    for (n, p), q in zip(nets[0].named_parameters(), nets[1].parameters()):
+        assert torch.equal(p, q), n

@@ -1,4 +1,5 @@
 """Host-side parts of the torch.optim integration (no GPU needed)."""
+import contextlib
 import math
 
 import pytest
@@ -95,3 +96,38 @@ def test_adamw_state_of_other_shapes_is_refused_whole(mine, theirs, bits):
     good["steps"] = [4] * len(mine)
     a.load_state_dict(good)
     assert a.steps.tolist() == [4] * len(mine)
+
+
+class _Stream:
+    """A stream that writes down who waits for whom."""
+
+    def __init__(self, name, handle, log, look):
+        self.name, self.cuda_stream, self.log, self.look = name, handle, log, look
+
+    def wait_stream(self, other):
+        self.log.append((self.name, "waits for", other.name, self.look()))
+
+
+@pytest.mark.parametrize("side", [True, False])
+@pytest.mark.parametrize("clip", [None, 1.0])
+def test_step_on_a_side_stream_waits_both_ways(side, clip, monkeypatch):
+    """The library's step runs on the default stream. It waits for the current one, after the gradients' copies, and
+    the current one for it; on the default stream nobody waits."""
+    from paper_2609_15037_amd import optim
+    log = []
+    w = torch.nn.Parameter(torch.zeros(4, 6, dtype=torch.bfloat16))
+    opt = None
+    copied = lambda: opt._g32[0] is not None and torch.equal(opt._g32[0], w.grad.float())
+    default = _Stream("default", 0, log, copied)
+    here = _Stream("here", 77, log, copied) if side else default
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: here)
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda *a: default)
+    monkeypatch.setattr(optim.MoARa, "_device", lambda self: contextlib.nullcontext())
+    monkeypatch.setattr(optim.MoARa, "_clip", lambda self: None)
+    monkeypatch.setattr(M, "moara_default_config", lambda **kw: None)
+    monkeypatch.setattr(M, "moara_create_state", lambda cfg, descs: "state")
+    monkeypatch.setattr(M, "moara_step_mixed", lambda st, *a, **kw: log.append("step"))
+    opt = optim.MoARa([(w, M.MOARA_Q)], [], max_grad_norm=clip)
+    w.grad = torch.full_like(w, 3.0)
+    opt.step()
+    assert log == ([("default", "waits for", "here", True), "step", ("here", "waits for", "default", True)] if side else ["step"])
