@@ -185,7 +185,9 @@ class MoARa(torch.optim.Optimizer):
     adamw_seed: of the random rounding of its 8-bit moments.
     max_grad_norm: None, or the norm that step() clips the gradients of all parameters to. Gradients
              of the targets are scaled in place, so are the others' with torch's AdamW. A norm that is
-             not finite clears the targets' gradients (their moments decay) and leaves the others alone.
+             not finite clears the gradients that are scaled: the targets, and with torch's AdamW the
+             others, take a step of zero gradients (their moments decay, and move them). The library's
+             AdamW leaves the others and their moments as they are.
              `grad_norm` holds the last step's norm, on the GPU.
     rank_table: per-module ranks r_tau (MOARA_NUM_MODULES entries, 0 = unused); see
              moara_allocate_ranks for the Phase 3 rule.

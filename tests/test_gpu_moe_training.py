@@ -296,3 +296,30 @@ def test_training_on_a_side_stream_equals_the_default_one(clip):
     side.synchronize()
     for (n, p), q in zip(nets[0].named_parameters(), nets[1].parameters()):
         assert torch.equal(p, q), n
+
+
+@pytest.mark.parametrize("bits", [None, 8, 32])
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+def test_what_a_norm_that_is_not_finite_does_to_each_adamw(bad, bits):
+    """torch's AdamW takes a step of zero gradients, bit for bit; the library's changes nothing. Nothing turns NaN."""
+    net, ref = Net(12).cuda(), Net(12).cuda()
+    opt, oref = _opt(net, adamw_bits=bits, max_grad_norm=1.0), _opt(ref, adamw_bits=bits, max_grad_norm=1.0)
+    for o, n in ((opt, net), (oref, ref)):
+        _backward(n, 0)
+        o.step()
+        o.zero_grad()
+    before = {n: p.detach().clone() for n, p in net.named_parameters()}
+    _backward(net, 1)
+    net.norm.weight.grad[5] = bad
+    opt.step()
+    for p in ref.parameters():
+        p.grad = torch.zeros_like(p)
+    oref.step()
+    for (n, p), q in zip(net.named_parameters(), ref.parameters()):
+        assert torch.isfinite(p).all()
+        if bits is None or "proj" in n:
+            assert torch.equal(p, q), n
+        else:
+            assert torch.equal(p.detach(), before[n]), n
+        if bits is None and "proj" not in n:
+            assert not torch.equal(p.detach(), before[n]), n        # it moves by its momentum
