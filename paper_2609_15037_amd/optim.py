@@ -306,8 +306,8 @@ class MoARa(torch.optim.Optimizer):
         coefficient. Runs on the current stream."""
         params = [p for g in self.param_groups for p in g["params"]]
         grads = [p.grad for p in params]
-        for i, g in enumerate(grads):
-            if g is not None and (g.layout != torch.strided or not g.is_contiguous()):
+        for i, g in enumerate(grads):       # what cannot be scaled in place (sparse, or with gaps) is replaced
+            if g is not None and (g.layout != torch.strided or not M._dense(g)):
                 params[i].grad = grads[i] = (g.to_dense() if g.layout != torch.strided else g).contiguous()
         with self._device():
             here = torch.cuda.current_stream()

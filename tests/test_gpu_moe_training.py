@@ -323,3 +323,33 @@ def test_what_a_norm_that_is_not_finite_does_to_each_adamw(bad, bits):
             assert torch.equal(p.detach(), before[n]), n
         if bits is None and "proj" not in n:
             assert not torch.equal(p.detach(), before[n]), n        # it moves by its momentum
+
+
+@pytest.mark.parametrize("bits", [None, 8, 32])
+def test_gradients_of_any_order_are_scaled_in_place(bits):
+    """Transposed gradients stay the caller's tensors, scaled where the class says so; expanded ones, whose elements
+    share memory, are replaced. The steps equal those of contiguous gradients."""
+    a, b = Net(6).cuda(), Net(6).cuda()
+    oa, ob = _opt(a, adamw_bits=bits, max_grad_norm=0.05), _opt(b, adamw_bits=bits, max_grad_norm=0.05)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for n, p in a.named_parameters():
+        if n == "norm.bias":
+            p.grad = torch.full((1,), 0.5, device="cuda").expand(p.shape)
+        else:
+            p.grad = torch.randn(p.shape[::-1], generator=g, device="cuda").t() if p.dim() == 2 else \
+                torch.randn(p.shape, generator=g, device="cuda")
+    for p, q in zip(a.parameters(), b.parameters()):
+        q.grad = p.grad.contiguous().clone()
+    held = {n: p.grad for n, p in a.named_parameters()}
+    before = {n: x.clone() for n, x in held.items()}
+    oa.step()
+    ob.step()
+    for (n, p), q in zip(a.named_parameters(), b.parameters()):
+        torch.testing.assert_close(p, q, rtol=1e-5, atol=1e-6, msg=n)      # the norm's order of summation differs
+        torch.testing.assert_close(p.grad, q.grad, rtol=1e-6, atol=0, msg=n)
+        if n == "norm.bias":
+            assert torch.equal(held[n], before[n])
+            continue
+        assert p.grad is held[n], n
+        scaled = bits is None or "proj" in n
+        assert torch.equal(p.grad, before[n]) != scaled, n
