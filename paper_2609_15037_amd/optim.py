@@ -213,6 +213,10 @@ class MoARa(torch.optim.Optimizer):
         wdt = {t.dtype for t, _ in targets}
         if len(wdt) != 1 or next(iter(wdt)) not in (torch.float32, torch.bfloat16):
             raise ValueError(f"target weights must all be fp32 or all bf16, got {wdt}")
+        if adamw_bits is not None:      # here, not in a step that has already moved the targets
+            for p in others:
+                if p.dtype not in (torch.float32, torch.bfloat16):
+                    raise ValueError(f"the library's AdamW steps fp32 and bf16 parameters, got {p.dtype}")
         groups = [{"params": [t for t, _ in targets], "moara": True}]
         if others:
             groups.append({"params": others, "moara": False})

@@ -131,3 +131,16 @@ def test_step_on_a_side_stream_waits_both_ways(side, clip, monkeypatch):
     w.grad = torch.full_like(w, 3.0)
     opt.step()
     assert log == ([("default", "waits for", "here", True), "step", ("here", "waits for", "default", True)] if side else ["step"])
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float64])
+def test_library_adamw_refuses_other_types_at_the_start(dtype, monkeypatch):
+    from paper_2609_15037_amd import optim
+    monkeypatch.setattr(M, "moara_default_config", lambda **kw: None)
+    monkeypatch.setattr(M, "moara_adamw_default_config", lambda **kw: M.moara_adamw_config(**kw))
+    w, p = torch.nn.Parameter(torch.zeros(4, 6)), torch.nn.Parameter(torch.zeros(5, dtype=dtype))
+    for bits in (8, 32):
+        with pytest.raises(ValueError):
+            optim.MoARa([(w, M.MOARA_Q)], [p], adamw_bits=bits)
+        optim.MoARa([(w, M.MOARA_Q)], [torch.nn.Parameter(p.detach().bfloat16())], adamw_bits=bits)
+    optim.MoARa([(w, M.MOARA_Q)], [p])
