@@ -56,6 +56,14 @@ class ExpertRouter(torch.nn.Module):
         self.register_buffer("bias", torch.zeros(experts, dtype=torch.float32))
         self.register_buffer("counts", torch.zeros(experts, dtype=torch.int64))
 
+    def _apply(self, fn, recurse=True):
+        """Casts of the model (`.bfloat16()`, `.to(dtype)`) leave the bias in fp32: it moves by 1e-3 a step."""
+        bias = self.bias
+        super()._apply(fn, recurse)
+        if self.bias.dtype != torch.float32:
+            self.bias = bias.to(self.bias.device)
+        return self
+
     def forward(self, x: torch.Tensor, mask: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
         """x: tokens x d_model; mask: tokens, False where a token is not routed. An index is -1 (weight 0)
         where there is no expert."""

@@ -353,3 +353,24 @@ def test_gradients_of_any_order_are_scaled_in_place(bits):
         assert p.grad is held[n], n
         scaled = bits is None or "proj" in n
         assert torch.equal(p.grad, before[n]) != scaled, n
+
+
+def test_router_in_a_bf16_model():
+    """Cast with its model, the router takes bf16 rows, has bf16 gradients, and its bias moves in fp32."""
+    from paper_2609_15037_amd.route import ExpertRouter
+    torch.manual_seed(13)
+    r = torch.nn.Sequential(ExpertRouter(32, 16, 3, renormalise=1)).cuda().bfloat16()[0]
+    same = ExpertRouter(32, 16, 3, renormalise=1).cuda()
+    same.load_state_dict({"weight": r.weight.float(), "bias": r.bias, "counts": r.counts})
+    for step in range(3):
+        x = torch.randn(50, 32, device="cuda").bfloat16()
+        c = torch.randn(50, 3, device="cuda")
+        out, want = r(x), same(x.float())
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+        (out[1] * c).sum().backward()
+        (want[1] * c).sum().backward()
+        assert r.weight.grad.dtype == torch.bfloat16 and torch.equal(r.weight.grad, same.weight.grad.bfloat16())
+        r.weight.grad = same.weight.grad = None
+        r.balance(1e-3)
+        same.balance(1e-3)
+        assert r.bias.dtype == torch.float32 and torch.equal(r.bias, same.bias) and r.bias.any()
