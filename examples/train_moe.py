@@ -46,11 +46,10 @@ class Layer(torch.nn.Module):
     def mixture(self, x):
         """Every token's experts on its row, weighted; experts without tokens are not called."""
         rows = x.reshape(-1, x.shape[-1])
-        before = self.router.load().copy()
         index, weight = self.router(rows)
         out = torch.zeros_like(rows)
-        for e in (self.router.load() - before).nonzero()[0]:
-            token, slot = (index == int(e)).nonzero(as_tuple=True)
+        for e in index[index >= 0].unique().tolist():
+            token, slot = (index == e).nonzero(as_tuple=True)
             y = self.experts[e](rows[token]) * weight[token, slot, None].to(rows.dtype)
             out = out.index_add(0, token, y)
         return out.view_as(x)

@@ -3,7 +3,7 @@ balancing bias's step).
 
     router = ExpertRouter(d_model, experts=64, top_k=6)
     index, weight = router(x)               # tokens x top_k; differentiable in x and the router's weight
-    load = router.load()                    # tokens of each expert since the last balance(), on the host
+    load = router.load()                    # tokens of each expert since the last balance(), on the host (training)
     loss.backward(); opt.step()
     router.balance(1e-3)                    # moves the bias, starts the counts again
 
@@ -47,7 +47,8 @@ class ExpertRouter(torch.nn.Module):
     """A linear router: fp32 logits of each token, its top_k experts and their weights.
 
     Keyword arguments are moara_route_config's (groups, top_groups, group_best, score, renormalise, scale).
-    `bias` (a buffer) only takes part in the choice; it moves with balance()."""
+    `bias` (a buffer) only takes part in the choice; it moves with balance(). `counts` are those of training: evaluation
+    passes (`eval()`) and the forward passes that activation checkpointing repeats in a backward pass add nothing."""
 
     def __init__(self, d_model: int, experts: int, top_k: int, **config):
         super().__init__()
@@ -69,10 +70,11 @@ class ExpertRouter(torch.nn.Module):
         where there is no expert."""
         with torch.autocast(x.device.type, enabled=False):      # the choice is sensitive to the logits' rounding
             logits = torch.nn.functional.linear(x.float(), self.weight.float())
-        return route(logits, self.cfg, self.bias, mask, self.counts)
+        again = torch._C._current_graph_task_id() != -1         # inside a backward pass
+        return route(logits, self.cfg, self.bias, mask, self.counts if self.training and not again else None)
 
     def load(self) -> np.ndarray:
-        """Tokens of each expert since the last balance() (waits for the GPU)."""
+        """Tokens of each expert in training since the last balance() (waits for the GPU)."""
         return self.counts.cpu().numpy()
 
     def balance(self, rate: float) -> None:

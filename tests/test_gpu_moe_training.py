@@ -374,3 +374,34 @@ def test_router_in_a_bf16_model():
         r.balance(1e-3)
         same.balance(1e-3)
         assert r.bias.dtype == torch.float32 and torch.equal(r.bias, same.bias) and r.bias.any()
+
+
+def _example():
+    spec = importlib.util.spec_from_file_location("train_moe", os.path.join(ROOT, "examples", "train_moe.py"))
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    return ex
+
+
+@pytest.mark.parametrize("reentrant", [None, False, True])
+def test_counts_are_those_of_training(reentrant):
+    """A layer of the example: evaluated, trained, and with its activations recomputed; output and gradients alike."""
+    from torch.utils.checkpoint import checkpoint
+    torch.manual_seed(14)
+    layer = _example().Layer(32, 2, 48, 8, 2).cuda()
+    x = torch.randn(2, 9, 32, device="cuda", requires_grad=True)
+    layer.eval()
+    want = layer(x)
+    want.square().sum().backward()
+    grads = [p.grad for p in layer.parameters()]
+    assert not layer.router.load().any()
+    layer.train()
+    layer.zero_grad()
+    out = layer(x) if reentrant is None else checkpoint(layer, x, use_reentrant=reentrant)
+    assert torch.equal(out, want)
+    out.square().sum().backward()
+    assert layer.router.load().sum() == 36
+    for p, g in zip(layer.parameters(), grads):
+        assert (p.grad is None) == (g is None)
+        if g is not None:
+            torch.testing.assert_close(p.grad, g, rtol=1e-4, atol=1e-5)     # attention's sums in any order

@@ -34,3 +34,31 @@ def test_casts_leave_the_bias_in_fp32(router, cast):
     index, weight = r(torch.randn(5, 8, dtype=r.weight.dtype))
     weight.sum().backward()
     assert r.weight.grad.dtype == r.weight.dtype
+
+
+def test_evaluation_counts_nothing(router):
+    x = torch.randn(7, 8)
+    router.eval()
+    router(x)
+    assert not router.load().any()
+    router.train()
+    router(x)
+    with torch.no_grad():
+        router(x)
+    assert router.load().sum() == 28
+
+
+@pytest.mark.parametrize("reentrant", [False, True])
+def test_a_recomputed_pass_counts_once(router, reentrant):
+    from torch.utils.checkpoint import checkpoint
+    x = torch.randn(7, 8, requires_grad=True)
+    passes = []
+
+    def block(x):
+        passes.append(1)
+        return router(x)[1] * x[:, :2]
+    checkpoint(block, x, use_reentrant=reentrant).sum().backward()
+    assert len(passes) == 2 and router.load().sum() == 14
+    assert router.weight.grad.any()
+    checkpoint(block, x, use_reentrant=reentrant).sum().backward()
+    assert len(passes) == 4 and router.load().sum() == 28
