@@ -55,7 +55,9 @@ class ExpertRouter(torch.nn.Module):
         self.cfg = M.moara_route_default_config(experts=experts, top_k=top_k, **config)
         self.weight = torch.nn.Parameter(torch.randn(experts, d_model) * d_model ** -0.5)
         self.register_buffer("bias", torch.zeros(experts, dtype=torch.float32))
-        self.register_buffer("counts", torch.zeros(experts, dtype=torch.int64))
+        # a tensor but no buffer: DistributedDataParallel gives every rank the first one's buffers at each forward
+        # pass, and a rank's counts are its own
+        self.counts = torch.zeros(experts, dtype=torch.int64)
 
     def _apply(self, fn, recurse=True):
         """Casts of the model (`.bfloat16()`, `.to(dtype)`) leave the bias in fp32: it moves by 1e-3 a step."""
@@ -63,13 +65,37 @@ class ExpertRouter(torch.nn.Module):
         super()._apply(fn, recurse)
         if self.bias.dtype != torch.float32:
             self.bias = bias.to(self.bias.device)
+        at = self.bias.device
+        self.counts = torch.zeros_like(self.counts, device=at) if self.counts.is_meta else self.counts.to(at)
         return self
+
+    def _save_to_state_dict(self, destination, prefix, keep_vars):
+        super()._save_to_state_dict(destination, prefix, keep_vars)
+        destination[prefix + "counts"] = self.counts
+
+    def _load_from_state_dict(self, state_dict, prefix, local_metadata, strict, missing_keys, unexpected_keys, error_msgs):
+        super()._load_from_state_dict(state_dict, prefix, local_metadata, strict, missing_keys, unexpected_keys, error_msgs)
+        key = prefix + "counts"
+        if key in unexpected_keys:
+            unexpected_keys.remove(key)
+        saved = state_dict.get(key)
+        if saved is None:
+            if strict:
+                missing_keys.append(key)
+        elif saved.shape != self.counts.shape:
+            error_msgs.append(f"size mismatch for {key}: {tuple(saved.shape)}, the router has {tuple(self.counts.shape)}")
+        elif local_metadata.get("assign_to_params_buffers", False):
+            self.counts = saved
+        else:
+            self.counts.copy_(saved)
 
     def forward(self, x: torch.Tensor, mask: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
         """x: tokens x d_model; mask: tokens, False where a token is not routed. An index is -1 (weight 0)
         where there is no expert."""
         with torch.autocast(x.device.type, enabled=False):      # the choice is sensitive to the logits' rounding
             logits = torch.nn.functional.linear(x.float(), self.weight.float())
+        if self.counts.device != x.device:      # where buffers are moved one by one
+            self.counts = self.counts.to(x.device)
         again = torch._C._current_graph_task_id() != -1         # inside a backward pass
         return route(logits, self.cfg, self.bias, mask, self.counts if self.training and not again else None)
 

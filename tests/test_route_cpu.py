@@ -1,4 +1,5 @@
 """The router module's host side, with a stand-in for the library's call (no GPU needed)."""
+import numpy as np
 import pytest
 import torch
 
@@ -62,3 +63,57 @@ def test_a_recomputed_pass_counts_once(router, reentrant):
     assert router.weight.grad.any()
     checkpoint(block, x, use_reentrant=reentrant).sum().backward()
     assert len(passes) == 4 and router.load().sum() == 28
+
+
+def test_counts_in_checkpoints_copies_and_moves(router):
+    import copy
+    router(torch.randn(7, 8))
+    load = router.load().copy()
+    assert load.sum() == 14
+    sd = router.state_dict()
+    assert list(sd) == ["weight", "bias", "counts"] and torch.equal(sd["counts"], router.counts)
+    other = torch.nn.ModuleDict({"a": copy.deepcopy(router)})
+    other["a"].counts.zero_()
+    assert np.array_equal(router.load(), load)
+    other.load_state_dict({"a." + k: v for k, v in sd.items()})
+    assert np.array_equal(other["a"].load(), load) and other["a"].counts is not sd["counts"]
+    for bad in ({k: v for k, v in sd.items() if k != "counts"}, {**sd, "counts": sd["counts"][:3]}):
+        with pytest.raises(RuntimeError):
+            router.load_state_dict(bad)
+    assert router.load_state_dict({"weight": sd["weight"]}, strict=False).missing_keys == ["bias", "counts"]
+    for cast in (router.half, router.double, lambda: router.type(torch.float32)):
+        cast()
+        assert router.counts.dtype == torch.int64 and np.array_equal(router.load(), load)
+    with torch.device("meta"):
+        empty = R.ExpertRouter(8, 6, 2)
+    empty.load_state_dict(sd, assign=True)
+    assert np.array_equal(empty.load(), load)
+    with torch.device("meta"):
+        empty = R.ExpertRouter(8, 6, 2)
+    assert not empty.to_empty(device="cpu").load().any()
+    assert empty.to("meta").counts.is_meta
+
+
+def _rank(rank, file):
+    torch.distributed.init_process_group("gloo", init_method=f"file://{file}", rank=rank, world_size=2)
+    M.moara_route_default_config = lambda **kw: M.moara_route_config(**kw)
+
+    def fake(logits, cfg, bias=None, mask=None, counts=None):
+        counts[rank] += logits.shape[0]
+        return torch.zeros(logits.shape[0], 2, dtype=torch.int32), logits.softmax(1)[:, :2]
+    R.route = fake
+    torch.manual_seed(0)
+    router = R.ExpertRouter(8, 6, 2)
+    ddp = torch.nn.parallel.DistributedDataParallel(router)
+    for _ in range(3):          # gradients accumulated over three passes, exchanged in each
+        ddp(torch.ones(5, 8))[1].sum().backward()
+    want = torch.zeros(6, dtype=torch.int64)
+    want[rank] = 15
+    assert torch.equal(router.counts, want), (rank, router.counts)
+    torch.distributed.all_reduce(router.counts)
+    assert router.counts.tolist() == [15, 15, 0, 0, 0, 0]
+    torch.distributed.destroy_process_group()
+
+
+def test_ranks_keep_their_own_counts(tmp_path):
+    torch.multiprocessing.spawn(_rank, args=(str(tmp_path / "rendezvous"),), nprocs=2)
