@@ -653,23 +653,26 @@ def moara_route_default_config(**overrides) -> moara_route_config:
 
 
 def _route_logits(cfg, logits):
-    """(GPU, tokens, row stride) of the logits, checked; cfg.logits_dtype follows them."""
+    """(configuration for the logits' type, GPU, tokens, row stride) of the logits, checked. The caller's
+    configuration stays as it is: threads may share one for logits of both types."""
     shape, strides = logits.shape, logits.stride()
     if len(shape) != 2 or shape[1] != cfg.experts or (shape[1] > 1 and strides[1] != 1):
         raise ValueError(f"logits: need tokens x {cfg.experts} with unit stride along the experts, got "
                          f"{tuple(shape)}, strides {strides}")
-    cfg.logits_dtype = _dtype_id(logits, "logits")
-    tokens = shape[0]
-    return _on_gpu(logits, None, "logits"), tokens, (strides[0] if tokens > 1 else shape[1])
+    dtype, tokens = _dtype_id(logits, "logits"), shape[0]
+    if cfg.logits_dtype != dtype:
+        cfg = moara_route_config.from_buffer_copy(cfg)
+        cfg.logits_dtype = dtype
+    return cfg, _on_gpu(logits, None, "logits"), tokens, (strides[0] if tokens > 1 else shape[1])
 
 
 @_streamed
 def moara_route(cfg: moara_route_config, logits, bias=None, mask=None, counts=None):
     """moara_route of the C ABI: (index int32, weight float32), both tokens x top_k. logits: tokens x experts,
-    float32 or bfloat16, rows any distance apart (cfg.logits_dtype follows). bias: float32, one for each
+    float32 or bfloat16, rows any distance apart (whatever cfg.logits_dtype says). bias: float32, one for each
     expert; mask: bool or uint8, one for each token; counts: int64, one for each expert, added to."""
     import torch
-    dev, tokens, ld = _route_logits(cfg, logits)
+    cfg, dev, tokens, ld = _route_logits(cfg, logits)
     if bias is not None:
         bias = _vector(bias, dev, torch.float32, cfg.experts, "bias")
     if mask is not None:
@@ -688,7 +691,7 @@ def moara_route_backward(cfg: moara_route_config, logits, index, grad_weight):
     """moara_route_backward of the C ABI: the gradient of the logits, contiguous, of their type. index: as
     moara_route gave it; grad_weight: float32, tokens x top_k."""
     import torch
-    dev, tokens, ld = _route_logits(cfg, logits)
+    cfg, dev, tokens, ld = _route_logits(cfg, logits)
     n = tokens * cfg.top_k
     i = _vector(index, dev, torch.int32, n, "index")
     w = _vector(grad_weight, dev, torch.float32, n, "grad_weight")

@@ -176,3 +176,21 @@ def test_oracle_pins_catch_planted_mistakes(plant, monkeypatch):
         pin = test_oracle_routing_of_a_known_row
     with pytest.raises(AssertionError):
         pin()
+
+
+# ---------------------------------------------------------------- the binding
+
+def test_a_shared_routing_configuration_is_not_written(monkeypatch):
+    """Calls on logits of both types, interleaved as threads may, each with its own type and the caller's other fields."""
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(M, "_on_gpu", lambda t, device, what: 0)
+    cfg = M.moara_route_config(experts=6, top_k=2, groups=3, top_groups=2, group_best=2, score=M.MOARA_SIGMOID, renormalise=1,
+                               logits_dtype=M.MOARA_F32, scale=2.5)
+    before = bytes(cfg)
+    half, dev, tokens, ld = M._route_logits(cfg, torch.zeros(4, 6, dtype=torch.bfloat16))
+    full = M._route_logits(cfg, torch.zeros(4, 6))[0]
+    assert bytes(cfg) == before
+    assert half.logits_dtype == M.MOARA_BF16 and full.logits_dtype == M.MOARA_F32 and (dev, tokens, ld) == (0, 4, 6)
+    for name, _ in M.moara_route_config._fields_:
+        if name != "logits_dtype":
+            assert getattr(half, name) == getattr(full, name) == getattr(cfg, name)
