@@ -23,6 +23,7 @@ from . import moara as M
 class _Route(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, cfg, bias, mask, counts):
+        cfg = M.moara_route_config.from_buffer_copy(cfg)        # the caller may change its own before the backward pass
         index, weight = M.moara_route(cfg, logits, bias=bias, mask=mask, counts=counts)
         ctx.cfg = cfg
         ctx.save_for_backward(logits, index)

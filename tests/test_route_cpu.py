@@ -117,3 +117,23 @@ def _rank(rank, file):
 
 def test_ranks_keep_their_own_counts(tmp_path):
     torch.multiprocessing.spawn(_rank, args=(str(tmp_path / "rendezvous"),), nprocs=2)
+
+
+def test_the_backward_pass_has_the_forward_pass_configuration(monkeypatch):
+    """A configuration that the caller changes in between, for another layer or step, does not reach the gradient."""
+    seen = []
+
+    def forward(cfg, logits, **kw):
+        return torch.zeros(4, 2, dtype=torch.int32), logits[:, :2] * cfg.scale
+
+    def backward(cfg, logits, index, grad):
+        seen.append((cfg.experts, cfg.top_k, cfg.score, cfg.scale))
+        return torch.zeros_like(logits)
+    monkeypatch.setattr(M, "moara_route", forward)
+    monkeypatch.setattr(M, "moara_route_backward", backward)
+    cfg = M.moara_route_config(experts=6, top_k=2, score=M.MOARA_SIGMOID, scale=2.5)
+    x = torch.randn(4, 6, requires_grad=True)
+    weight = R.route(x, cfg)[1]
+    cfg.experts, cfg.top_k, cfg.score, cfg.scale = 64, 8, M.MOARA_SOFTMAX, 1.0
+    weight.sum().backward()
+    assert seen == [(6, 2, M.MOARA_SIGMOID, 2.5)]
