@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+from collections.abc import Collection, Iterator
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -490,17 +491,42 @@ def _call(device: int, fn, *args):
         _check(rc)
 
 
+def _device_of(values) -> Optional[int]:
+    """The GPU of the first tensor (or GradArgs, AdamWArgs) among the arguments of a call and in its lists."""
+    for v in values:
+        if isinstance(v, (GradArgs, AdamWArgs)):
+            d = v.device
+        elif hasattr(v, "get_device"):
+            d = v.get_device()
+        else:
+            d = _device_of(v) if isinstance(v, Collection) and not isinstance(v, (str, np.ndarray)) else None
+        if d is not None and d >= 0:
+            return d
+    return None
+
+
+def _stream_on(stream, device: Optional[int]):
+    """The torch stream that `stream` names on the tensors' GPU: a torch stream of it, or the handle of a HIP stream
+    of it (0: its default stream). No tensors (device None): the current GPU for a handle."""
+    import torch
+    if isinstance(stream, int):
+        return torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+    if device is not None and stream.device_index != device:
+        raise ValueError(f"the stream is on cuda:{stream.device_index}, the tensors are on cuda:{device}")
+    return stream
+
+
 def _streamed(f):
-    """Adds the argument `stream` (a torch stream or a hipStream_t as an int; None: the current one): the call runs
-    with it as the current stream, so what it allocates belongs to that stream too."""
+    """Adds the argument `stream` (a torch stream or a hipStream_t as an int, of the tensors' GPU; None: the current
+    one there): the call runs with it as the current stream, so what it allocates belongs to that stream too."""
     @functools.wraps(f)
     def call(*args, stream=None, **kw):
         if stream is None:
             return f(*args, **kw)
         import torch
-        if isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
-        with torch.cuda.stream(stream):
+        args = [list(a) if isinstance(a, Iterator) else a for a in args]
+        kw = {k: list(a) if isinstance(a, Iterator) else a for k, a in kw.items()}
+        with torch.cuda.stream(_stream_on(stream, _device_of((*args, *kw.values())))):
             return f(*args, **kw)
     return call
 

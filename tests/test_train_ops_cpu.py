@@ -194,3 +194,54 @@ def test_a_shared_routing_configuration_is_not_written(monkeypatch):
     for name, _ in M.moara_route_config._fields_:
         if name != "logits_dtype":
             assert getattr(half, name) == getattr(full, name) == getattr(cfg, name)
+
+
+class _OnGpu:
+    """What the binding asks a tensor for, on a GPU that is not here."""
+
+    def __init__(self, device):
+        self.device = device
+
+    def get_device(self):
+        return self.device
+
+
+def test_a_given_stream_is_one_of_the_tensors_gpu(monkeypatch):
+    """With the tensors on GPU 1 and GPU 0 current: handles are of GPU 1, streams of GPU 0 are refused, and the call
+    sees the stream as the current one."""
+    torch = pytest.importorskip("torch")
+    now = []
+
+    class Stream:
+        def __init__(self, handle, device_index):
+            self.cuda_stream, self.device_index = handle, device_index
+
+    class Current:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            now.append(self.stream)
+
+        def __exit__(self, *exc):
+            now.pop()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda device=None: Stream(0, 0 if device is None else device))
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: Stream(handle, 0 if device is None else device))
+    monkeypatch.setattr(torch.cuda, "stream", Current)
+    call = M._streamed(lambda *a, **kw: (now[-1].cuda_stream, now[-1].device_index, [list(x) for x in a if isinstance(x, list)])
+                       if now else None)
+    t, cpu = _OnGpu(1), _OnGpu(-1)
+    marshalled = M.GradArgs.__new__(M.GradArgs)
+    marshalled.device = 1
+    cfg = M.moara_route_config()
+    for args, kw in (((t,), {}), ((cfg, t), {}), (([None, cpu, t],), {}), ((None, 1.0), dict(args=marshalled)),
+                     (({0: t}.values(), 1.0), {}), ((None, 1.0), dict(lr=np.float32(1), steps=np.zeros(2), grads=(t,)))):
+        assert call(*args, **kw) is None
+        assert call(*args, stream=0, **kw)[:2] == (0, 1)
+        assert call(*args, stream=77, **kw)[:2] == (77, 1)
+        assert call(*args, stream=Stream(5, 1), **kw)[:2] == (5, 1)
+        with pytest.raises(ValueError):
+            call(*args, stream=Stream(5, 0), **kw)
+    assert call((x for x in (None, t)), stream=77) == (77, 1, [[None, t]])      # a generator is read once
+    assert call([], stream=77)[:2] == (77, 0) and call([], stream=Stream(5, 1))[:2] == (5, 1)
