@@ -451,7 +451,8 @@ int moara_route_default_config(moara_route_config* out);
  * the top_groups best groups by their best (or two best) c are kept, and of their experts
  * the top_k largest c are chosen, in falling order, the lowest index first among equals. The
  * weights are s (without the bias) of the chosen experts, over their sum if renormalise, times
- * scale. Scores and sums are fp32 (the softmax's sum 64 bits).
+ * scale. Scores and sums are fp32 (the softmax's sum 64 bits; groups whose
+ * sums are less than fp32 holds are still in order, ahead of groups with nothing to choose).
  *   logits: tokens x experts, row_stride elements from one row to the next.
  *   bias:   experts floats, or null. -infinity takes an expert out.
  *   mask:   tokens bytes, or null; a token with 0 is not routed.

@@ -125,6 +125,12 @@ __device__ __forceinline__ uint32_t order_key(float c) {
 __device__ __forceinline__ float key_value(uint32_t k) {
   return __uint_as_float((int)k < 0 ? k & 0x7FFFFFFFu : ~k);
 }
+// The key of a + b. Two finite values (biases of the type's lowest one) may sum to less than fp32 holds: half of it,
+// at most -2^127, has a key from 2^23 to 2^24 - 1, half of which is above 0 and below all keys of finite sums.
+__device__ __forceinline__ uint32_t sum_key(float a, float b) {
+  const float s = a + b;
+  return s > -__builtin_inff() ? order_key(s) : order_key(0.5f * a + 0.5f * b) >> 1;
+}
 
 // A row's largest logit and its sum of exponentials (softmax). The sum is taken in 64 bits: an expert's
 // score must not depend on the order of the others.
@@ -301,7 +307,7 @@ __device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const RouteParam
   wave_sync();
   for (int g = lane; g < p.groups; g += LANES) {
     const uint32_t best = (uint32_t)(x.value[g] >> 32), next = (uint32_t)x.value[g];
-    const uint32_t v = p.group_best == 2 && next ? order_key(key_value(best) + key_value(next)) : best;
+    const uint32_t v = p.group_best == 2 && next ? sum_key(key_value(best), key_value(next)) : best;
     x.value[g] = (uint64_t)v << 32 | (uint32_t)(ROUTE_MAX_GROUPS - 1 - g);
   }
   wave_sync();

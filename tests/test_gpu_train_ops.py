@@ -779,3 +779,28 @@ def test_calls_in_a_captured_graph():
         got = [t.clone() for t in res] + [t.clone() for t in state]
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want)), k
+
+
+@pytest.mark.parametrize("E,groups", [(16, 4), (60, 6), (64, 32), (256, 8), (300, 3), (1024, 64)])
+@pytest.mark.parametrize("best", [1, 2])
+def test_route_groups_whose_experts_have_the_lowest_bias(E, groups, best):
+    """A bias of the type's lowest value keeps an expert for when nothing else is left, in groups as without: two of
+    them sum to less than fp32 holds. The first group has nothing at all (-inf); biases are all the lowest value, or
+    but for one expert of the last group, or from 0.6 to 1 of it, in any order."""
+    M = _M()
+    low = float(torch.finfo(F32).min)
+    x, g = _logits(6, E, 81, F32)
+    for form in ("all", "but one", "spread"):
+        bias = np.full(E, low, np.float32)
+        if form == "spread":
+            bias *= np.float32(0.6 + 0.4 * g.random(E))
+        bias[:E // groups] = -math.inf
+        if form == "but one":
+            bias[E - 1] = 0
+        for top in (1, groups - 1):
+            cfg = M.moara_route_default_config(experts=E, top_k=2, groups=groups, top_groups=top, group_best=best)
+            index, weight = M.moara_route(cfg, x, bias=torch.from_numpy(bias).cuda())
+            ri, rw, _ = O.route(_np(x), 2, False, bias.astype(np.float64), groups=groups, top_groups=top, group_best=best)
+            assert (ri >= 0).all()
+            assert np.array_equal(index.cpu().numpy(), ri), (form, top)
+            np.testing.assert_allclose(_np(weight), rw, rtol=16 * EPS32 * math.log2(E), atol=1e-12)
