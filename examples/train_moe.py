@@ -74,8 +74,9 @@ class Model(torch.nn.Module):
         return self.head(self.norm(x))
 
 
-def train(steps=40, bits=8, seed=0, say=print):
-    """Losses of the steps and the largest share of the tokens an expert had in the last one (layer by layer)."""
+def train(steps=40, bits=8, seed=0, rate=1e-2, say=print):
+    """Losses of the steps and the largest share of the tokens an expert had in the last one (layer by layer).
+    rate: of the balancing bias."""
     torch.manual_seed(seed)
     model = Model().cuda()
     targets, others = moara_targets(model)
@@ -94,7 +95,7 @@ def train(steps=40, bits=8, seed=0, say=print):
         opt.zero_grad()
         share = [float(layer.router.load().max() / layer.router.load().sum()) for layer in model.layers]
         for layer in model.layers:
-            layer.router.balance(1e-2)
+            layer.router.balance(rate)
         losses.append(float(loss.detach()))
         if step % 10 == 0 or step == steps - 1:
             say(f"step {step}: loss {losses[-1]:.4f}, gradient norm {float(opt.grad_norm):.3f}, "

@@ -405,3 +405,12 @@ def test_counts_are_those_of_training(reentrant):
         assert (p.grad is None) == (g is None)
         if g is not None:
             torch.testing.assert_close(p.grad, g, rtol=1e-4, atol=1e-5)     # attention's sums in any order
+
+
+def test_balancing_spreads_the_example_tokens():
+    """The bias moves by 0.4 in 40 steps, between scores from 0 to 1. Towards an even load no layer's busiest expert has
+    over twice an even share (an eighth); the other way those above the mean stay there and gain, fewer and fewer."""
+    even = _example().train(steps=40, rate=1e-2, say=lambda s: print("[moe]", s, flush=True))[1]
+    uneven = _example().train(steps=40, rate=-1e-2, say=lambda s: print("[moe]", s, flush=True))[1]
+    assert max(even) <= 0.25, even
+    assert min(uneven) > max(even), (even, uneven)
