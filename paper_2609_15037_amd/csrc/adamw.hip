@@ -7,8 +7,6 @@ namespace {
 // Vectors of any alignment (the hardware takes unaligned vector accesses). A lane's 16 bytes and the next
 // lane's are neighbours in every access: lanes that took 32 consecutive bytes of fp32 in two halves
 // touched each line twice (32-bit AdamW over 66 M elements 254 us instead of 227 side by side).
-typedef uint16_t u16x4u __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint16_t u16x8u __attribute__((ext_vector_type(8), aligned(2)));
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32u __attribute__((aligned(1)));
 typedef uint16_t u16u __attribute__((aligned(1)));
