@@ -111,25 +111,24 @@ class _AdamW:
                     raise ValueError(f"parameter {i}: strides {p.stride()} of shape {tuple(p.shape)} leave gaps")
             self.state, self.form = [M.moara_adamw_state(p, self.cfg.bits) for p in self.params], form
 
-    @staticmethod
-    def _grad(g: torch.Tensor, p: torch.Tensor) -> torch.Tensor:
-        if g.layout == torch.strided and g.stride() == p.stride():
-            return g
-        return torch.empty_like(p, dtype=g.dtype).copy_(g.to_dense() if g.layout != torch.strided else g)
-
     def step(self, lr: float, clip: Optional[torch.Tensor]) -> None:
         self._make()
-        params, grads, copies = list(self.params), [], []
-        for i, (p, (shape, stride)) in enumerate(zip(self.params, self.form)):
-            if p.shape != shape:
-                raise ValueError(f"parameter {i} has shape {tuple(p.shape)}, its moments {shape}")
-            g = p.grad
-            if g is not None:
-                if p.stride() != stride and _order(shape, p.stride()) != _order(shape, stride):
-                    params[i] = torch.empty_strided(shape, stride, dtype=p.dtype, device=p.device).copy_(p)
+        params, grads, copies = list(self.params), [p.grad for p in self.params], []
+        strided = torch.strided
+        for i, (p, g) in enumerate(zip(self.params, grads)):    # the usual case is a few attribute reads
+            if g is None:
+                continue
+            stride = p.stride()
+            if stride != self.form[i][1]:
+                shape, made = self.form[i]
+                if p.shape != shape:
+                    raise ValueError(f"parameter {i} has shape {tuple(p.shape)}, its moments {shape}")
+                if _order(shape, stride) != _order(shape, made):
+                    params[i] = p = torch.empty_strided(shape, made, dtype=p.dtype, device=p.device).copy_(p)
+                    stride = made
                     copies.append(i)
-                g = self._grad(g, params[i])
-            grads.append(g)
+            if g.layout is not strided or g.stride() != stride:
+                grads[i] = torch.empty_like(p, dtype=g.dtype).copy_(g if g.layout is strided else g.to_dense())
         args = M.AdamWArgs(params, grads, *([s[k] for s in self.state] for k in (0, 1)),
                            scales=[s[2] for s in self.state] if self.cfg.bits == 8 else None,
                            weight_decay=[self.weight_decay if p.dim() > 1 else 0.0 for p in self.params])
