@@ -347,9 +347,9 @@ int moara_reset_kernel_stats(moara_state* st, void* stream);
 /* ------------------------------------------------------------------------------------
  * Operators of a training step beside the projected matrices' update: the norm of all
  * gradients and their clipping (the paper clips at 1.0), AdamW for the parameters that are
- * not projected (Appendix D), and the routing of tokens to experts, whose counts say which
- * experts' matrices a step is for. They hold no state: every buffer is the caller's, lists
- * travel in the kernels' arguments, nothing is allocated and nothing synchronises, so a call
+ * not projected (Appendix D), and the routing of tokens to experts (one without tokens has no
+ * gradient: its matrices are not active in moara_step). They hold no state: every buffer is the caller's,
+ * lists travel in the kernels' arguments, nothing is allocated and nothing synchronises, so a call
  * can be captured in a graph (its pointers and numbers are then the graph's). They act on the
  * current device. Pointers need the alignment of their element type only; vectors are
  * wide loads from any such address. Results do not depend on timing: the same arguments
@@ -451,8 +451,8 @@ int moara_route_default_config(moara_route_config* out);
  * the top_groups best groups by their best (or two best) c are kept, and of their experts
  * the top_k largest c are chosen, in falling order, the lowest index first among equals. The
  * weights are s (without the bias) of the chosen experts, over their sum if renormalise, times
- * scale. Scores and sums are fp32 (the softmax's sum 64 bits; groups whose
- * sums are less than fp32 holds are still in order, ahead of groups with nothing to choose).
+ * scale. Scores and sums are fp32 (the softmax's sum 64 bits; groups whose sums are less than fp32
+ * holds are still in order, ahead of groups with nothing to choose).
  *   logits: tokens x experts, row_stride elements from one row to the next.
  *   bias:   experts floats, or null. -infinity takes an expert out.
  *   mask:   tokens bytes, or null; a token with 0 is not routed.

@@ -336,9 +336,10 @@ __device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const RouteParam
 // addition in about 20 ns, so at most 256 workgroups walk over the tokens (with 1024 the counts cost 20 us of
 // 26 for 16384 tokens of 64 experts, with 128 the rest takes as much longer). They are whole numbers: the
 // order of the additions does not change them.
-// fp32 logits, with bias and counts: 8 tokens, 64 experts, top 6: 4.2 us; 16384 tokens of the same 8.7 us (6.5
-// without counts); 32768 tokens, 256 experts in 8 groups, top 8: 23 us (18; a scan of all candidates for each
-// choice, with divisions and one lane for a group, took 41); 16384 tokens, 512 experts, top 12: 28 us.
+// fp32 logits, with bias and counts, in a captured graph (a kernel trace gives up to 10 % more): 113 tokens, 64
+// experts, top 6: 4.8 us; 16384 tokens of the same 8.6 us (6.4 without counts); 32768 tokens, 256 experts in 8 groups,
+// top 8: 23.4 us (18.1; a scan of all candidates for each choice, with divisions and one lane for a group, took 41);
+// without groups 20.1 (15.3); 16384 tokens, 512 experts, top 12: 27.9 us.
 enum { NO_GROUPS, EVEN_GROUPS, ANY_GROUPS };
 constexpr int ROUTE_THREADS = 1024;
 template <int LANES, int V, int DEP, int GROUPS>
@@ -432,8 +433,10 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_route(RouteParams p) {
 // renormalised, t_j = u_j (dw_j - sum dw u) and d l_j = t_j, times 1 - s_j for the sigmoid (the softmax's own
 // sum vanishes); else t_j = dw_j s_j, times 1 - s_j for the sigmoid, and d l_e = t_e - s_e sum t for the softmax,
 // the only form that needs the whole row.
-// A row is put together in LDS and written once. Bound by the write: 32768 tokens, 256 experts, fp32,
-// renormalised: 9.2 us, 3.6 TB/s; the whole softmax row 14 us; 16384 tokens of 64 experts 4 us, most of it the launch.
+// A row is put together in LDS and written once. 32768 tokens, 256 experts, fp32 (in a captured graph): renormalised 9.1
+// us, 3.9 TB/s of which the write alone would take 6: a token's index, its logit, the shares and the row follow one
+// another, and a workgroup begins the next token when they are done; the whole softmax row 13.4 us, 5.2 TB/s;
+// 16384 tokens of 64 experts 3.3 and 4.0 us, most of it the launch.
 template <int LANES, int V>
 __global__ __launch_bounds__(256) void k_route_backward(RouteParams p) {
   constexpr int TOK = 256 / LANES;
@@ -501,11 +504,15 @@ __global__ __launch_bounds__(256) void k_route_balance(int E, long long* __restr
 // Lanes of a token: as few as hold its choices, and its experts at sixteen a lane (eight lanes: at four, or at
 // eight where there are tokens for half of the CUs). Fewer lanes share a wave's instructions among more
 // tokens: 65536 tokens of 8 experts, top 2, take 6 us on eight lanes and 12 on sixteen; 16384 of 512 experts, top
-// 12, with counts 28 us on 32 lanes and 34 on a wave. Top 6 of 64 experts with counts, on eight and on sixteen
-// lanes: 4096 tokens 6.6 and 6.1 us, 8192 7.3 and 7.5, 16384 8.7 and 10.4, 65536 15.5 and 18.5.
+// 12, with counts 28 us on 32 lanes and 34 on a wave. Top 6 of 64 experts on eight and on sixteen lanes, with counts:
+// 4096 tokens 6.6 and 6.0 us, 8192 7.2 and 7.4, 14000 8.2 and 9.4, 16384 8.6 and 10.3, 65536 15.5 and 18.5; without:
+// 8192 6.3 and 4.7, 16384 6.4 and 4.8, 32768 6.7 and 7.6, 65536 10.7 and 13.1. One rule for both, between the two
+// crossings.
 // Few tokens take more lanes, as long as one round of workgroups holds them (of 64 where each adds to the
 // counts: 8192 tokens of 256 experts 10.8 us with 128 workgroups, 12.5 with 256): a lane's experts are straight
-// code that such a call runs once (113 tokens of 138 experts 9.4 us on sixteen lanes, 4.5 on a wave).
+// code that such a call runs once (113 tokens of 138 experts 7.9 us on sixteen lanes, 5.3 on a wave).
+// The backward pass takes the same lanes: over these shapes it is at most 0.4 us behind the best for it (4096 tokens
+// of 256 experts 3.7 us on a wave, 3.4 on sixteen or 32 lanes).
 int lanes_of(const RouteParams& p) {
   const int most8 = p.tokens >= 128 * (ROUTE_THREADS / 8) ? 64 : 32;
   int lanes = p.k <= 8 && p.E <= most8 ? 8 : p.k <= 16 && p.E <= 256 ? 16 : p.k <= 32 && p.E <= 512 ? 32 : 64;
@@ -524,7 +531,7 @@ int64_t workgroups(const RouteParams& p, int threads, int64_t most) {
 hipError_t launch_route(const RouteParams& p, hipStream_t st) {
   const dim3 g((uint32_t)workgroups(p, ROUTE_THREADS, 256)), b(ROUTE_THREADS);
   const int s = (int)p.group_size;
-  // the same 32768 tokens through the form for groups of any size: 26.9 us
+  // the same 32768 tokens, with counts: 23.3 us, through the form for groups of any size 26.7
   const int groups = p.groups == 1 ? NO_GROUPS : s >= 4 && s <= 64 && (s & (s - 1)) == 0 ? EVEN_GROUPS : ANY_GROUPS;
 #define ROUTE(LANES, V, DEP)                                                                                     \
   do {                                                                                                           \
@@ -533,8 +540,8 @@ hipError_t launch_route(const RouteParams& p, hipStream_t st) {
     else hipLaunchKernelGGL((k_route<LANES, V, DEP, ANY_GROUPS>), g, b, 0, st, p);                               \
   } while (0)
   const int lanes = lanes_of(p);
-  // a lane's best eight are enough: 32768 tokens of 256 experts in 8 groups, with counts, 24.1 us, with lists of
-  // sixteen 26.4
+  // a lane's best eight are enough: 32768 tokens of 256 experts in 8 groups, with counts, 23.3 us, with lists of
+  // sixteen 26.2
   const bool few = p.k <= 8;
 #define ROUTE_ON(LANES)                                   \
   do {                                                    \
