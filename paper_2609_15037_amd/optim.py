@@ -288,12 +288,13 @@ class MoARa(torch.optim.Optimizer):
             if any(active):
                 # torch's side streams and the default one do not wait for each other by themselves: gradients (and
                 # their copies) are made on the current stream, weights and gradients used or freed on it afterwards
-                here, default = torch.cuda.current_stream(), torch.cuda.default_stream()
-                if here != default:
+                here = torch.cuda.current_stream()
+                default = torch.cuda.default_stream() if here.cuda_stream != 0 else None
+                if default is not None:
                     default.wait_stream(here)
                 M.moara_step_mixed(self._st, tg["params"], grads, self._g32, lr=float(tg["lr"]),
                                    active=None if all(active) else active)
-                if here != default:
+                if default is not None:
                     here.wait_stream(default)
         if self._adamw is not None:
             og = self.param_groups[1]
