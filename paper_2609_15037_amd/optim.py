@@ -355,12 +355,12 @@ class MoARa(torch.optim.Optimizer):
     def load_state_dict(self, sd: Dict) -> None:
         if (self._own is not None and sd.get("adamw") is not None) or (self._adamw is not None and "adamw_own" in sd):
             raise ValueError("the state is of the other AdamW (adamw_bits) than this optimizer's")
-        for g, lr in zip(self.param_groups, sd["lr"]):
-            g["lr"] = lr
         if self._adamw is not None and sd["adamw"] is not None:
             self._adamw.load_state_dict(sd["adamw"])
         if self._own is not None and sd.get("adamw_own") is not None:
             self._own.load_state_dict(sd["adamw_own"])
+        for g, lr in zip(self.param_groups, sd["lr"]):      # after what may be refused
+            g["lr"] = lr
         if sd["moara"] is None:
             return
         with self._device():

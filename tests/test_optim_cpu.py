@@ -144,3 +144,16 @@ def test_library_adamw_refuses_other_types_at_the_start(dtype, monkeypatch):
             optim.MoARa([(w, M.MOARA_Q)], [p], adamw_bits=bits)
         optim.MoARa([(w, M.MOARA_Q)], [torch.nn.Parameter(p.detach().bfloat16())], adamw_bits=bits)
     optim.MoARa([(w, M.MOARA_Q)], [p])
+
+
+def test_a_refused_state_leaves_the_rates(monkeypatch):
+    from paper_2609_15037_amd import optim
+    monkeypatch.setattr(M, "moara_default_config", lambda **kw: None)
+    monkeypatch.setattr(M, "moara_adamw_default_config", lambda **kw: M.moara_adamw_config(**kw))
+    make = lambda n, lr: optim.MoARa([(torch.nn.Parameter(torch.zeros(4, 6)), M.MOARA_Q)], [torch.nn.Parameter(torch.zeros(n))],
+                                     lr=lr, adamw_bits=8)
+    a, b = make(5, 1e-2), make(7, 3e-3)
+    with pytest.raises(ValueError):
+        a.load_state_dict(b.state_dict())
+    assert [g["lr"] for g in a.param_groups] == [1e-2] * 2
+    make(7, 1e-2).load_state_dict(b.state_dict())
