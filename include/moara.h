@@ -477,6 +477,168 @@ int moara_route_backward(const moara_route_config* cfg, const void* logits, int6
  * counts are set to zero. Errors: MOARA_E_ARG, MOARA_E_HIP. */
 int moara_route_balance(int32_t experts, int64_t* counts, float* bias, float rate, void* stream);
 
+/* ------------------------------------------------------------------------------------
+ * Losses of a training step, forward and backward: log-probabilities of given tokens under
+ * logits, losses of paired responses and of a clipped policy over those log-probabilities,
+ * and the load-balancing loss of expert routing. As the operators above they hold no state,
+ * allocate nothing, do not synchronise, can be captured, act on the current device, take
+ * pointers of their element type's alignment, and give the same bits for the same arguments.
+ *
+ * Packed tokens. The losses over sequences take `tokens` values one after another. Sequence s
+ * of `sequences` is [offsets[s], offsets[s + 1]) (int64 device memory, sequences + 1 values that do
+ * not fall, from 0 to tokens; sequences may be empty), or, without offsets, the s-th of equal
+ * parts (tokens is a multiple of sequences). mask (tokens bytes, or null): a token with 0 is
+ * left out, as are tokens before the first and behind the last sequence: whatever values they
+ * have, they add nothing, and their gradients are 0. What is outside [0, tokens) is never read
+ * or written, whatever the offsets are; offsets that fall give sums of some of the tokens.
+ * ------------------------------------------------------------------------------------ */
+
+/* Log-probabilities of labels. With x = scale logits[t] and p = softmax(x):
+ *   out_logp[t] = log p[label],  out_entropy[t] = -sum_j p_j log p_j  (null: not wanted).
+ * A label outside [0, vocab) has no log-probability: both are 0 and its row is not read. A row
+ * with a NaN or +infinite logit, or with none above -infinity, gives NaN.
+ *   logits: tokens rows of vocab consecutive elements; row r starts at element
+ *           (r / inner) outer_stride + (r % inner) row_stride (inner = tokens: rows row_stride apart;
+ *           otherwise e.g. a batch whose last positions are left out).
+ *   scale:  > 0, e.g. the reciprocal of a temperature.
+ *   out_stats: 4 floats for each token, 16-byte aligned, for moara_token_logps_backward.
+ * Sums are fp32 within a lane and 64 bits across them; log-probabilities near 0 keep their
+ * relative accuracy (the others' exponentials are summed apart from the label's).
+ * Errors: MOARA_E_ARG, MOARA_E_SHAPE (tokens or vocab out of range: at most 2^40 tokens and 2^30 words;
+ * overlapping rows), MOARA_E_HIP. */
+int moara_token_logps(const void* logits, int32_t logits_dtype, int64_t tokens, int64_t vocab, int64_t row_stride,
+                      int64_t inner, int64_t outer_stride, float scale, const int64_t* labels, float* out_logp,
+                      float* out_entropy, float* out_stats, void* stream);
+
+/* Gradient of the logits, of their type, from those of the log-probabilities and (or null) of
+ * the entropies, which then are `entropy`'s, as moara_token_logps gave them:
+ *   scale (g (1[j = label] - p_j) - h p_j (log p_j + entropy)).
+ * Rows without a label, and rows whose g and h are both 0, are 0 (and are not read). out_grad: rows
+ * grad_stride elements apart; it may be the logits themselves (inner = tokens, grad_stride =
+ * row_stride): every element is read before it is written. Errors as moara_token_logps. */
+int moara_token_logps_backward(const void* logits, int32_t logits_dtype, int64_t tokens, int64_t vocab, int64_t row_stride,
+                               int64_t inner, int64_t outer_stride, float scale, const int64_t* labels, const float* stats,
+                               const float* grad_logp, const float* entropy, const float* grad_entropy, void* out_grad,
+                               int64_t grad_stride, void* stream);
+
+/* Bytes of the workspace of moara_preference_loss and moara_policy_loss: device memory, 8-byte
+ * aligned, of any contents, for one call at a time. */
+#define MOARA_LOSS_WORKSPACE(tokens, sequences) (56 * ((sequences) + (tokens) / 1024 + 2))
+
+enum { MOARA_PREF_SIGMOID = 0, MOARA_PREF_HINGE = 1, MOARA_PREF_SQUARE = 2 };
+
+typedef struct {
+  double beta;            /* > 0 */
+  double margin;          /* of the sigmoid and the hinge */
+  double smoothing;       /* of the sigmoid: in [0, 1] */
+  int32_t kind;           /* MOARA_PREF_* */
+  int32_t average;        /* nonzero: a sequence counts with its tokens' mean, not their sum */
+} moara_preference_config;
+
+/* beta 0.1, sigmoid, no margin, no smoothing, sums. */
+int moara_preference_default_config(moara_preference_config* out);
+
+/* Loss of pairs of responses, sequence 2p the chosen one and 2p + 1 the rejected. With D the sum
+ * (or mean) over a sequence of logp - ref_logp (ref_logp null: of logp), h = D(2p) - D(2p + 1) and
+ * z = beta h - margin:
+ *   sigmoid  (1 - smoothing) log(1 + e^-z) + smoothing log(1 + e^z)
+ *   hinge    max(0, 1 - z)
+ *   square   (h - 1 / (2 beta))^2
+ * out: 3 floats, means over the pairs with a token: the loss, the share with h > 0, beta h. 0 where
+ *      there is no such pair.
+ * out_rewards, out_slope: a float for each sequence: beta D, and the loss's derivative by each
+ *      logp of the sequence.
+ * Sums are 64 bits. Errors: MOARA_E_ARG, MOARA_E_SHAPE (an odd number of sequences, tokens no
+ * multiple of them without offsets, over 2^33 tokens or 2^22 sequences), MOARA_E_HIP. */
+int moara_preference_loss(const moara_preference_config* cfg, const float* logp, const float* ref_logp, const uint8_t* mask,
+                          int64_t tokens, const int64_t* offsets, int64_t sequences, float* out, float* out_rewards,
+                          float* out_slope, void* workspace, void* stream);
+
+/* out_grad[t] = *grad_loss slope[sequence of t], 0 where t is left out. grad_loss: one float of
+ * device memory, the gradient of out[0]. Errors as moara_preference_loss. */
+int moara_preference_loss_backward(const float* slope, const float* grad_loss, const uint8_t* mask, int64_t tokens,
+                                   const int64_t* offsets, int64_t sequences, float* out_grad, void* stream);
+
+enum { MOARA_KL_EXP = 0, MOARA_KL_LINEAR = 1, MOARA_KL_SQUARE = 2 };
+enum { MOARA_MEAN_TOKENS = 0, MOARA_MEAN_SEQUENCES = 1 };
+
+typedef struct {
+  double clip_low, clip_high;   /* the ratio is clipped to [1 - clip_low, 1 + clip_high]; in [0, 1], >= 0 (or infinite) */
+  double kl_coef;               /* needs ref_logp where it is not 0 */
+  double entropy_coef;          /* needs entropy where it is not 0 */
+  double divisor;               /* > 0: the number of tokens (or sequences) that means are taken over; 0: of this call */
+  int32_t kl;                   /* MOARA_KL_* */
+  int32_t reduce;               /* MOARA_MEAN_TOKENS, or the mean over sequences of the means over their tokens */
+  int32_t sequence_advantages;  /* nonzero: advantages has a float for each sequence, else for each token */
+  int32_t reserved;
+} moara_policy_config;
+
+/* Clipping at 0.2 both ways, no KL term, no entropy term, means over tokens, their own advantages. */
+int moara_policy_default_config(moara_policy_config* out);
+
+/* Loss of a policy by the tokens of its answers. With d = logp - old_logp (old_logp null: 0, the
+ * policy is the one that sampled), r = e^d, A the advantage and q = ref_logp - logp, a token's terms are
+ *   gain = min(r A, clip(r, 1 - clip_low, 1 + clip_high) A),
+ *   kl   = e^q - q - 1 (EXP), -q (LINEAR) or q^2 / 2 (SQUARE),
+ * and with w its weight in the mean, the loss is sum w (-gain + kl_coef kl - entropy_coef entropy).
+ * Whether a token is clipped (r beyond the bound on the side that A pushes to) is decided in 64 bits.
+ * out: 6 floats: the loss, sum -w gain, sum w kl, sum w entropy, sum w [clipped], sum w (e^d - d - 1)
+ *      (the distance to the old policy). 0 where no token is left.
+ * out_weight: a float for each sequence: its tokens' w (0 where the sequence has none).
+ * advantages have no gradient, nor have old_logp and ref_logp. Sums are 64 bits.
+ * Errors: MOARA_E_ARG, MOARA_E_SHAPE (as moara_preference_loss), MOARA_E_HIP. */
+int moara_policy_loss(const moara_policy_config* cfg, const float* logp, const float* old_logp, const float* ref_logp,
+                      const float* entropy, const float* advantages, const uint8_t* mask, int64_t tokens,
+                      const int64_t* offsets, int64_t sequences, float* out, float* out_weight, void* workspace,
+                      void* stream);
+
+/* Gradients of logp and (or null) of the entropies: *grad_loss times the derivatives of out[0], 0
+ * where a token is left out. weight: as moara_policy_loss gave it. Errors as moara_policy_loss. */
+int moara_policy_loss_backward(const moara_policy_config* cfg, const float* logp, const float* old_logp, const float* ref_logp,
+                               const float* advantages, const uint8_t* mask, int64_t tokens, const int64_t* offsets,
+                               int64_t sequences, const float* weight, const float* grad_loss, float* out_grad_logp,
+                               float* out_grad_entropy, void* stream);
+
+typedef struct {
+  int32_t experts;        /* E, at most 1024 */
+  int32_t top_k;          /* columns of index, at most 64 */
+  int32_t score;          /* MOARA_SOFTMAX, or MOARA_SIGMOID (scores are divided by a token's sum) */
+  int32_t logits_dtype;   /* MOARA_F32 or MOARA_BF16 */
+  double balance_coef, z_coef;
+} moara_balance_config;
+
+/* 64 experts, 6 a token, softmax, fp32 logits, balance_coef 0.01, z_coef 0. */
+int moara_balance_default_config(moara_balance_config* out);
+
+/* Bytes of the workspace of moara_balance_loss: device memory, 8-byte aligned, of any contents, for
+ * one call at a time. */
+#define MOARA_BALANCE_WORKSPACE(experts, tokens, sequences) ((8 * (experts) + 64) * ((sequences) + (tokens) / 32 + 2))
+
+/* Load-balancing loss of routed tokens. For each sequence with tokens, c_e the number of its tokens that
+ * index gives to expert e, f_e = E c_e / sum_e c_e (0 where nothing is given), P_e the mean of its tokens'
+ * scores: balance = sum_e f_e P_e (1 where either is even). z: the mean over all tokens of the squared
+ * log-sum-exp of a token's logits (0 and not computed where z_coef is 0). The loss is balance_coef times the
+ * mean of the sequences' balance plus z_coef z. For a whole batch at once: offsets null, sequences 1.
+ *   logits, index, mask: as moara_route takes and gives them; indices outside [0, experts) are not
+ *           counted. A token without scores (moara_route gives it to no expert: NaN, a softmax row with
+ *           +infinity or nothing above -infinity; of sigmoid scores a row of -infinity) is left out.
+ *   load:   experts int64, or null: counts that take the place of every sequence's c in f, e.g. those of
+ *           all ranks or of several accumulated batches.
+ *   out:    3 floats: the loss, the mean balance, z.
+ *   out_counts: sequences x experts int64: c, of this call's tokens.
+ *   out_slope: sequences x experts + 2 floats for moara_balance_loss_backward.
+ * c has no gradient. Errors: MOARA_E_ARG, MOARA_E_SHAPE (as moara_preference_loss but for the odd number;
+ * overlapping rows), MOARA_E_UNSUPPORTED (over the limits above), MOARA_E_HIP. */
+int moara_balance_loss(const moara_balance_config* cfg, const void* logits, int64_t tokens, int64_t row_stride,
+                       const int32_t* index, const uint8_t* mask, const int64_t* offsets, int64_t sequences,
+                       const int64_t* load, float* out, int64_t* out_counts, float* out_slope, void* workspace, void* stream);
+
+/* Gradient of the logits (tokens x experts, contiguous, their type): *grad_loss times the derivative of
+ * out[0], 0 where a token is left out. Errors as moara_balance_loss. */
+int moara_balance_loss_backward(const moara_balance_config* cfg, const void* logits, int64_t tokens, int64_t row_stride,
+                                const uint8_t* mask, const int64_t* offsets, int64_t sequences, const float* slope,
+                                const float* grad_loss, void* out_grad, void* stream);
+
 /* Number of matrices in the state and one matrix's resolved layout. */
 int moara_matrix_info(const moara_state* st, int32_t mat, int64_t* rows, int64_t* cols,
                       int32_t* rank, int32_t* side, int32_t* n_blocks);

@@ -19,7 +19,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "libmoara.so")
 SOURCES = ["decompose.hip", "gemm.hip", "gemm_nt.hip", "decproj.hip", "refresh.hip", "chol.hip", "moara_api.hip",
-           "adamw.hip", "route.hip", "train_api.hip"]
+           "adamw.hip", "route.hip", "train_api.hip", "logps.hip", "loss.hip", "balance.hip", "loss_api.hip"]
 
 
 def hipcc() -> str:

@@ -77,3 +77,76 @@ constexpr int ROUTE_MAX_EXPERTS = 1024, ROUTE_MAX_K = 64, ROUTE_MAX_GROUPS = 64;
 hipError_t launch_route(const RouteParams& p, hipStream_t st);
 hipError_t launch_route_backward(const RouteParams& p, hipStream_t st);
 hipError_t launch_route_balance(int E, long long* counts, float* bias, float rate, hipStream_t st);
+
+// ---------------------------------------------------------------- log-probabilities of tokens
+struct LogpsParams {
+  const void* logits;
+  int64_t tokens, vocab, ld, inner, outer;      // row r at (r / inner) outer + (r % inner) ld
+  const int64_t* labels;
+  float* logp;                  // backward: its gradient
+  float* entropy;               // null: not wanted; backward: null, or the entropies
+  const float* grad_entropy;
+  float* stats;                 // of a token: largest logit, log2 of the sum, 1 - p of the label, its log-probability
+  void* grad;
+  int64_t grad_ld;
+  float scale, log2_scale;      // log2_scale: scale log2 e
+  int bf16;
+};
+hipError_t launch_logps(const LogpsParams& p, hipStream_t st);
+hipError_t launch_logps_backward(const LogpsParams& p, hipStream_t st);
+
+// ---------------------------------------------------------------- losses over packed sequences
+struct Packed {
+  const int64_t* offsets;       // null: sequences of `length` tokens each
+  const uint8_t* mask;
+  int64_t tokens, sequences, length;
+};
+// Sequences and tiles of CELL tokens cut the tokens into cells. Along the tokens either the sequence or the tile
+// advances, so sequence + tile numbers the cells: at most sequences + tiles - 1 of them.
+constexpr int LOSS_CELL = 1024;
+constexpr int64_t MAX_LOSS_TOKENS = (int64_t)1 << 33, MAX_SEQUENCES = (int64_t)1 << 22;
+struct PreferenceParams {
+  Packed q;
+  const float *logp, *ref;
+  double beta, margin, smoothing;
+  int kind, average;
+  float *out, *rewards, *slope;
+  double* sums;                 // workspace: sum and number of a cell's tokens
+};
+hipError_t launch_preference(const PreferenceParams& p, hipStream_t st);
+hipError_t launch_preference_backward(const Packed& q, const float* slope, const float* grad_loss, float* grad, hipStream_t st);
+struct PolicyParams {
+  Packed q;
+  const float *logp, *old, *ref, *entropy, *advantages;
+  double low, high;             // log(1 - clip_low), log(1 + clip_high): of d, beyond which a token is clipped
+  float at_low, at_high;        // the bounds themselves
+  double kl_coef, entropy_coef, divisor;
+  int kl, by_sequence, sequence_advantages;
+  float *out, *weight;
+  double* sums;                 // workspace: a cell's number of tokens and five sums
+  const float* grad_loss;
+  float *grad_logp, *grad_entropy;
+};
+constexpr int POLICY_SUMS = 6;
+hipError_t launch_policy(const PolicyParams& p, hipStream_t st);
+hipError_t launch_policy_backward(const PolicyParams& p, hipStream_t st);
+
+// ---------------------------------------------------------------- load balancing
+struct BalanceParams {
+  Packed q;
+  const void* logits;
+  int64_t ld;
+  const int32_t* index;
+  const int64_t* load;
+  int E, k, sigmoid, bf16, want_z;
+  double balance_coef, z_coef;
+  float* out;
+  long long* counts;
+  float* slope;
+  void* workspace;
+  const float* grad_loss;
+  void* grad;
+};
+constexpr int BALANCE_LEAST_TILE = 32;
+hipError_t launch_balance(const BalanceParams& p, hipStream_t st);
+hipError_t launch_balance_backward(const BalanceParams& p, hipStream_t st);

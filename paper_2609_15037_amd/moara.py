@@ -32,6 +32,9 @@ MOARA_KERN_DECOMPOSE, MOARA_KERN_PROJECT, MOARA_KERN_BACKPROJ, MOARA_KERN_REFRES
 MOARA_NUM_KERNELS = 5
 MOARA_SOFTMAX, MOARA_SIGMOID = 0, 1
 MOARA_GRAD_NORM_WORKSPACE = 16384
+MOARA_PREF_SIGMOID, MOARA_PREF_HINGE, MOARA_PREF_SQUARE = range(3)
+MOARA_KL_EXP, MOARA_KL_LINEAR, MOARA_KL_SQUARE = range(3)
+MOARA_MEAN_TOKENS, MOARA_MEAN_SEQUENCES = 0, 1
 
 EXPORTED = (
     "moara_default_config", "moara_allocate_ranks", "moara_resolve_matrix", "moara_state_bytes",
@@ -43,6 +46,10 @@ EXPORTED = (
     "moara_destroy_state", "moara_last_error", "moara_version",
     "moara_grad_norm", "moara_grad_scale", "moara_adamw_default_config", "moara_adamw_step",
     "moara_route_default_config", "moara_route", "moara_route_backward", "moara_route_balance",
+    "moara_token_logps", "moara_token_logps_backward",
+    "moara_preference_default_config", "moara_preference_loss", "moara_preference_loss_backward",
+    "moara_policy_default_config", "moara_policy_loss", "moara_policy_loss_backward",
+    "moara_balance_default_config", "moara_balance_loss", "moara_balance_loss_backward",
 )
 
 
@@ -99,6 +106,22 @@ class moara_route_config(ctypes.Structure):
                 ("renormalise", ctypes.c_int32), ("logits_dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
+class moara_preference_config(ctypes.Structure):
+    _fields_ = [("beta", ctypes.c_double), ("margin", ctypes.c_double), ("smoothing", ctypes.c_double),
+                ("kind", ctypes.c_int32), ("average", ctypes.c_int32)]
+
+
+class moara_policy_config(ctypes.Structure):
+    _fields_ = [("clip_low", ctypes.c_double), ("clip_high", ctypes.c_double), ("kl_coef", ctypes.c_double),
+                ("entropy_coef", ctypes.c_double), ("divisor", ctypes.c_double), ("kl", ctypes.c_int32),
+                ("reduce", ctypes.c_int32), ("sequence_advantages", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class moara_balance_config(ctypes.Structure):
+    _fields_ = [("experts", ctypes.c_int32), ("top_k", ctypes.c_int32), ("score", ctypes.c_int32),
+                ("logits_dtype", ctypes.c_int32), ("balance_coef", ctypes.c_double), ("z_coef", ctypes.c_double)]
+
+
 _lib = None
 
 
@@ -144,6 +167,19 @@ def lib():
         "moara_route": (ctypes.c_int, [P(moara_route_config), vp, i64, i64, vp, vp, vp, vp, vp, vp]),
         "moara_route_backward": (ctypes.c_int, [P(moara_route_config), vp, i64, i64, vp, vp, vp, vp]),
         "moara_route_balance": (ctypes.c_int, [i32, vp, vp, ctypes.c_float, vp]),
+        "moara_token_logps": (ctypes.c_int, [vp, i32, i64, i64, i64, i64, i64, ctypes.c_float, vp, vp, vp, vp, vp]),
+        "moara_token_logps_backward": (ctypes.c_int, [vp, i32, i64, i64, i64, i64, i64, ctypes.c_float, vp, vp, vp, vp, vp,
+                                                      vp, i64, vp]),
+        "moara_preference_default_config": (ctypes.c_int, [P(moara_preference_config)]),
+        "moara_preference_loss": (ctypes.c_int, [P(moara_preference_config), vp, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp]),
+        "moara_preference_loss_backward": (ctypes.c_int, [vp, vp, vp, i64, vp, i64, vp, vp]),
+        "moara_policy_default_config": (ctypes.c_int, [P(moara_policy_config)]),
+        "moara_policy_loss": (ctypes.c_int, [P(moara_policy_config), vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, vp]),
+        "moara_policy_loss_backward": (ctypes.c_int, [P(moara_policy_config), vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp,
+                                                      vp, vp]),
+        "moara_balance_default_config": (ctypes.c_int, [P(moara_balance_config)]),
+        "moara_balance_loss": (ctypes.c_int, [P(moara_balance_config), vp, i64, i64, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp]),
+        "moara_balance_loss_backward": (ctypes.c_int, [P(moara_balance_config), vp, i64, i64, vp, vp, i64, vp, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -734,3 +770,265 @@ def moara_route_balance(counts, bias, rate: float):
     n = counts.numel()
     c = _vector(counts, dev, torch.int64, n, "counts")
     _call(dev, lib().moara_route_balance, n, c, _vector(bias, dev, torch.float32, n, "bias"), float(rate))
+
+
+# ---------------------------------------------------------------- losses
+
+def _logits_rows(logits):
+    """(GPU, type, tokens, vocabulary, row stride, rows of a group, stride of the groups) of logits whose last axis is the
+    vocabulary, and which have one or two axes before it, a batch's or a view's of it."""
+    shape, strides = logits.shape, logits.stride()
+    if len(shape) not in (2, 3) or shape[-1] < 1 or (shape[-1] > 1 and strides[-1] != 1):
+        raise ValueError(f"logits: need (batch x) tokens x vocabulary with unit stride along the vocabulary, got {tuple(shape)}, "
+                         f"strides {strides}")
+    dev, dtype, vocab, rows = _on_gpu(logits, None, "logits"), _dtype_id(logits, "logits"), shape[-1], shape[-2]
+    ld = strides[-2] if rows > 1 else vocab
+    if len(shape) == 2 or shape[0] <= 1:
+        return dev, dtype, rows * (shape[0] if len(shape) == 3 else 1), vocab, ld, max(rows, 1), 0
+    if rows == 1:       # a batch of single tokens: rows a batch's stride apart
+        return dev, dtype, shape[0], vocab, strides[0], max(shape[0], 1), 0
+    return dev, dtype, shape[0] * rows, vocab, ld, max(rows, 1), strides[0]
+
+
+@_streamed
+def moara_token_logps(logits, labels, scale: float = 1.0, entropy: bool = False):
+    """moara_token_logps of the C ABI: (logp, entropy or None, stats). logits: tokens x vocabulary or batch x tokens x
+    vocabulary, float32 or bfloat16, rows any distance apart (e.g. `logits[:, :-1]`); labels: int64, one for each row,
+    contiguous. logp and entropy: float32 of the labels' shape; stats is for the backward call."""
+    import torch
+    dev, dtype, tokens, vocab, ld, inner, outer = _logits_rows(logits)
+    at = _vector(labels, dev, torch.int64, tokens, "labels")
+    logp = torch.empty_like(labels, dtype=torch.float32)
+    bits = torch.empty_like(logp) if entropy else None
+    stats = logp.new_empty((tokens, 4))
+    _call(dev, lib().moara_token_logps, logits.data_ptr(), dtype, tokens, vocab, ld, inner, outer, scale, at, logp.data_ptr(),
+          bits.data_ptr() if entropy else None, stats.data_ptr())
+    return logp, bits, stats
+
+
+@_streamed
+def moara_token_logps_backward(logits, labels, stats, grad_logp, scale: float = 1.0, entropy=None, grad_entropy=None, out=None):
+    """moara_token_logps_backward of the C ABI: the gradient of the logits, of their type and shape. stats and entropy as
+    moara_token_logps gave them; grad_logp and (or None) grad_entropy: float32, one for each row. out: a tensor for the
+    gradient, contiguous or the logits themselves where they have two axes; else a new one."""
+    import torch
+    dev, dtype, tokens, vocab, ld, inner, outer = _logits_rows(logits)
+    at = _vector(labels, dev, torch.int64, tokens, "labels")
+    s = _vector(stats, dev, torch.float32, 4 * tokens, "stats")
+    g = _vector(grad_logp, dev, torch.float32, tokens, "grad_logp")
+    h = e = None
+    if grad_entropy is not None:
+        if entropy is None:
+            raise ValueError("grad_entropy needs the entropies")
+        h, e = _vector(grad_entropy, dev, torch.float32, tokens, "grad_entropy"), _vector(entropy, dev, torch.float32, tokens, "entropy")
+    grad_ld = vocab
+    if out is None:
+        out = torch.empty_like(logits, memory_format=torch.contiguous_format)
+    elif out.dtype != logits.dtype or out.shape != logits.shape:
+        raise ValueError(f"out: need {tuple(logits.shape)} of {logits.dtype}, got {tuple(out.shape)} of {out.dtype}")
+    elif out.data_ptr() == logits.data_ptr() and out.stride() == logits.stride() and out.dim() == 2:
+        grad_ld = ld
+    elif not out.is_contiguous() or _overlap(out, logits):
+        raise ValueError("out: need a contiguous tensor apart from the logits, or the logits themselves (of two axes)")
+    _on_gpu(out, dev, "out")
+    _call(dev, lib().moara_token_logps_backward, logits.data_ptr(), dtype, tokens, vocab, ld, inner, outer, scale, at, s, g, e, h,
+          out.data_ptr(), grad_ld)
+    return out
+
+
+def _overlap(a, b) -> bool:
+    """Whether the memory from the first to the last element of a and of b has bytes in common."""
+    span = lambda t: (t.data_ptr(), t.data_ptr() + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))))
+    if not a.numel() or not b.numel():
+        return False
+    (a0, a1), (b0, b1) = span(a), span(b)
+    return a0 < b1 and b0 < a1
+
+
+def _packed(logp, offsets, mask):
+    """(GPU, tokens, mask's address, offsets' address, sequences) of packed tokens, checked: logp flat with offsets, or
+    sequences x length without."""
+    import torch
+    dev, tokens = _on_gpu(logp, None, "logp"), logp.numel()
+    at = _vector(logp, dev, torch.float32, tokens, "logp")
+    if mask is not None:
+        if mask.shape != logp.shape:
+            raise ValueError(f"mask: shape {tuple(mask.shape)}, logp has {tuple(logp.shape)}")
+        mask = _vector(mask, dev, torch.bool if mask.dtype == torch.bool else torch.uint8, tokens, "mask")
+    if offsets is None:
+        if logp.dim() != 2:
+            raise ValueError(f"logp: need sequences x length without offsets, got {tuple(logp.shape)}")
+        return dev, tokens, at, mask, None, logp.shape[0]
+    if logp.dim() != 1:
+        raise ValueError(f"logp: need one axis with offsets, got {tuple(logp.shape)}")
+    n = offsets.numel()
+    return dev, tokens, at, mask, _vector(offsets, dev, torch.int64, n, "offsets"), n - 1
+
+
+def _like(t, logp, dev, what: str):
+    """Address of a float32 tensor of logp's shape; None for None."""
+    import torch
+    if t is None:
+        return None
+    if t.shape != logp.shape:
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, logp has {tuple(logp.shape)}")
+    return _vector(t, dev, torch.float32, t.numel(), what)
+
+
+def _loss_workspace(logp, tokens: int, sequences: int):
+    import torch
+    return torch.empty(7 * (max(sequences, 0) + tokens // 1024 + 2), dtype=torch.float64, device=logp.device)
+
+
+def moara_preference_default_config(**overrides) -> moara_preference_config:
+    c = moara_preference_config()
+    _check(lib().moara_preference_default_config(ctypes.byref(c)))
+    for k, v in overrides.items():
+        setattr(c, k, v)
+    return c
+
+
+@_streamed
+def moara_preference_loss(cfg: moara_preference_config, logp, ref_logp=None, offsets=None, mask=None):
+    """moara_preference_loss of the C ABI: (out, rewards, slope), float32; out: loss, share of the pairs with the chosen
+    response ahead, mean of beta h; rewards: one for each sequence; slope is for the backward call. logp (and ref_logp):
+    float32, sequences x length, or flat with offsets (int64, sequences + 1); sequences 2p and 2p + 1 are a pair, the
+    chosen one first. mask: bool or uint8, of logp's shape."""
+    import torch
+    dev, tokens, at, m, o, n = _packed(logp, offsets, mask)
+    ref = _like(ref_logp, logp, dev, "ref_logp")
+    out = logp.new_empty(3)
+    rewards = logp.new_empty(max(n, 0))
+    slope = torch.empty_like(rewards)
+    workspace = _loss_workspace(logp, tokens, n)
+    _call(dev, lib().moara_preference_loss, cfg, at, ref, m, tokens, o, n, out.data_ptr(), rewards.data_ptr(), slope.data_ptr(),
+          workspace.data_ptr())
+    return out, rewards, slope
+
+
+@_streamed
+def moara_preference_loss_backward(cfg: moara_preference_config, logp, slope, grad_loss, offsets=None, mask=None):
+    """moara_preference_loss_backward of the C ABI: the gradient of logp. slope as moara_preference_loss gave it; grad_loss:
+    a float32 tensor of one element on the GPU; the others as they were."""
+    import torch
+    dev, tokens, _, m, o, n = _packed(logp, offsets, mask)
+    s, g = _vector(slope, dev, torch.float32, n, "slope"), _vector(grad_loss, dev, torch.float32, 1, "grad_loss")
+    grad = torch.empty_like(logp)
+    _call(dev, lib().moara_preference_loss_backward, s, g, m, tokens, o, n, grad.data_ptr())
+    return grad
+
+
+def moara_policy_default_config(**overrides) -> moara_policy_config:
+    c = moara_policy_config()
+    _check(lib().moara_policy_default_config(ctypes.byref(c)))
+    for k, v in overrides.items():
+        setattr(c, k, v)
+    return c
+
+
+def _advantages(cfg, advantages, logp, sequences: int, dev: int) -> int:
+    import torch
+    if cfg.sequence_advantages:
+        return _vector(advantages, dev, torch.float32, sequences, "advantages")
+    return _like(advantages, logp, dev, "advantages")
+
+
+@_streamed
+def moara_policy_loss(cfg: moara_policy_config, logp, advantages, old_logp=None, ref_logp=None, entropy=None, offsets=None,
+                      mask=None):
+    """moara_policy_loss of the C ABI: (out, weight), float32; out: loss, policy term, distance to the reference, entropy,
+    share of clipped tokens, distance to the old policy; weight is for the backward call. logp: float32, sequences x
+    length, or flat with offsets (int64, sequences + 1); old_logp, ref_logp, entropy, mask (bool or uint8) of its shape or
+    None; advantages of its shape, or one for each sequence where cfg.sequence_advantages."""
+    dev, tokens, at, m, o, n = _packed(logp, offsets, mask)
+    old, ref, bits = (_like(t, logp, dev, w) for t, w in ((old_logp, "old_logp"), (ref_logp, "ref_logp"), (entropy, "entropy")))
+    a = _advantages(cfg, advantages, logp, n, dev)
+    out = logp.new_empty(6)
+    weight = logp.new_empty(max(n, 0))
+    workspace = _loss_workspace(logp, tokens, n)
+    _call(dev, lib().moara_policy_loss, cfg, at, old, ref, bits, a, m, tokens, o, n, out.data_ptr(), weight.data_ptr(),
+          workspace.data_ptr())
+    return out, weight
+
+
+@_streamed
+def moara_policy_loss_backward(cfg: moara_policy_config, logp, advantages, weight, grad_loss, old_logp=None, ref_logp=None,
+                               entropy=None, offsets=None, mask=None):
+    """moara_policy_loss_backward of the C ABI: the gradients of logp and of the entropies (None without entropy). weight as
+    moara_policy_loss gave it; grad_loss: a float32 tensor of one element on the GPU; the others as they were."""
+    import torch
+    dev, tokens, at, m, o, n = _packed(logp, offsets, mask)
+    old, ref = _like(old_logp, logp, dev, "old_logp"), _like(ref_logp, logp, dev, "ref_logp")
+    a = _advantages(cfg, advantages, logp, n, dev)
+    w, g = _vector(weight, dev, torch.float32, n, "weight"), _vector(grad_loss, dev, torch.float32, 1, "grad_loss")
+    grad = torch.empty_like(logp)
+    bits = None if entropy is None else torch.empty_like(logp)
+    _call(dev, lib().moara_policy_loss_backward, cfg, at, old, ref, a, m, tokens, o, n, w, g, grad.data_ptr(),
+          None if bits is None else bits.data_ptr())
+    return grad, bits
+
+
+def moara_balance_default_config(**overrides) -> moara_balance_config:
+    c = moara_balance_config()
+    _check(lib().moara_balance_default_config(ctypes.byref(c)))
+    for k, v in overrides.items():
+        setattr(c, k, v)
+    return c
+
+
+def _balance_args(cfg, logits, offsets, sequences, mask):
+    """(configuration for the logits' type, GPU, tokens, row stride, mask's and offsets' address, sequences), checked."""
+    import torch
+    shape, strides = logits.shape, logits.stride()
+    if len(shape) != 2 or shape[1] != cfg.experts or (shape[1] > 1 and strides[1] != 1):
+        raise ValueError(f"logits: need tokens x {cfg.experts} with unit stride along the experts, got "
+                         f"{tuple(shape)}, strides {strides}")
+    dtype, tokens, dev = _dtype_id(logits, "logits"), shape[0], _on_gpu(logits, None, "logits")
+    if cfg.logits_dtype != dtype:       # threads may share a configuration: the caller's stays as it is
+        cfg = moara_balance_config.from_buffer_copy(cfg)
+        cfg.logits_dtype = dtype
+    if mask is not None:
+        mask = _vector(mask, dev, torch.bool if mask.dtype == torch.bool else torch.uint8, tokens, "mask")
+    if offsets is not None:
+        if sequences is not None:
+            raise ValueError("offsets or a number of equal sequences, not both")
+        n = offsets.numel()
+        offsets, sequences = _vector(offsets, dev, torch.int64, n, "offsets"), n - 1
+    return cfg, dev, tokens, (strides[0] if tokens > 1 else shape[1]), mask, offsets, 1 if sequences is None else int(sequences)
+
+
+@_streamed
+def moara_balance_loss(cfg: moara_balance_config, logits, index, offsets=None, mask=None, load=None,
+                       sequences: Optional[int] = None):
+    """moara_balance_loss of the C ABI: (out, counts, slope); out: loss, mean balance, z (float32); counts: int64, sequences
+    x experts; slope is for the backward call. logits: tokens x experts, float32 or bfloat16, rows any distance apart
+    (whatever cfg.logits_dtype says); index: as moara_route gives it; offsets: int64, of packed sequences, each balanced
+    for itself, or `sequences`, a number of equal ones (1: all tokens together); mask: bool or uint8, one for each token;
+    load: int64, one for each expert, for f in place of the counts."""
+    import torch
+    cfg, dev, tokens, ld, m, o, n = _balance_args(cfg, logits, offsets, sequences, mask)
+    i = _vector(index, dev, torch.int32, tokens * cfg.top_k, "index")
+    if load is not None:
+        load = _vector(load, dev, torch.int64, cfg.experts, "load")
+    E, s = cfg.experts, max(n, 0)
+    out = logits.new_empty(3, dtype=torch.float32)
+    counts = out.new_empty((s, E), dtype=torch.int64)
+    slope = out.new_empty(s * E + 2)
+    workspace = out.new_empty((E + 8) * (s + tokens // 32 + 2), dtype=torch.float64)
+    _call(dev, lib().moara_balance_loss, cfg, logits.data_ptr(), tokens, ld, i, m, o, n, load, out.data_ptr(), counts.data_ptr(),
+          slope.data_ptr(), workspace.data_ptr())
+    return out, counts, slope
+
+
+@_streamed
+def moara_balance_loss_backward(cfg: moara_balance_config, logits, slope, grad_loss, offsets=None, mask=None,
+                                sequences: Optional[int] = None):
+    """moara_balance_loss_backward of the C ABI: the gradient of the logits, contiguous, of their type. slope as
+    moara_balance_loss gave it; grad_loss: a float32 tensor of one element on the GPU; the others as they were."""
+    import torch
+    cfg, dev, tokens, ld, m, o, n = _balance_args(cfg, logits, offsets, sequences, mask)
+    s = _vector(slope, dev, torch.float32, max(n, 0) * cfg.experts + 2, "slope")
+    g = _vector(grad_loss, dev, torch.float32, 1, "grad_loss")
+    grad = torch.empty_like(logits, memory_format=torch.contiguous_format)
+    _call(dev, lib().moara_balance_loss_backward, cfg, logits.data_ptr(), tokens, ld, m, o, n, s, g, grad.data_ptr())
+    return grad
