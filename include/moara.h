@@ -504,8 +504,8 @@ int moara_route_balance(int32_t experts, int64_t* counts, float* bias, float rat
  *   out_stats: 4 floats for each token, 16-byte aligned, for moara_token_logps_backward.
  * Sums are fp32 within a lane and 64 bits across them; log-probabilities near 0 keep their
  * relative accuracy (the others' exponentials are summed apart from the label's).
- * Errors: MOARA_E_ARG, MOARA_E_SHAPE (tokens or vocab out of range: at most 2^40 tokens and 2^30 words;
- * overlapping rows), MOARA_E_HIP. */
+ * Errors: MOARA_E_ARG, MOARA_E_SHAPE (over 2^40 tokens, 2^30 words or a stride of 2^44; a stride below
+ * vocab), MOARA_E_HIP. */
 int moara_token_logps(const void* logits, int32_t logits_dtype, int64_t tokens, int64_t vocab, int64_t row_stride,
                       int64_t inner, int64_t outer_stride, float scale, const int64_t* labels, float* out_logp,
                       float* out_entropy, float* out_stats, void* stream);

@@ -14,6 +14,7 @@ namespace {
   } while (0)
 
 bool misaligned(const void* p, int size) { return ((uintptr_t)p & (uintptr_t)(size - 1)) != 0; }
+constexpr int64_t MAX_STRIDE = (int64_t)1 << 44;
 int size_of(int32_t dtype) { return dtype == MOARA_BF16 ? 2 : 4; }
 
 int check_packed(Packed& q, const uint8_t* mask, int64_t tokens, const int64_t* offsets, int64_t sequences) {
@@ -33,8 +34,8 @@ int check_logps(LogpsParams& p, const void* logits, int32_t dtype, int64_t token
     return moara_fail(MOARA_E_SHAPE, "%lld tokens, vocabulary of %lld", (long long)tokens, (long long)vocab);
   if (!(scale > 0) || !isfinite(scale)) return moara_fail(MOARA_E_ARG, "scale must be positive");
   if (tokens == 0) return MOARA_OK;
-  if (inner < 1 || (inner > 1 && tokens > 1 && row_stride < vocab) ||
-      (inner < tokens && outer_stride < (__int128)(inner - 1) * row_stride + vocab))
+  if (inner < 1 || (inner > 1 && tokens > 1 && row_stride < vocab) || (inner < tokens && outer_stride < vocab) ||
+      row_stride > MAX_STRIDE || outer_stride > MAX_STRIDE)
     return moara_fail(MOARA_E_SHAPE, "rows overlap: strides %lld, %lld of %lld rows", (long long)row_stride,
                       (long long)outer_stride, (long long)inner);
   if (!logits || !labels || misaligned(logits, size_of(dtype)) || misaligned(labels, 8))
@@ -68,7 +69,7 @@ int check_policy(const moara_policy_config* c, PolicyParams& p, const float* log
     return moara_fail(MOARA_E_ARG, "a coefficient or the divisor is not finite, or the divisor is negative");
   if (c->kl < MOARA_KL_EXP || c->kl > MOARA_KL_SQUARE) return moara_fail(MOARA_E_ARG, "bad kl");
   if (c->reduce != MOARA_MEAN_TOKENS && c->reduce != MOARA_MEAN_SEQUENCES) return moara_fail(MOARA_E_ARG, "bad reduce");
-  if (c->kl_coef != 0 && !ref_logp) return moara_fail(MOARA_E_ARG, "a KL term needs ref_logp");
+  if (tokens > 0 && c->kl_coef != 0 && !ref_logp) return moara_fail(MOARA_E_ARG, "a KL term needs ref_logp");
   p = PolicyParams{};
   const int rc = check_packed(p.q, mask, tokens, offsets, sequences);
   if (rc != MOARA_OK) return rc;
@@ -148,7 +149,7 @@ int moara_token_logps_backward(const void* logits, int32_t logits_dtype, int64_t
   if (rc != MOARA_OK || tokens == 0) return rc;
   if (!stats || !grad_logp || !out_grad) return moara_fail(MOARA_E_ARG, "null statistics, gradient or output");
   if (grad_entropy && !entropy) return moara_fail(MOARA_E_ARG, "the entropies' gradient needs the entropies");
-  if (grad_stride < vocab && tokens > 1) return moara_fail(MOARA_E_SHAPE, "rows overlap: stride %lld", (long long)grad_stride);
+  if ((grad_stride < vocab && tokens > 1) || grad_stride > MAX_STRIDE) return moara_fail(MOARA_E_SHAPE, "rows overlap: stride %lld", (long long)grad_stride);
   if (misaligned(stats, 16) || misaligned(grad_logp, 4) || misaligned(entropy, 4) || misaligned(grad_entropy, 4) ||
       misaligned(out_grad, size_of(logits_dtype)))
     return moara_fail(MOARA_E_ARG, "pointer not aligned");
@@ -227,7 +228,7 @@ int moara_policy_loss(const moara_policy_config* cfg, const float* logp, const f
   PolicyParams p;
   const int rc = check_policy(cfg, p, logp, old_logp, ref_logp, advantages, mask, tokens, offsets, sequences);
   if (rc != MOARA_OK) return rc;
-  if (cfg->entropy_coef != 0 && !entropy) return moara_fail(MOARA_E_ARG, "an entropy term needs entropy");
+  if (tokens > 0 && cfg->entropy_coef != 0 && !entropy) return moara_fail(MOARA_E_ARG, "an entropy term needs entropy");
   if (!out || !out_weight || !workspace) return moara_fail(MOARA_E_ARG, "null output or workspace");
   if (misaligned(entropy, 4) || misaligned(out, 4) || misaligned(out_weight, 4) || misaligned(workspace, 8))
     return moara_fail(MOARA_E_ARG, "pointer not aligned");

@@ -778,7 +778,7 @@ def _logits_rows(logits):
     """(GPU, type, tokens, vocabulary, row stride, rows of a group, stride of the groups) of logits whose last axis is the
     vocabulary, and which have one or two axes before it, a batch's or a view's of it."""
     shape, strides = logits.shape, logits.stride()
-    if len(shape) not in (2, 3) or shape[-1] < 1 or (shape[-1] > 1 and strides[-1] != 1):
+    if len(shape) not in (2, 3) or shape[-1] < 1 or (shape[-1] > 1 and strides[-1] != 1 and logits.numel()):
         raise ValueError(f"logits: need (batch x) tokens x vocabulary with unit stride along the vocabulary, got {tuple(shape)}, "
                          f"strides {strides}")
     dev, dtype, vocab, rows = _on_gpu(logits, None, "logits"), _dtype_id(logits, "logits"), shape[-1], shape[-2]
@@ -980,7 +980,7 @@ def _balance_args(cfg, logits, offsets, sequences, mask):
     """(configuration for the logits' type, GPU, tokens, row stride, mask's and offsets' address, sequences), checked."""
     import torch
     shape, strides = logits.shape, logits.stride()
-    if len(shape) != 2 or shape[1] != cfg.experts or (shape[1] > 1 and strides[1] != 1):
+    if len(shape) != 2 or shape[1] != cfg.experts or (shape[1] > 1 and strides[1] != 1 and logits.numel()):
         raise ValueError(f"logits: need tokens x {cfg.experts} with unit stride along the experts, got "
                          f"{tuple(shape)}, strides {strides}")
     dtype, tokens, dev = _dtype_id(logits, "logits"), shape[0], _on_gpu(logits, None, "logits")

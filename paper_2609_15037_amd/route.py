@@ -8,7 +8,9 @@ balancing bias's step).
     router.balance(1e-3)                    # moves the bias, starts the counts again
 
 An expert without tokens has no gradient: the MoARa optimizer skips its matrices. Data-parallel ranks add up
-`router.counts` (int64) before balance().
+`router.counts` (int64) before balance(). Instead of the bias, or beside it, a loss can keep the load even:
+
+    index, weight, loss = router(x, balance=router.balance_config(balance_coef=1e-2, z_coef=1e-3))
 """
 from __future__ import annotations
 
@@ -17,6 +19,7 @@ from typing import Optional, Tuple
 import numpy as np
 import torch
 
+from . import losses
 from . import moara as M
 
 
@@ -90,15 +93,26 @@ class ExpertRouter(torch.nn.Module):
         else:
             self.counts.copy_(saved)
 
-    def forward(self, x: torch.Tensor, mask: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    def balance_config(self, **config) -> M.moara_balance_config:
+        """The balance loss's configuration for this router: keyword arguments are balance_coef and z_coef."""
+        return M.moara_balance_default_config(experts=self.cfg.experts, top_k=self.cfg.top_k, score=self.cfg.score, **config)
+
+    def forward(self, x: torch.Tensor, mask: Optional[torch.Tensor] = None,
+                balance: Optional[M.moara_balance_config] = None, offsets: Optional[torch.Tensor] = None,
+                load: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, ...]:
         """x: tokens x d_model; mask: tokens, False where a token is not routed. An index is -1 (weight 0)
-        where there is no expert."""
+        where there is no expert. With `balance` (as balance_config gives it) a third value: the balance loss of these
+        tokens, together or within each of the packed sequences of `offsets`; load: counts that it takes in place of
+        these tokens' own, e.g. `counts` of several accumulated batches."""
         with torch.autocast(x.device.type, enabled=False):      # the choice is sensitive to the logits' rounding
             logits = torch.nn.functional.linear(x.float(), self.weight.float())
         if self.counts.device != x.device:      # where buffers are moved one by one
             self.counts = self.counts.to(x.device)
         again = torch._C._current_graph_task_id() != -1         # inside a backward pass
-        return route(logits, self.cfg, self.bias, mask, self.counts if self.training and not again else None)
+        out = route(logits, self.cfg, self.bias, mask, self.counts if self.training and not again else None)
+        if balance is None:
+            return out
+        return *out, losses.balance_loss(balance, logits, out[0], offsets=offsets, mask=mask, load=load)[0]
 
     def load(self) -> np.ndarray:
         """Tokens of each expert in training since the last balance() (waits for the GPU)."""
