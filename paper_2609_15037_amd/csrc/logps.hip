@@ -3,6 +3,9 @@
 // writes the gradient. Both are bound by memory.
 #include <float.h>
 
+#include <type_traits>
+
+#include "lanes.h"
 #include "train.h"
 
 namespace {
@@ -11,48 +14,50 @@ constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.693147180559945309417f;
 // Exponents of 2 below this have no weight in any sum; a bound keeps -inf out of products with 0.
 constexpr float LEAST = -200.f;
 
-typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint16_t u16x8u __attribute__((ext_vector_type(8), aligned(2)));
-// Sixteen bytes a lane: 4 fp32 or 8 bf16, of any alignment; `left` of them exist, the others are -inf and not written.
-__device__ __forceinline__ void load(const float* q, int left, float (&x)[4]) {
-  if (left >= 4) {
-    const f32x4u a = *reinterpret_cast<const f32x4u*>(q);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = a[j];
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = j < left ? q[j] : -__builtin_inff();
-  }
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x4h __attribute__((ext_vector_type(4), aligned(2)));
+// Sixteen bytes a lane, 4 fp32 or 8 bf16, of any alignment; ONCE: past the caches. A vector is loaded as it is and taken
+// apart later: taken apart where it may not exist, each load would be waited for before the next.
+template <bool ONCE, typename V> __device__ __forceinline__ u32x4 get(const V* q) {
+  return ONCE ? __builtin_nontemporal_load(q) : *q;
 }
-__device__ __forceinline__ void load(const bf16* q, int left, float (&x)[8]) {
-  if (left >= 8) {
-    const u16x8u a = *reinterpret_cast<const u16x8u*>(q);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = __uint_as_float((uint32_t)a[j] << 16);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = j < left ? bf2f(q[j]) : -__builtin_inff();
-  }
+template <bool ONCE, typename V> __device__ __forceinline__ void put(V* q, const V& x) {
+  if (ONCE) __builtin_nontemporal_store(x, q); else *q = x;
 }
-__device__ __forceinline__ void store(float* q, int left, const float (&x)[4]) {
-  if (left >= 4) {
-    *reinterpret_cast<f32x4u*>(q) = f32x4u{x[0], x[1], x[2], x[3]};
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) if (j < left) q[j] = x[j];
-  }
+template <bool ONCE> __device__ __forceinline__ u32x4 load(const float* q) {
+  return get<ONCE>(reinterpret_cast<const u32x4u*>(q));
 }
-__device__ __forceinline__ void store(bf16* q, int left, const float (&x)[8]) {
-  if (left >= 8) {
-    u16x8u a;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) a[j] = __builtin_bit_cast(uint16_t, f2bf(x[j]));
-    *reinterpret_cast<u16x8u*>(q) = a;
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) if (j < left) q[j] = f2bf(x[j]);
-  }
+template <bool ONCE> __device__ __forceinline__ u32x4 load(const bf16* q) {
+  return get<ONCE>(reinterpret_cast<const u32x4h*>(q));
 }
+template <typename T> __device__ __forceinline__ u32x4 nothing() {      // -inf
+  const uint32_t x = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+  return u32x4{x, x, x, x};
+}
+__device__ __forceinline__ void apart(const u32x4& a, float (&x)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = __uint_as_float(a[j]);
+}
+__device__ __forceinline__ void apart(const u32x4& a, float (&x)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(j & 1 ? a[j / 2] & 0xFFFF0000u : a[j / 2] << 16);
+}
+template <bool ONCE> __device__ __forceinline__ void store(float* q, const float (&x)[4]) {
+  u32x4u a;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) a[j] = __float_as_uint(x[j]);
+  put<ONCE>(reinterpret_cast<u32x4u*>(q), a);
+}
+template <bool ONCE> __device__ __forceinline__ void store(bf16* q, const float (&x)[8]) {
+  u32x4h a;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    a[j] = (uint32_t)__builtin_bit_cast(uint16_t, f2bf(x[2 * j + 1])) << 16 | __builtin_bit_cast(uint16_t, f2bf(x[2 * j]));
+  put<ONCE>(reinterpret_cast<u32x4h*>(q), a);
+}
+__device__ __forceinline__ void store1(float* q, float x) { *q = x; }
+__device__ __forceinline__ void store1(bf16* q, float x) { *q = f2bf(x); }
 __device__ __forceinline__ float value(const float* q) { return *q; }
 __device__ __forceinline__ float value(const bf16* q) { return bf2f(*q); }
 
@@ -66,23 +71,26 @@ struct Part {
   float top;
   double sum, bits;
 };
-__device__ __forceinline__ Part joined(const Part& a, const Part& b, float k, bool entropy) {
-  const float top = fmaxf(a.top, b.top);
-  const float da = fmaxf((a.top - top) * k, LEAST), db = fmaxf((b.top - top) * k, LEAST);
-  const double fa = exp2f(da), fb = exp2f(db);
-  Part r = {top, a.sum * fa + b.sum * fb, 0};
-  if (entropy) r.bits = fa * (a.bits + da * a.sum) + fb * (b.bits + db * b.sum);
+// The parts that LANES neighbouring lanes hold, put together in each of them.
+template <int LANES, bool ENTROPY> __device__ __forceinline__ Part together(const Part& a, float k) {
+  Part r = {max_of<LANES>(a.top), 0, 0};
+  const float d = fmaxf((a.top - r.top) * k, LEAST);
+  const double f = __builtin_amdgcn_exp2f(d);
+  r.sum = sum_of<LANES>(f * a.sum);
+  if (ENTROPY) r.bits = sum_of<LANES>(f * fma((double)d, a.sum, a.bits));
   return r;
 }
 
 // THREADS threads take a row. The label is left out of the sum, which is then small where the label has nearly all of
 // the probability: log p = a - log1p(sum + (e_label - 1)) with a = scale (x_label - top) keeps its relative accuracy.
-template <typename T, int THREADS, bool ENTROPY>
+template <typename T, int THREADS, int U, bool ENTROPY, bool ONCE>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void k_logps(LogpsParams p) {
-  constexpr int N = 16 / sizeof(T), U = 4, BLOCK = THREADS < 256 ? 256 : THREADS, ROWS = BLOCK / THREADS;
-  __shared__ Part parts[THREADS / 64];
+  constexpr int N = 16 / sizeof(T), BLOCK = THREADS < 256 ? 256 : THREADS, ROWS = BLOCK / THREADS;
+  constexpr int WAVES = THREADS < 64 ? 1 : THREADS / 64, LANES = THREADS < 64 ? THREADS : 64;
+  __shared__ Part parts[2][WAVES];
   const int lane = threadIdx.x % THREADS;
   const float k = p.log2_scale;
+  int turn = 0;
   for (int64_t r = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS; r < p.tokens; r += (int64_t)gridDim.x * ROWS) {
     const int64_t label = p.labels[r];
     if (label < 0 || label >= p.vocab) {
@@ -97,136 +105,198 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void k_logps(LogpsPa
     const int V = (int)p.vocab, own = (int)label;
     const float xl = value(row + own);
     float top = -FLT_MAX, sum = 0, bits = 0;
-    for (int base = N * lane; base < V; base += N * THREADS * U) {
-      float x[U][N];
+    // U vectors a lane; in the last ones (whole: false) those that there are, and of the row's last V % N elements one a lane
+    auto take = [&](int base, auto whole) {
+      constexpr bool WHOLE = decltype(whole)::value;
+      u32x4 raw[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int e = base + u * N * THREADS;
-        load(row + e, V - e, x[u]);
+        if (!WHOLE) raw[u] = nothing<T>();
+        if (WHOLE || e + N <= V) raw[u] = load<ONCE>(row + e);
       }
-      float most = top;
+      const int rag = (V & -N) + lane;
+      const float more = !WHOLE && rag < V && rag != own ? value(row + rag) : -__builtin_inff();
+      float x[U][N];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int at = own - (base + u * N * THREADS);
-        if ((unsigned)at < (unsigned)N)
+      for (int u = 0; u < U; ++u) apart(raw[u], x[u]);
+      const unsigned at = own - base;
+      if (at < N * THREADS * U && at % (N * THREADS) < N)
 #pragma unroll
-          for (int j = 0; j < N; ++j) x[u][j] = j == at ? -__builtin_inff() : x[u][j];
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int j = 0; j < N; ++j) most = fmaxf(most, x[u][j]);
-      }
-      const float d = fmaxf((top - most) * k, LEAST), f = exp2f(d);
-      if (ENTROPY) bits = f * (bits + d * sum);
-      sum *= f;
-      top = most;
+          for (int j = 0; j < N; ++j) x[u][j] = at == u * N * THREADS + j ? -__builtin_inff() : x[u][j];
+      float most = WHOLE ? top : fmaxf(top, more);
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-          const float t = (x[u][j] - top) * k, e = __builtin_amdgcn_exp2f(t);
-          sum += e;
-          if (ENTROPY) bits = fmaf(e, fmaxf(t, LEAST), bits);
-        }
-    }
-    Part a = {top, sum, bits};
-    for (int o = 32; o > 0; o >>= 1)
-      a = joined(a, Part{__shfl_xor(a.top, o, 64), __shfl_xor(a.sum, o, 64), __shfl_xor(a.bits, o, 64)}, k, ENTROPY);
-    if (THREADS > 64) {
-      __syncthreads();          // the last row's have been read
-      if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = a;
+        for (int j = 0; j < N; ++j) most = fmaxf(most, x[u][j]);
+      const float d = fmaxf((top - most) * k, LEAST), f = __builtin_amdgcn_exp2f(d);
+      if (ENTROPY) bits = f * fmaf(d, sum, bits);
+      sum *= f;
+      top = most;
+      auto add = [&](float y) {
+        const float t = (y - top) * k, e = __builtin_amdgcn_exp2f(t);
+        sum += e;
+        if (ENTROPY) bits = fmaf(e, fmaxf(t, LEAST), bits);
+      };
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int j = 0; j < N; ++j) add(x[u][j]);
+      if (!WHOLE) add(more);
+    };
+    int at = 0;
+    for (; at + N * THREADS * U <= V; at += N * THREADS * U) take(at + N * lane, std::true_type{});
+    if (at < V) take(at + N * lane, std::false_type{});
+    Part a = together<LANES, ENTROPY>(Part{top, sum, bits}, k);
+    if (WAVES > 1) {
+      // one barrier a row: the next row's parts go to the other half, and the first wave has read this one's when it
+      // comes to the next barrier
+      if ((threadIdx.x & 63) == 0) parts[turn][threadIdx.x >> 6] = a;
       __syncthreads();
-      a = parts[0];
-      for (int i = 1; i < THREADS / 64; ++i) a = joined(a, parts[i], k, ENTROPY);
+      const int wave = threadIdx.x >> 6, i = threadIdx.x & 15;
+      a = i < WAVES ? parts[turn][i] : Part{-FLT_MAX, 0, 0};
+      turn ^= 1;
+      if (wave) continue;
+      a = together<16, ENTROPY>(a, k);
     }
     if (lane == 0) {
-      const float last = fmaxf(a.top, xl);
-      a = joined(a, Part{last, 0, 0}, k, ENTROPY);
-      const float el = exp2f((xl - last) * k);
-      const double total = a.sum + (double)el;
-      const float log = log1pf((float)(a.sum + ((double)el - 1)));
+      const float last = fmaxf(a.top, xl), d = fmaxf((a.top - last) * k, LEAST);
+      const double f = __builtin_amdgcn_exp2f(d), el = __builtin_amdgcn_exp2f((xl - last) * k);
+      if (ENTROPY) a.bits = f * fma((double)d, a.sum, a.bits);
+      a.sum *= f;
+      const double total = a.sum + el;
+      const float log = log1pf((float)(a.sum + (el - 1)));
       const float logp = (xl - last) * p.scale - log;
       p.logp[r] = logp;
       if (ENTROPY)
-        p.entropy[r] = (float)((a.sum * log - (double)LN2 * a.bits) / total - (el > 0 ? (double)el / total * logp : 0));
+        p.entropy[r] = (float)((a.sum * log - (double)LN2 * a.bits) / total - (el > 0 ? el / total * logp : 0));
       reinterpret_cast<float4*>(p.stats)[r] = float4{last, log * LOG2E, (float)(a.sum / total), logp};
     }
   }
 }
 
-// 2^((x - top) k - log2 sum) is p; a workgroup takes U vectors a lane of a row. The label's own value has 1 - p and
+// 2^((x - top) k - log2 sum) is p; GROUP threads take U vectors a lane of a row. The label's own value has 1 - p and
 // log p from the forward pass.
-template <typename T, bool ENTROPY> __global__ __launch_bounds__(256) void k_logps_backward(LogpsParams p, int parts) {
-  constexpr int N = 16 / sizeof(T), U = 4, SPAN = 256 * N * U;
+template <typename T, int GROUP, bool ENTROPY, bool ONCE_IN, bool ONCE_OUT>
+__global__ __launch_bounds__(256) void k_logps_backward(LogpsParams p, uint32_t parts) {
+  constexpr int N = 16 / sizeof(T), U = 4, SPAN = GROUP * N * U, GROUPS = 256 / GROUP;
+  const int lane = threadIdx.x % GROUP;
   const int64_t units = p.tokens * parts;
-  for (int64_t i = blockIdx.x; i < units; i += gridDim.x) {
-    const int64_t r = i / parts;
-    const int base = (int)(i - r * parts) * SPAN + N * threadIdx.x, V = (int)p.vocab;
+  for (int64_t i = (int64_t)blockIdx.x * GROUPS + threadIdx.x / GROUP; i < units; i += (int64_t)gridDim.x * GROUPS) {
+    const int64_t r = parts == 1 ? i : i <= 0xFFFFFFFF ? (uint32_t)i / parts : i / parts;
+    const int at = (int)(i - r * parts) * SPAN, base = at + N * lane, V = (int)p.vocab;
+    const bool whole = at + SPAN <= V;
+    const int rag = (V & -N) + lane;             // of the row's last V % N elements one a lane
     T* out = (T*)p.grad + r * p.grad_ld;
     const int64_t label = p.labels[r];
     const float g = p.logp[r], h = ENTROPY ? p.grad_entropy[r] : 0.f;
     if (label < 0 || label >= p.vocab || (g == 0 && h == 0)) {
-      float zero[N] = {};
+      const float zero[N] = {};
 #pragma unroll
-      for (int u = 0; u < U; ++u) store(out + base + u * N * 256, V - (base + u * N * 256), zero);
+      for (int u = 0; u < U; ++u)
+        if (whole || base + u * N * GROUP + N <= V) store<ONCE_OUT>(out + base + u * N * GROUP, zero);
+      if (!whole && rag < V) store1(out + rag, 0.f);
       continue;
     }
     const T* row = row_of<T>(p, r);
+    u32x4 raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int e = base + u * N * GROUP;
+      raw[u] = nothing<T>();
+      if (whole || e + N <= V) raw[u] = load<ONCE_IN>(row + e);
+    }
+    const float more = !whole && rag < V ? value(row + rag) : 0.f;
     const float4 s = reinterpret_cast<const float4*>(p.stats)[r];
     const float H = ENTROPY ? p.entropy[r] : 0.f, k = p.log2_scale;
     const float c0 = -p.scale * fmaf(h, H, g), c1 = -p.scale * h * LN2;
-    float x[U][N];
+    auto slope = [&](float x) {
+      const float t = fmaf(x - s.x, k, -s.y), q = __builtin_amdgcn_exp2f(t);
+      return ENTROPY ? q * fmaf(c1, fmaxf(t, LEAST), c0) : q * c0;
+    };
+    // scale (g (1 - p) - h p (log p + H)); p log p is 0 where p is
+    auto own = [&] {
+      const float q = exp2f(s.w * LOG2E), b = ENTROPY && q > 0 ? h * q * (s.w + H) : 0.f;
+      return p.scale * (g * s.z - b);
+    };
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int e = base + u * N * 256;
-      load(row + e, V - e, x[u]);
-    }
+      const int e = base + u * N * GROUP;
+      float x[N];
+      apart(raw[u], x);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int e = base + u * N * 256, at = (int)label - e;
+      for (int j = 0; j < N; ++j) x[j] = slope(x[j]);
+      const unsigned hit = (int)label - e;
+      if (hit < N) {
+        const float y = own();
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float t = fmaf(x[u][j] - s.x, k, -s.y), q = __builtin_amdgcn_exp2f(t);
-        x[u][j] = ENTROPY ? q * fmaf(c1, fmaxf(t, LEAST), c0) : q * c0;
+        for (int j = 0; j < N; ++j) x[j] = hit == j ? y : x[j];
       }
-      if ((unsigned)at < (unsigned)N) {
-        // scale (g (1 - p) - h p (log p + H)); p log p is 0 where p is
-        const float q = exp2f(s.w * LOG2E), b = ENTROPY && q > 0 ? h * q * (s.w + H) : 0.f;
-        const float y = p.scale * (g * s.z - b);
-#pragma unroll
-        for (int j = 0; j < N; ++j) x[u][j] = j == at ? y : x[u][j];
-      }
-      store(out + e, V - e, x[u]);
+      if (whole || e + N <= V) store<ONCE_OUT>(out + e, x);
     }
+    if (!whole && rag < V) store1(out + rag, rag == label ? own() : slope(more));
   }
 }
 
+// Logits that do not fit the memory-side cache go past the caches: forward 8192 x 32000 bf16 84 us instead of 96, 4096 x
+// 131072 fp32 312 and 340 (8192 x 16384 bf16, 268 MB, 45 and 43); backward 8192 x 32000 bf16 173 and 208, 4096 x 131072 340 and
+// 369; where the logits alone would fit, gradients only: 16384 x 4096 fp32 80 and 94, with the logits past them too 86.
+constexpr double CACHE = 256 << 20;
+template <typename T> double bytes_of(const LogpsParams& p) { return (double)p.tokens * (double)p.vocab * sizeof(T); }
 constexpr int64_t MOST_GROUPS = 1 << 22;        // workgroups of a launch: fewer than 2^32 threads
 
-template <typename T, int THREADS> void forward(const LogpsParams& p, hipStream_t st) {
+template <typename T, int THREADS, int U, bool ONCE> void forward(const LogpsParams& p, hipStream_t st) {
   constexpr int block = THREADS < 256 ? 256 : THREADS, rows = block / THREADS;
   const int64_t n = (p.tokens + rows - 1) / rows;
   const dim3 g((uint32_t)(n < MOST_GROUPS ? n : MOST_GROUPS)), b(block);
-  if (p.entropy) hipLaunchKernelGGL((k_logps<T, THREADS, true>), g, b, 0, st, p);
-  else hipLaunchKernelGGL((k_logps<T, THREADS, false>), g, b, 0, st, p);
+  if (p.entropy) hipLaunchKernelGGL((k_logps<T, THREADS, U, true, ONCE>), g, b, 0, st, p);
+  else hipLaunchKernelGGL((k_logps<T, THREADS, U, false, ONCE>), g, b, 0, st, p);
 }
-template <typename T> void backward(const LogpsParams& p, hipStream_t st) {
-  constexpr int span = 256 * 4 * (16 / sizeof(T));
-  const int parts = (int)((p.vocab + span - 1) / span);
-  const int64_t n = p.tokens * parts;
+template <typename T, int THREADS, int U> void forward(const LogpsParams& p, hipStream_t st) {
+  if (bytes_of<T>(p) > CACHE) forward<T, THREADS, U, true>(p, st); else forward<T, THREADS, U, false>(p, st);
+}
+template <typename T, int GROUP, bool ONCE_IN, bool ONCE_OUT> void backward(const LogpsParams& p, hipStream_t st) {
+  constexpr int span = GROUP * 4 * (16 / sizeof(T)), groups = 256 / GROUP;
+  const uint32_t parts = (uint32_t)((p.vocab + span - 1) / span);
+  const int64_t n = (p.tokens * parts + groups - 1) / groups;
   const dim3 g((uint32_t)(n < MOST_GROUPS ? n : MOST_GROUPS)), b(256);
-  if (p.grad_entropy) hipLaunchKernelGGL((k_logps_backward<T, true>), g, b, 0, st, p, parts);
-  else hipLaunchKernelGGL((k_logps_backward<T, false>), g, b, 0, st, p, parts);
+  if (p.grad_entropy) hipLaunchKernelGGL((k_logps_backward<T, GROUP, true, ONCE_IN, ONCE_OUT>), g, b, 0, st, p, parts);
+  else hipLaunchKernelGGL((k_logps_backward<T, GROUP, false, ONCE_IN, ONCE_OUT>), g, b, 0, st, p, parts);
+}
+template <typename T, int GROUP> void backward(const LogpsParams& p, hipStream_t st) {
+  const double bytes = bytes_of<T>(p);
+  if (bytes > CACHE) backward<T, GROUP, true, true>(p, st);
+  else if (2 * bytes > CACHE) backward<T, GROUP, false, true>(p, st);
+  else backward<T, GROUP, false, false>(p, st);
 }
 
 }  // namespace
 
+// Threads of a row. Many rows, bf16 (fp32), us, from the caches: 65536 x 512 (x 256) 15 (13) on 16 lanes, 44 (33) on a wave;
+// 32768 x 2048 28 on a wave, 87 on 256 threads; 8192 x 8192 26 and 27 (16384 x 4096 43 and 41); 8192 x 32000 95 (174) on 256,
+// 128 (169) on 1024; 4096 x 131072 190 (351) and 174 (339). Few rows: 64 x 131072 11.4 and 9.0, 256 x 32000 5.6 and 5.0, 512 x
+// 32000 7.8 and 8.9.
 hipError_t launch_logps(const LogpsParams& p, hipStream_t st) {
-  const bool small = p.vocab <= 2048;
-  if (p.bf16) small ? forward<bf16, 64>(p, st) : forward<bf16, 256>(p, st);
-  else small ? forward<float, 64>(p, st) : forward<float, 256>(p, st);
+  const int64_t vectors = (p.vocab + (p.bf16 ? 7 : 3)) / (p.bf16 ? 8 : 4);
+#define LOGPS(THREADS, U) p.bf16 ? forward<bf16, THREADS, U>(p, st) : forward<float, THREADS, U>(p, st)
+  if (vectors <= 128) LOGPS(16, 2);
+  else if (vectors <= 512) LOGPS(64, 4);
+  else if (vectors <= 8192 && (vectors < 2048 || p.tokens > 256)) LOGPS(256, 4);
+  else LOGPS(1024, 4);
+#undef LOGPS
   return hipGetLastError();
 }
 
+// Threads of a row's part, by the same cases: 65536 x 512 bf16 22 us on 16 lanes, 35 on a wave, 114 on 256 threads; 32768 x 2048
+// 44, 44 and 67.
 hipError_t launch_logps_backward(const LogpsParams& p, hipStream_t st) {
-  if (p.bf16) backward<bf16>(p, st); else backward<float>(p, st);
+  const int64_t vectors = (p.vocab + (p.bf16 ? 7 : 3)) / (p.bf16 ? 8 : 4);
+#define LOGPS(GROUP) p.bf16 ? backward<bf16, GROUP>(p, st) : backward<float, GROUP>(p, st)
+  if (vectors <= 128) LOGPS(16);
+  else if (vectors <= 512) LOGPS(64);
+  else LOGPS(256);
+#undef LOGPS
   return hipGetLastError();
 }

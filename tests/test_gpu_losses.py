@@ -51,8 +51,8 @@ def _close(got, want, tol, what=""):
 
 # ---------------------------------------------------------------- log-probabilities of tokens
 # With a = scale (x - max): the difference, the factor and their product are rounded (3 u |a| in the exponent), the
-# exponential is good to a step (2 u), and a sum adds u for each of the terms that one lane adds up (at most V / 64 for
-# vocabularies up to 2048, V / 256 above, and two for each 16 of them where its maximum moves). So e_j is good to
+# exponential is good to a step (2 u), and a sum adds u for each of the terms that one lane adds up (a row is on at least 16
+# lanes, on 64 above a vocabulary of 1024, on 256 above 4096) and two for each 16 of them where its maximum moves. So e_j is good to
 # (3 |a_j| + 2) u, their sum to s = (3 sum p_j |a_j| + 2 + n) u; log1p to two steps (4 u).
 # The label is apart from the others' sum R, whose own error over the whole sum S is that of its terms alone: with d e_j <=
 # (3 |a_j| + 2 + n) u e_j, d R / S <= sum over j != label of p_j (3 |a_j| + 2 + n) u =: o. It is what log S = log1p(R + e - 1)
@@ -63,7 +63,7 @@ def _close(got, want, tol, what=""):
 # them are off by at most V 2^-126 in R, and so in log p, which is as small there.
 
 def _adds(V):
-    return V / (64 if V <= 2048 else 256) * 1.125 + 12
+    return V / (16 if V <= 1024 else 64 if V <= 4096 else 256) * 1.125 + 12
 
 
 def _others(a, p, lab):
