@@ -523,7 +523,7 @@ int moara_token_logps_backward(const void* logits, int32_t logits_dtype, int64_t
 
 /* Bytes of the workspace of moara_preference_loss and moara_policy_loss: device memory, 8-byte
  * aligned, of any contents, for one call at a time. */
-#define MOARA_LOSS_WORKSPACE(tokens, sequences) (56 * ((sequences) + (tokens) / 1024 + 2))
+#define MOARA_LOSS_WORKSPACE(tokens, sequences) (48 * ((sequences) + (tokens) / 512 + 130))
 
 enum { MOARA_PREF_SIGMOID = 0, MOARA_PREF_HINGE = 1, MOARA_PREF_SQUARE = 2 };
 
@@ -546,16 +546,17 @@ int moara_preference_default_config(moara_preference_config* out);
  *   square   (h - 1 / (2 beta))^2
  * out: 3 floats, means over the pairs with a token: the loss, the share with h > 0, beta h. 0 where
  *      there is no such pair.
- * out_rewards, out_slope: a float for each sequence: beta D, and the loss's derivative by each
- *      logp of the sequence.
+ * out_rewards: a float for each sequence: beta D.
+ * out_slope: sequences + 1 floats: the derivative of a pair's loss by each logp of a sequence, and the
+ *      factor of the mean (slope[s] slope[sequences] is the derivative of out[0]).
  * Sums are 64 bits. Errors: MOARA_E_ARG, MOARA_E_SHAPE (an odd number of sequences, tokens no
- * multiple of them without offsets, over 2^33 tokens or 2^22 sequences), MOARA_E_HIP. */
+ * multiple of them without offsets, over 2^33 tokens or 2^21 sequences), MOARA_E_HIP. */
 int moara_preference_loss(const moara_preference_config* cfg, const float* logp, const float* ref_logp, const uint8_t* mask,
                           int64_t tokens, const int64_t* offsets, int64_t sequences, float* out, float* out_rewards,
                           float* out_slope, void* workspace, void* stream);
 
-/* out_grad[t] = *grad_loss slope[sequence of t], 0 where t is left out. grad_loss: one float of
- * device memory, the gradient of out[0]. Errors as moara_preference_loss. */
+/* out_grad[t] = *grad_loss slope[sequences] slope[sequence of t], 0 where t is left out. grad_loss: one
+ * float of device memory, the gradient of out[0]. Errors as moara_preference_loss. */
 int moara_preference_loss_backward(const float* slope, const float* grad_loss, const uint8_t* mask, int64_t tokens,
                                    const int64_t* offsets, int64_t sequences, float* out_grad, void* stream);
 
@@ -584,7 +585,8 @@ int moara_policy_default_config(moara_policy_config* out);
  * Whether a token is clipped (r beyond the bound on the side that A pushes to) is decided in 64 bits.
  * out: 6 floats: the loss, sum -w gain, sum w kl, sum w entropy, sum w [clipped], sum w (e^d - d - 1)
  *      (the distance to the old policy). 0 where no token is left.
- * out_weight: a float for each sequence: its tokens' w (0 where the sequence has none).
+ * out_weight: sequences + 1 floats: w of a sequence's tokens (0 where it has none) is weight[s]
+ *      weight[sequences].
  * advantages have no gradient, nor have old_logp and ref_logp. Sums are 64 bits.
  * Errors: MOARA_E_ARG, MOARA_E_SHAPE (as moara_preference_loss), MOARA_E_HIP. */
 int moara_policy_loss(const moara_policy_config* cfg, const float* logp, const float* old_logp, const float* ref_logp,

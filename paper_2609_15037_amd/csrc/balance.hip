@@ -1,14 +1,14 @@
 // Load-balancing loss of expert routing, its counts and its gradient. Forward: a workgroup sums the scores and counts
 // the experts of a cell's tokens, a second launch adds up each sequence's cells and forms its loss, and where there
-// are several sequences a third one their mean. Backward: the scores again, and a row of the gradient for each token.
+// are several sequences a third one their mean; a few tokens of one sequence take one launch. Backward: the scores
+// again, and a row of the gradient for each token.
 #include <float.h>
 
-#include "lanes.h"
 #include "packed.h"
 
 namespace {
 
-constexpr int THREADS = 256, END_THREADS = 1024;
+constexpr int FORWARD_THREADS = 1024, BACKWARD_THREADS = 256, END_THREADS = 1024;
 
 // What a cell leaves in the workspace, experts padded to an even number: its scores' sums, its counts, z and its tokens.
 struct CellSums {
@@ -26,31 +26,50 @@ __device__ __forceinline__ double* about_sequences(const BalanceParams& p, int64
 
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
 
-// A token's scores (of a sigmoid over their sum, which exists where they underflow) and, for the gradient, 1 - sigmoid;
-// with z the softmax and the logits' log-sum-exp. False where it has no scores.
-template <int LANES, int V, bool BACKWARD>
-__device__ __forceinline__ bool token_scores(const float (&l)[V], int sigmoid, int want_z, float (&s)[V], float (&rest)[V],
-                                             float (&soft)[V], float& lse) {
-  float top = l[0], sum = 0;
+// A token's scores s (of a sigmoid over their sum, which exists where they underflow); for the gradient w = s times 1 -
+// sigmoid, or s; with z the softmax and the logits' log-sum-exp. False where it has no scores.
+template <int LANES, int V, bool SIGMOID, bool Z, bool BACKWARD>
+__device__ __forceinline__ bool token_scores(const float (&l)[V], float (&s)[V], float (&w)[V], float (&soft)[V], float& lse) {
+  float top = 0, sum = 0;
+  auto find_top = [&] {
+    top = l[0];
 #pragma unroll
-  for (int j = 1; j < V; ++j) top = fmaxf(top, l[j]);
-  top = max_of<LANES>(top);
+    for (int j = 1; j < V; ++j) top = fmaxf(top, l[j]);
+    top = max_of<LANES>(top);
+  };
+  if (Z || !SIGMOID) find_top();
   lse = 0;
-  if (sigmoid) {
-    const float shift = fminf(top, 0.f);
+  if (SIGMOID) {
+    // e^min(l, 0) / (1 + e^-|l|): e^min(l, 0) is the other exponential or 1
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const float q = exp_of(-fabsf(l[j])), r = 1.f / (1.f + q);
-      s[j] = exp_of(fminf(l[j], 0.f) - shift) * r;
-      if (BACKWARD) rest[j] = l[j] > 0 ? q * r : r;
+      const float q = exp_of(-fabsf(l[j])), r = __builtin_amdgcn_rcpf(1.f + q);
+      const float low = q * r;
+      s[j] = l[j] < 0 ? low : r;
+      if (BACKWARD) w[j] = l[j] < 0 ? r : low;
       sum += s[j];
     }
     sum = sum_of<LANES>(sum);
-    const bool there = sum > 0;         // not NaN, not a row of -infinity
-    const float y = 1.f / sum;
+    if (!(sum > 0x1p-30f)) {            // where they are small, or underflow, their quotients from the logits less the largest
+      if (!Z) find_top();
+      const float shift = fminf(top, 0.f);
+      sum = 0;
 #pragma unroll
-    for (int j = 0; j < V; ++j) s[j] *= y;
-    if (want_z) {
+      for (int j = 0; j < V; ++j) {
+        const float q = exp_of(-fabsf(l[j])), r = __builtin_amdgcn_rcpf(1.f + q);
+        s[j] = exp_of(fminf(l[j], 0.f) - shift) * r;
+        if (BACKWARD) w[j] = l[j] < 0 ? r : q * r;
+        sum += s[j];
+      }
+      sum = sum_of<LANES>(sum);
+    }
+    const float y = __builtin_amdgcn_rcpf(sum);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      s[j] *= y;
+      if (BACKWARD) w[j] *= s[j];
+    }
+    if (Z) {
       float total = 0;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
@@ -59,13 +78,11 @@ __device__ __forceinline__ bool token_scores(const float (&l)[V], int sigmoid, i
       }
       total = sum_of<LANES>(total);
       lse = top + logf(total);
-      if (BACKWARD) {
-        const float w = 1.f / total;
+      const float v = __builtin_amdgcn_rcpf(total);
 #pragma unroll
-        for (int j = 0; j < V; ++j) soft[j] *= w;
-      }
+      for (int j = 0; j < V; ++j) soft[j] *= v;
     }
-    return there;
+    return sum > 0;                     // not NaN, not a row of -infinity
   }
 #pragma unroll
   for (int j = 0; j < V; ++j) {
@@ -73,12 +90,11 @@ __device__ __forceinline__ bool token_scores(const float (&l)[V], int sigmoid, i
     sum += s[j];
   }
   sum = sum_of<LANES>(sum);
-  const bool there = sum > 0;           // not NaN: a row of -infinity, one with a NaN or +infinity
-  const float y = 1.f / sum;
+  const float y = __builtin_amdgcn_rcpf(sum);
 #pragma unroll
   for (int j = 0; j < V; ++j) s[j] *= y;
-  if (want_z) lse = top + logf(sum);
-  return there;
+  if (Z) lse = top + logf(sum);
+  return sum > 0;                       // not NaN: a row of -infinity, one with a NaN or +infinity
 }
 
 template <int LANES, int V> __device__ __forceinline__ void fetch(const BalanceParams& p, int64_t t, int lane, float (&l)[V]) {
@@ -89,54 +105,80 @@ template <int LANES, int V> __device__ __forceinline__ void fetch(const BalanceP
   }
 }
 
-template <int LANES, int V> __global__ __launch_bounds__(THREADS) void k_balance(BalanceParams p, int tile) {
-  constexpr int TOK = THREADS / LANES;
-  __shared__ float red[TOK * LANES * V];
-  __shared__ uint32_t hist[LANES * V];
-  __shared__ double part[THREADS / 64];
-  const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
-  const int64_t i = blockIdx.x;
-  const Cell c = cell_at(p.q, i, tile);
-  for (int e = threadIdx.x; e < LANES * V; e += THREADS) hist[e] = 0;
-  __syncthreads();
-  float sum[V] = {};
-  double z = 0, n = 0;
-  for (int64_t t0 = c.begin; t0 < c.end; t0 += TOK) {
-    const int64_t t = t0 + slot;
-    const bool in = t < c.end;
-    float l[V], s[V], rest[V], soft[V], lse;
-    fetch<LANES, V>(p, in ? t : t0, lane, l);
-    const bool there = token_scores<LANES, V, false>(l, p.sigmoid, p.want_z, s, rest, soft, lse);
-    const bool on = in && there && !(p.q.mask && !p.q.mask[t]);
-    if (!on) continue;
-#pragma unroll
-    for (int j = 0; j < V; ++j) sum[j] += s[j];
-    if (lane == 0) {
-      n += 1;
-      z += (double)lse * (double)lse;
-    }
-    for (int j = lane; j < p.k; j += LANES) {
-      const int e = p.index[t * p.k + j];
-      if (e >= 0 && e < p.E) atomicAdd(&hist[e], 1u);
-    }
+// Sum over the tokens that share a wave: over the lanes of the same place in each group of LANES.
+template <int LANES> __device__ __forceinline__ float over_tokens(float x) {
+  float a, b;
+  if (LANES <= 8) x += __shfl_xor(x, 8, 64);
+  if (LANES <= 16) {
+    rows_apart<16>(x, a, b);
+    x = a + b;
   }
+  if (LANES <= 32) {
+    rows_apart<32>(x, a, b);
+    x = a + b;
+  }
+  return x;
+}
+
+// The sums of tokens [begin, end): scores in red[0 .. E), counts in hist, z and the number of tokens in about[0 .. 2).
+template <int LANES, int V, bool SIGMOID, bool Z> struct Sums {
+  static constexpr int WAVES = FORWARD_THREADS / 64, WIDE = LANES * V;
+  float red[WAVES][WIDE];
+  uint32_t hist[WIDE];
+  double part[WAVES][2];
+  __device__ __forceinline__ void add(const BalanceParams& p, int64_t begin, int64_t end, double (&about)[2]) {
+    constexpr int TOK = FORWARD_THREADS / LANES;
+    const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES, wave = threadIdx.x >> 6;
+    for (int e = threadIdx.x; e < WIDE; e += FORWARD_THREADS) hist[e] = 0;
+    float sum[V] = {}, l[V];
+    about[0] = about[1] = 0;
+    if (begin + slot < end) fetch<LANES, V>(p, begin + slot, lane, l);
+    __syncthreads();
+    for (int64_t t = begin + slot; t < end; t += TOK) {
+      const bool live = !p.q.mask || p.q.mask[t];
+      int e = lane < p.k ? p.index[t * p.k + lane] : -1;
+      float s[V], w[V], soft[V], lse;
+      const bool on = token_scores<LANES, V, SIGMOID, Z, false>(l, s, w, soft, lse) && live;
+      if (t + TOK < end) fetch<LANES, V>(p, t + TOK, lane, l);
 #pragma unroll
-  for (int j = 0; j < V; ++j) red[slot * (LANES * V) + expert_of<LANES>(j, lane)] = sum[j];
-  z = group_sum<THREADS>(z, part);
-  n = group_sum<THREADS>(n, part);
-  __syncthreads();
-  const CellSums w = {(char*)p.workspace, p.E};
-  for (int e = threadIdx.x; e < p.E; e += THREADS) {
+      for (int j = 0; j < V; ++j) sum[j] += on ? s[j] : 0.f;
+      if (on && lane == 0) {
+        about[0] += (double)lse * (double)lse;
+        about[1] += 1;
+      }
+      for (int j = lane; on && j < p.k; j += LANES) {
+        if (j != lane) e = p.index[t * p.k + j];
+        if (e >= 0 && e < p.E) atomicAdd(&hist[e], 1u);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float x = over_tokens<LANES>(sum[j]);
+      if ((threadIdx.x & 63) < LANES) red[wave][expert_of<LANES>(j, lane)] = x;
+    }
+    group_sums<FORWARD_THREADS>(about, part);           // its barrier is red's and hist's too
+  }
+  __device__ __forceinline__ float score(int e) const {
     float x = 0;
-#pragma unroll 4
-    for (int k = 0; k < TOK; ++k) x += red[k * (LANES * V) + e];
-    w.scores(i)[e] = x;
-    w.counts(i)[e] = hist[e];
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) x += red[i][e];
+    return x;
   }
-  if (threadIdx.x == 0) {
-    w.about(i)[0] = z;
-    w.about(i)[1] = n;
+};
+
+template <int LANES, int V, bool SIGMOID, bool Z>
+__global__ __launch_bounds__(FORWARD_THREADS) void k_balance(BalanceParams p, int shift) {
+  __shared__ Sums<LANES, V, SIGMOID, Z> sums;
+  const int64_t i = blockIdx.x;
+  const Cell c = cell_at(p.q, i, shift);
+  double about[2];
+  sums.add(p, c.begin, c.end, about);
+  const CellSums w = {(char*)p.workspace, p.E};
+  if ((int)threadIdx.x < p.E) {
+    w.scores(i)[threadIdx.x] = sums.score(threadIdx.x);
+    w.counts(i)[threadIdx.x] = sums.hist[threadIdx.x];
   }
+  if (threadIdx.x < 2) w.about(i)[threadIdx.x] = about[threadIdx.x];
 }
 
 // out and the factors of the gradient, from the sums over the sequences.
@@ -150,19 +192,54 @@ __device__ __forceinline__ void balance_out(const BalanceParams& p, double balan
   tail[1] = (float)(2 * p.z_coef * per);
 }
 
+// A sequence's balance from its experts' sums, x and c of expert e in the threads of one row (mine); total: of c.
+__device__ __forceinline__ double sequence_balance(const BalanceParams& p, int64_t s, int e, bool mine, double x, double c,
+                                                   double total, double n, double (*part)[1]) {
+  // f less its mean, 1: scores sum to 1, so a constant has no gradient, and nothing cancels where the load is even
+  const double f = total > 0 ? p.E * c / total : 0, per = n > 0 ? 1 / n : 0;
+  if (mine) p.slope[s * p.E + e] = total > 0 ? (float)((f - 1) * per) : 0.f;
+  double balance[1] = {mine ? f * x * per : 0.0};
+  group_sums<END_THREADS>(balance, part);
+  return balance[0];
+}
+
+// All tokens of one sequence in one workgroup.
+template <int LANES, int V, bool SIGMOID, bool Z>
+__global__ __launch_bounds__(FORWARD_THREADS) void k_balance_small(BalanceParams p, int shift) {
+  __shared__ Sums<LANES, V, SIGMOID, Z> sums;
+  __shared__ double part[END_THREADS / 64][1], part2[END_THREADS / 64][1];
+  const int64_t begin = first_token(p.q, 0), end = first_token(p.q, 1);
+  double about[2];
+  sums.add(p, begin, end, about);
+  const int e = threadIdx.x;
+  const bool mine = e < p.E;
+  const int64_t own = mine ? sums.hist[e] : 0, c = mine && p.load ? p.load[e] : own;
+  if (mine) p.counts[e] = own;
+  double total[1] = {(double)c};
+  group_sums<END_THREADS>(total, part);
+  const double balance = sequence_balance(p, 0, e, mine, mine ? sums.score(e) : 0.0, (double)c, total[0], about[1], part2);
+  if (threadIdx.x == 0) balance_out(p, balance, about[1] > 0 ? 1 : 0, about[0], about[1]);
+}
+
 // One workgroup for each sequence: threads take an expert and every so many-th cell.
-__global__ __launch_bounds__(END_THREADS) void k_balance_end(BalanceParams p, int tile, int64_t cells) {
+__global__ __launch_bounds__(END_THREADS) void k_balance_end(BalanceParams p, int shift, int64_t cells) {
   __shared__ double score[END_THREADS];
   __shared__ long long count[END_THREADS];
-  __shared__ double part[END_THREADS / 64];
+  __shared__ double part[END_THREADS / 64][3], part2[END_THREADS / 64][1];
   const int64_t s = blockIdx.x;
   const CellSums w = {(char*)p.workspace, p.E};
   int64_t first, last;
-  cells_of(p.q, s, tile, first, last);
+  cells_of(p.q, s, shift, first, last);
   int width = 64;
   while (width < p.E) width *= 2;
   const int e = threadIdx.x & (width - 1), row = threadIdx.x / width, rows = END_THREADS / width;
-  double x = 0;
+  const bool mine = row == 0 && e < p.E;
+  const long long load = mine && p.load ? p.load[e] : 0;
+  double all[3] = {}, x = 0;            // counts, z, tokens
+  for (int64_t i = first + threadIdx.x; i < last; i += END_THREADS) {
+    all[1] += w.about(i)[0];
+    all[2] += w.about(i)[1];
+  }
   long long c = 0;
   if (e < p.E) {
 #pragma unroll 4
@@ -171,91 +248,77 @@ __global__ __launch_bounds__(END_THREADS) void k_balance_end(BalanceParams p, in
       c += w.counts(i)[e];
     }
   }
-  double z = 0, n = 0;
-  for (int64_t i = first + threadIdx.x; i < last; i += END_THREADS) {
-    z += w.about(i)[0];
-    n += w.about(i)[1];
-  }
-  z = group_sum<END_THREADS>(z, part);
-  n = group_sum<END_THREADS>(n, part);
+  all[0] = p.load ? (double)load : (double)c;
   score[threadIdx.x] = x;
   count[threadIdx.x] = c;
-  __syncthreads();
-  const bool mine = row == 0 && e < p.E;
-  x = 0;
-  c = 0;
+  group_sums<END_THREADS>(all, part);
   if (mine) {
-    for (int k = 0; k < rows; ++k) {
+#pragma unroll 4
+    for (int k = 1; k < rows; ++k) {
       x += score[k * width + e];
       c += count[k * width + e];
     }
     p.counts[s * p.E + e] = c;
-    if (p.load) c = p.load[e];
+    if (p.load) c = load;
   }
-  const double total = group_sum<END_THREADS>(mine ? (double)c : 0.0, part);
-  // f less its mean, 1: scores sum to 1, so a constant has no gradient, and nothing cancels where the load is even
-  const double f = total > 0 ? p.E * (double)c / total : 0, per = n > 0 ? 1 / n : 0;
-  const double balance = group_sum<END_THREADS>(mine ? f * x * per : 0.0, part);
-  if (mine) p.slope[s * p.E + e] = total > 0 ? (float)((f - 1) * per) : 0.f;
+  const double balance = sequence_balance(p, s, e, mine, x, (double)c, all[0], all[2], part2);
   if (threadIdx.x) return;
   if (p.q.sequences == 1) {
-    balance_out(p, balance, n > 0 ? 1 : 0, z, n);
+    balance_out(p, balance, all[2] > 0 ? 1 : 0, all[1], all[2]);
   } else {
     double* a = about_sequences(p, cells) + 4 * s;
     a[0] = balance;
-    a[1] = n > 0 ? 1 : 0;
-    a[2] = z;
-    a[3] = n;
+    a[1] = all[2] > 0 ? 1 : 0;
+    a[2] = all[1];
+    a[3] = all[2];
   }
 }
 __global__ __launch_bounds__(END_THREADS) void k_balance_out(BalanceParams p, int64_t cells) {
-  __shared__ double part[END_THREADS / 64];
+  __shared__ double part[END_THREADS / 64][4];
   const double* a = about_sequences(p, cells);
   double sum[4] = {};
   for (int64_t s = threadIdx.x; s < p.q.sequences; s += END_THREADS)
 #pragma unroll
     for (int k = 0; k < 4; ++k) sum[k] += a[4 * s + k];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) sum[k] = group_sum<END_THREADS>(sum[k], part);
+  group_sums<END_THREADS>(sum, part);
   if (threadIdx.x == 0) balance_out(p, sum[0], sum[1], sum[2], sum[3]);
 }
 
-template <int LANES, int V> __global__ __launch_bounds__(THREADS) void k_balance_backward(BalanceParams p, int tile) {
-  constexpr int TOK = THREADS / LANES;
+template <int LANES, int V, bool SIGMOID, bool Z>
+__global__ __launch_bounds__(BACKWARD_THREADS) void k_balance_backward(BalanceParams p, int shift) {
+  constexpr int TOK = BACKWARD_THREADS / LANES;
   const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
-  const Cell c = cell_at(p.q, blockIdx.x, tile);
   const float* tail = p.slope + p.q.sequences * p.E;
   const float g = *p.grad_loss, a = g * tail[0], b = g * tail[1];
-  float f[V];
+  const Cell c = cell_at(p.q, blockIdx.x, shift);
+  float f[V], l[V];
+  if (c.begin + slot < c.end) fetch<LANES, V>(p, c.begin + slot, lane, l);
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     const int e = expert_of<LANES>(j, lane);
     f[j] = c.seq >= 0 && e < p.E ? p.slope[c.seq * p.E + e] * a : 0.f;
   }
-  for (int64_t t0 = c.begin; t0 < c.end; t0 += TOK) {
-    const int64_t t = t0 + slot;
-    const bool in = t < c.end;
-    float l[V], s[V], rest[V], soft[V], lse;
-    fetch<LANES, V>(p, in ? t : t0, lane, l);
-    const bool there = token_scores<LANES, V, true>(l, p.sigmoid, p.want_z, s, rest, soft, lse);
-    const bool on = in && there && !(p.q.mask && !p.q.mask[t]);
+  for (int64_t t = c.begin + slot; t < c.end; t += TOK) {
+    const bool live = !p.q.mask || p.q.mask[t];
+    float s[V], w[V], soft[V], lse;
+    const bool on = token_scores<LANES, V, SIGMOID, Z, true>(l, s, w, soft, lse) && live;
+    if (t + TOK < c.end) fetch<LANES, V>(p, t + TOK, lane, l);
     float mean = 0;
 #pragma unroll
     for (int j = 0; j < V; ++j) mean = fmaf(f[j], s[j], mean);
     mean = sum_of<LANES>(mean);
-    if (!in) continue;
-    float x[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      float d = s[j] * (f[j] - mean);
-      if (p.sigmoid) d *= rest[j];
-      if (p.want_z) d = fmaf(b * lse, p.sigmoid ? soft[j] : s[j], d);
-      x[j] = on ? d : 0.f;
-    }
+    const float zl = b * lse;
 #pragma unroll
     for (int j = 0; j < V; j += 4) {
+      float x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float d = (SIGMOID ? w[j + i] : s[j + i]) * (f[j + i] - mean);
+        if (Z) d = fmaf(zl, SIGMOID ? soft[j + i] : s[j + i], d);
+        x[i] = on ? d : 0.f;
+      }
       const int e = expert_of<LANES>(j, lane);
-      store4(p.grad, p.bf16, t * p.E + e, p.E - e, x + j);
+      store4(p.grad, p.bf16, t * p.E + e, p.E - e, x);
     }
   }
   auto clear = [&](int64_t from, int64_t to) {
@@ -271,33 +334,51 @@ template <int LANES, int V> __global__ __launch_bounds__(THREADS) void k_balance
   clear(c.fill2, c.fill3);
 }
 
-// Tokens of a tile: enough for 256 workgroups, a multiple of what one takes at a time.
-int tile_of(const BalanceParams& p) {
-  int64_t tile = BALANCE_LEAST_TILE;
-  while (tile * 256 < p.q.tokens && tile < 1 << 20) tile *= 2;
-  return (int)tile;
+// Tokens of a tile, as a power of 2: no more workgroups than `most`, if 2^20 tokens a tile do.
+int tile_of(const BalanceParams& p, int64_t most) {
+  int shift = BALANCE_LEAST_SHIFT;
+  while (most << shift < p.q.tokens && shift < 20) ++shift;
+  return shift;
 }
+
+#define BALANCE_FORM(kernel, LANES, V)                                                                              \
+  do {                                                                                                              \
+    if (p.sigmoid && p.want_z) hipLaunchKernelGGL((kernel<LANES, V, true, true>), g, b, 0, st, p, shift);           \
+    else if (p.sigmoid) hipLaunchKernelGGL((kernel<LANES, V, true, false>), g, b, 0, st, p, shift);                 \
+    else if (p.want_z) hipLaunchKernelGGL((kernel<LANES, V, false, true>), g, b, 0, st, p, shift);                  \
+    else hipLaunchKernelGGL((kernel<LANES, V, false, false>), g, b, 0, st, p, shift);                               \
+  } while (0)
+#define BALANCE_ON(kernel)                                \
+  do {                                                    \
+    if (p.E <= 32) BALANCE_FORM(kernel, 8, 4);            \
+    else if (p.E <= 64) BALANCE_FORM(kernel, 16, 4);      \
+    else if (p.E <= 128) BALANCE_FORM(kernel, 16, 8);     \
+    else if (p.E <= 256) BALANCE_FORM(kernel, 32, 8);     \
+    else if (p.E <= 512) BALANCE_FORM(kernel, 64, 8);     \
+    else BALANCE_FORM(kernel, 64, 16);                    \
+  } while (0)
+
+int lanes_of(int E) { return E <= 32 ? 8 : E <= 128 ? 16 : E <= 256 ? 32 : 64; }
 
 }  // namespace
 
-#define BALANCE_ON(kernel, ...)                                                                                       \
-  do {                                                                                                                \
-    const dim3 g((uint32_t)cells), b(THREADS);                                                                        \
-    if (p.E <= 32) hipLaunchKernelGGL((kernel<8, 4>), g, b, 0, st, __VA_ARGS__);                                      \
-    else if (p.E <= 64) hipLaunchKernelGGL((kernel<16, 4>), g, b, 0, st, __VA_ARGS__);                                \
-    else if (p.E <= 128) hipLaunchKernelGGL((kernel<16, 8>), g, b, 0, st, __VA_ARGS__);                               \
-    else if (p.E <= 256) hipLaunchKernelGGL((kernel<16, 16>), g, b, 0, st, __VA_ARGS__);                              \
-    else if (p.E <= 512) hipLaunchKernelGGL((kernel<32, 16>), g, b, 0, st, __VA_ARGS__);                              \
-    else hipLaunchKernelGGL((kernel<64, 16>), g, b, 0, st, __VA_ARGS__);                                              \
-  } while (0)
-
 hipError_t launch_balance(const BalanceParams& p, hipStream_t st) {
-  const int tile = tile_of(p);
-  const int64_t cells = cells_of_all(p.q, tile);
-  if (cells > 0) BALANCE_ON(k_balance, p, tile);
+  int shift = 0;
+  const dim3 b(FORWARD_THREADS);
+  if (p.q.sequences == 1 && p.q.tokens <= 8 * (FORWARD_THREADS / lanes_of(p.E))) {
+    const dim3 g(1);
+    BALANCE_ON(k_balance_small);
+    return hipGetLastError();
+  }
+  shift = tile_of(p, 256);
+  const int64_t cells = cells_of_all(p.q, shift);
+  if (cells > 0) {
+    const dim3 g((uint32_t)cells);
+    BALANCE_ON(k_balance);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_balance_end, dim3((uint32_t)p.q.sequences), dim3(END_THREADS), 0, st, p, tile, cells);
+  hipLaunchKernelGGL(k_balance_end, dim3((uint32_t)p.q.sequences), dim3(END_THREADS), 0, st, p, shift, cells);
   e = hipGetLastError();
   if (e != hipSuccess || p.q.sequences == 1) return e;
   hipLaunchKernelGGL(k_balance_out, dim3(1), dim3(END_THREADS), 0, st, p, cells);
@@ -305,8 +386,11 @@ hipError_t launch_balance(const BalanceParams& p, hipStream_t st) {
 }
 
 hipError_t launch_balance_backward(const BalanceParams& p, hipStream_t st) {
-  const int tile = tile_of(p);
-  const int64_t cells = cells_of_all(p.q, tile);
-  if (cells > 0) BALANCE_ON(k_balance_backward, p, tile);
+  const int shift = tile_of(p, 2048);
+  const int64_t cells = cells_of_all(p.q, shift);
+  if (cells > 0) {
+    const dim3 g((uint32_t)cells), b(BACKWARD_THREADS);
+    BALANCE_ON(k_balance_backward);
+  }
   return hipGetLastError();
 }

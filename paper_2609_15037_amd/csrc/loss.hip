@@ -1,27 +1,87 @@
 // Losses over packed sequences of tokens' log-probabilities: pairs of responses, and a clipped policy. Both sum
-// over a sequence's tokens, so their forward pass is two steps: a wave sums a cell (tokens of one sequence within
-// one tile) in 64 bits, then one workgroup adds up each sequence's cells, in order, and forms the loss.
+// over a sequence's tokens, so their forward pass is two steps: a wave sums a cell (the tokens of one sequence in one
+// tile) in 64 bits, and a workgroup of several the neighbouring cells of one sequence, then one workgroup adds up each sequence's
+// sums, in order, and forms the loss. Few cells take both steps in one launch. Their gradients are one launch, a wave for
+// each cell.
 #include "packed.h"
 
 namespace {
 
-constexpr int END_THREADS = 1024;
+constexpr int END_THREADS = 1024;           // of both steps
+constexpr int ONE = 8;          // a tile of which a lane takes four tokens, as a power of 2
+constexpr int FEW = END_THREADS / 64;   // cells that one launch takes
+constexpr int GROUP = 8;                // else cells of a workgroup
 
-// e^q - q - 1. The three cancel near 0: there its series, q^2 (1/2 + q/6 + ..), to 1e-9 of its value at |q| = 1/2.
-__device__ __forceinline__ float exp_excess(float q) {
-  if (fabsf(q) < 0.5f) {
-    float s = 1.f / 3628800.f;
-    s = fmaf(s, q, 1.f / 362880.f);
-    s = fmaf(s, q, 1.f / 40320.f);
-    s = fmaf(s, q, 1.f / 5040.f);
-    s = fmaf(s, q, 1.f / 720.f);
-    s = fmaf(s, q, 1.f / 120.f);
-    s = fmaf(s, q, 1.f / 24.f);
-    s = fmaf(s, q, 1.f / 6.f);
-    s = fmaf(s, q, 0.5f);
-    return s * q * q;
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32u __attribute__((aligned(1)));
+// A cell's tokens counted from its tile's first: its own [begin, end), those it clears, and how many there are at all.
+struct Span {
+  int64_t seq, tile;
+  int begin, end, fill0, fill1, fill2, fill3, left;
+};
+template <int SHIFT> __device__ __forceinline__ Span span_of(const Packed& q, int64_t i) {
+  const Cell c = cell_at(q, i, SHIFT);
+  auto from_tile = [&](int64_t t) {
+    const int64_t d = t - c.tile;
+    return d < 0 ? 0 : d > 1 << SHIFT ? 1 << SHIFT : (int)d;
+  };
+  return Span{c.seq, c.tile, from_tile(c.begin), from_tile(c.end), from_tile(c.fill0), from_tile(c.fill1), from_tile(c.fill2),
+              from_tile(c.fill3), from_tile(q.tokens)};
+}
+__device__ __forceinline__ int within(int r, int from, int to) { return r >= from && r < to; }
+// Four tokens from the r-th of a tile: all in one access where they exist.
+__device__ __forceinline__ void load4(const float* q, const Span& c, int r, float (&x)[4]) {
+  q += c.tile;
+  if (r + 4 <= c.left) {
+    const f32x4u a = *reinterpret_cast<const f32x4u*>(q + r);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = a[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = r + j < c.left ? q[r + j] : 0.f;
   }
-  return expf(q) - 1.f - q;
+}
+__device__ __forceinline__ void zero4(float (&x)[4]) { x[0] = x[1] = x[2] = x[3] = 0.f; }
+// Which of four tokens are in the cell: bit j for token r + j. And of these the ones that count: the mask's bytes are asked
+// for with the tokens' values, not before them.
+__device__ __forceinline__ int inside4(const Span& c, int r) {
+  int in = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) in |= within(r + j, c.begin, c.end) << j;
+  return in;
+}
+__device__ __forceinline__ uint32_t mask4(const Packed& q, const Span& c, int r) {
+  if (!q.mask) return 0x01010101u;
+  const uint8_t* m = q.mask + c.tile;
+  if (r + 4 <= c.left) return *reinterpret_cast<const u32u*>(m + r);
+  uint32_t x = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (r + j < c.left) x |= (uint32_t)m[r + j] << (8 * j);
+  return x;
+}
+__device__ __forceinline__ int live4(int in, uint32_t mask) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) in &= ~((mask >> (8 * j) & 0xFF ? 0 : 1) << j);
+  return in;
+}
+// Writes four tokens' gradients, the cell's and the zeros it has to clear.
+__device__ __forceinline__ void store4(float* q, const Span& c, int r, const float (&x)[4]) {
+  const int own = inside4(c, r);
+  int clear = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) clear |= (within(r + j, c.fill0, c.fill1) | within(r + j, c.fill2, c.fill3)) << j;
+  q += c.tile;
+  if ((own | clear) == 15) {
+    f32x4u a;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a[j] = own >> j & 1 ? x[j] : 0.f;
+    *reinterpret_cast<f32x4u*>(q + r) = a;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if ((own | clear) >> j & 1) q[r + j] = own >> j & 1 ? x[j] : 0.f;
+  }
 }
 
 // Lanes of a sequence in the second step: as many as there are for each.
@@ -36,95 +96,152 @@ __device__ __forceinline__ double over_lanes(double x, int lanes) {
   return x;
 }
 
+// Cells' sums of a workgroup, and whose they are.
+template <int N, int W> struct CellSums {
+  double sum[W][N];
+  int64_t seq[W];
+};
+// What the workgroup's cells, from cell i0 on, leave: at the first cell of each sequence the sum of its cells among them.
+template <int N, int W> __device__ __forceinline__ void leave(const CellSums<N, W>& s, int64_t i0, int64_t cells, double* sums) {
+  __syncthreads();
+  const int w = threadIdx.x / N, k = threadIdx.x % N;
+  if (w >= W || i0 + w >= cells || (w > 0 && s.seq[w] == s.seq[w - 1])) return;
+  double x = 0;
+  for (int v = w; v < W && i0 + v < cells && s.seq[v] == s.seq[w]; ++v) x += s.sum[v][k];
+  sums[(i0 + w) * N + k] = x;
+}
+// Adds up a sequence's sums, of cells [first, last), by `lanes` lanes: those at its first cell and at each workgroup's
+// first. Four at a time, past the end the last one without weight.
+template <int W, int N> __device__ __forceinline__ void gather(const double* sums, int64_t first, int64_t last, int lane, int lanes,
+                                                        double (&own)[N]) {
+#pragma unroll
+  for (int k = 0; k < N; ++k) own[k] = 0;
+  const int64_t group = first / W, n = last > first ? (last - 1) / W - group + 1 : 0;
+  for (int64_t j = lane; j < n; j += 4 * lanes)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t at = j + u * lanes, e = at < n ? at : n - 1;
+      const double* x = sums + N * (e ? (group + e) * W : first);
+#pragma unroll
+      for (int k = 0; k < N; ++k) own[k] += at < n ? x[k] : 0.0;
+    }
+}
+
 // ---------------------------------------------------------------- pairs of responses
-__device__ __forceinline__ void preference_cell(const PreferenceParams& p, int64_t i) {
-  const Cell c = cell_at(p.q, i, LOSS_CELL);
-  double sum = 0, n = 0;
-#pragma unroll 4
-  for (int64_t t = c.begin + (threadIdx.x & 63); t < c.end; t += 64) {
-    const bool on = !p.q.mask || p.q.mask[t];
-    const double d = (double)p.logp[t] - (p.ref ? (double)p.ref[t] : 0.0);
-    sum += on ? d : 0.0;
-    n += on ? 1.0 : 0.0;
+constexpr int PREFERENCE_SUMS = 2;      // of logp - ref, and the number of tokens
+
+template <int SHIFT, int W>
+__device__ __forceinline__ void preference_cell(const PreferenceParams& p, int64_t i, CellSums<PREFERENCE_SUMS, W>& s) {
+  constexpr int TURNS = 1 << (SHIFT - ONE);
+  const Span c = span_of<SHIFT>(p.q, i);
+  double sum = 0;
+  int count = 0, in[TURNS];
+  uint32_t mask[TURNS];
+  float x[TURNS][4], y[TURNS][4];
+#pragma unroll
+  for (int v = 0; v < TURNS; ++v) {     // all of a lane's loads are on their way before the first is used
+    const int r = 4 * (threadIdx.x & 63) + 256 * v;
+    in[v] = inside4(c, r);
+    mask[v] = 0;
+    zero4(x[v]);
+    zero4(y[v]);
+    if (in[v]) {
+      mask[v] = mask4(p.q, c, r);
+      load4(p.logp, c, r, x[v]);
+      if (p.ref) load4(p.ref, c, r, y[v]);
+    }
   }
-  sum = wave_sum_d(sum);
-  n = wave_sum_d(n);
+#pragma unroll
+  for (int v = 0; v < TURNS; ++v) {
+    const int on = live4(in[v], mask[v]);
+    count += __popc(on);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum += on >> j & 1 ? (double)x[v][j] - (double)y[v][j] : 0.0;
+  }
+  sum = sum_of<64>(sum);
+  const double n = sum_of<64>((double)count);
   if ((threadIdx.x & 63) == 0) {
-    p.sums[2 * i] = sum;
-    p.sums[2 * i + 1] = n;
+    const int w = threadIdx.x >> 6;
+    s.sum[w][0] = sum;
+    s.sum[w][1] = n;
+    s.seq[w] = c.seq;
   }
 }
 
-__device__ __forceinline__ double log1p_exp(double z) { return fmax(z, 0.0) + log1p(exp(-fabs(z))); }
-
-__device__ __forceinline__ void preference_end(const PreferenceParams& p) {
-  __shared__ double part[END_THREADS / 64];
+template <int SHIFT, int W> __device__ __forceinline__ void preference_end(const PreferenceParams& p, const double* sums) {
+  __shared__ double part[END_THREADS / 64][4];
   const int64_t pairs = p.q.sequences / 2;
   const int lanes = lanes_of_each(pairs), lane = threadIdx.x & (lanes - 1);
-  double loss = 0, ahead = 0, margin = 0, live = 0;
+  double all[4] = {};           // loss, pairs ahead, margin, pairs with a token
   for (int64_t pair = threadIdx.x / lanes; pair < pairs; pair += END_THREADS / lanes) {
     double d[2], n[2];
+#pragma unroll
     for (int k = 0; k < 2; ++k) {
       int64_t first, last;
-      cells_of(p.q, 2 * pair + k, LOSS_CELL, first, last);
-      double s = 0, m = 0;
-      for (int64_t i = first + lane; i < last; i += lanes) {
-        s += p.sums[2 * i];
-        m += p.sums[2 * i + 1];
+      cells_of(p.q, 2 * pair + k, SHIFT, first, last);
+      double own[PREFERENCE_SUMS];
+      gather<W>(sums, first, last, lane, lanes, own);
+      d[k] = over_lanes(own[0], lanes);
+      n[k] = over_lanes(own[1], lanes);
+    }
+    if (lane == 0) {
+      const double per0 = p.average && n[0] > 0 ? 1 / n[0] : 1, per1 = p.average && n[1] > 0 ? 1 / n[1] : 1;
+      d[0] *= per0;
+      d[1] *= per1;
+      const double h = d[0] - d[1], z = p.beta * h - p.margin;
+      double l, dl;             // the loss and its derivative by h
+      if (p.kind == 0) {
+        // log(1 + e^-z) = max(-z, 0) + log(1 + u), u = e^-|z|, and the same of z; 1 / (1 + e^z) from u too
+        const double u = exp(-fabs(z)), log = log1p(u), y = 1 / (1 + u);
+        l = (1 - p.smoothing) * (fmax(-z, 0.0) + log) + (p.smoothing != 0 ? p.smoothing * (fmax(z, 0.0) + log) : 0);
+        dl = p.beta * (p.smoothing - (z > 0 ? u * y : y));
+      } else if (p.kind == 1) {
+        l = z < 1 ? 1 - z : z != z ? z : 0;
+        dl = z < 1 ? -p.beta : 0;
+      } else {
+        const double off = h - 0.5 / p.beta;
+        l = off * off;
+        dl = 2 * off;
       }
-      d[k] = over_lanes(s, lanes);
-      n[k] = over_lanes(m, lanes);
-    }
-    if (lane) continue;
-    const double per0 = p.average && n[0] > 0 ? 1 / n[0] : 1, per1 = p.average && n[1] > 0 ? 1 / n[1] : 1;
-    d[0] *= per0;
-    d[1] *= per1;
-    const double h = d[0] - d[1], z = p.beta * h - p.margin;
-    double l, dl;               // the loss and its derivative by h
-    if (p.kind == 0) {
-      l = (1 - p.smoothing) * log1p_exp(-z) + p.smoothing * log1p_exp(z);
-      dl = p.beta * (p.smoothing - 1 / (1 + exp(z)));
-    } else if (p.kind == 1) {
-      l = z < 1 ? 1 - z : z != z ? z : 0;
-      dl = z < 1 ? -p.beta : 0;
-    } else {
-      l = (h - 0.5 / p.beta) * (h - 0.5 / p.beta);
-      dl = 2 * (h - 0.5 / p.beta);
-    }
-    p.rewards[2 * pair] = (float)(p.beta * d[0]);
-    p.rewards[2 * pair + 1] = (float)(p.beta * d[1]);
-    const bool on = n[0] + n[1] > 0;
-    p.slope[2 * pair] = on ? (float)(dl * per0) : 0.f;
-    p.slope[2 * pair + 1] = on ? (float)(-dl * per1) : 0.f;
-    if (on) {
-      loss += l;
-      ahead += h > 0 ? 1 : 0;
-      margin += p.beta * h;
-      live += 1;
+      p.rewards[2 * pair] = (float)(p.beta * d[0]);
+      p.rewards[2 * pair + 1] = (float)(p.beta * d[1]);
+      const bool on = n[0] + n[1] > 0;
+      p.slope[2 * pair] = on ? (float)(dl * per0) : 0.f;
+      p.slope[2 * pair + 1] = on ? (float)(-dl * per1) : 0.f;
+      if (on) {
+        all[0] += l;
+        all[1] += h > 0 ? 1 : 0;
+        all[2] += p.beta * h;
+        all[3] += 1;
+      }
     }
   }
-  loss = group_sum<END_THREADS>(loss, part);
-  ahead = group_sum<END_THREADS>(ahead, part);
-  margin = group_sum<END_THREADS>(margin, part);
-  live = group_sum<END_THREADS>(live, part);
-  const double share = live > 0 ? 1 / live : 0;
-  for (int64_t pair = threadIdx.x / lanes; pair < pairs; pair += END_THREADS / lanes) {
-    if (lane) continue;         // the thread that wrote them
-    p.slope[2 * pair] = (float)(p.slope[2 * pair] * share);
-    p.slope[2 * pair + 1] = (float)(p.slope[2 * pair + 1] * share);
-  }
+  group_sums<END_THREADS>(all, part);
   if (threadIdx.x == 0) {
-    p.out[0] = (float)(loss * share);
-    p.out[1] = (float)(ahead * share);
-    p.out[2] = (float)(margin * share);
+    const double share = all[3] > 0 ? 1 / all[3] : 0;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) p.out[k] = (float)(all[k] * share);
+    p.slope[p.q.sequences] = (float)share;
   }
 }
 
-__global__ __launch_bounds__(256) void k_preference_cells(PreferenceParams p, int64_t cells) {
-  const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (i < cells) preference_cell(p, i);
+template <int SHIFT> __global__ __launch_bounds__(64 * GROUP) void k_preference_cells(PreferenceParams p, int64_t cells) {
+  __shared__ CellSums<PREFERENCE_SUMS, GROUP> s;
+  const int64_t i0 = (int64_t)blockIdx.x * GROUP, i = i0 + (threadIdx.x >> 6);
+  if (i < cells) preference_cell<SHIFT>(p, i, s);
+  leave(s, i0, cells, p.sums);
 }
-__global__ __launch_bounds__(END_THREADS) void k_preference_end(PreferenceParams p) { preference_end(p); }
+template <int SHIFT> __global__ __launch_bounds__(END_THREADS) void k_preference_end(PreferenceParams p) { preference_end<SHIFT, GROUP>(p, p.sums); }
+// All cells in one workgroup.
+__global__ __launch_bounds__(END_THREADS) void k_preference_small(PreferenceParams p, int64_t cells) {
+  __shared__ CellSums<PREFERENCE_SUMS, FEW> s;
+  __shared__ double sums[FEW * PREFERENCE_SUMS];
+  const int64_t i = threadIdx.x >> 6;
+  if (i < cells) preference_cell<ONE>(p, i, s);
+  leave(s, 0, cells, sums);
+  __syncthreads();
+  preference_end<ONE, FEW>(p, sums);
+}
 
 // A token's gradient is its sequence's slope: written once, nothing but the mask is read for it.
 __global__ __launch_bounds__(256) void k_preference_backward(Packed q, const float* __restrict__ slope,
@@ -132,160 +249,229 @@ __global__ __launch_bounds__(256) void k_preference_backward(Packed q, const flo
                                                              int64_t cells) {
   const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (i >= cells) return;
-  const int lane = threadIdx.x & 63;
-  const Cell c = cell_at(q, i, LOSS_CELL);
-  const float g = c.seq >= 0 ? slope[c.seq] * *grad_loss : 0.f;
-  for (int64_t t = c.begin + lane; t < c.end; t += 64) grad[t] = !q.mask || q.mask[t] ? g : 0.f;
-  for (int64_t t = c.fill0 + lane; t < c.fill1; t += 64) grad[t] = 0.f;
-  for (int64_t t = c.fill2 + lane; t < c.fill3; t += 64) grad[t] = 0.f;
+  const float all = slope[q.sequences] * *grad_loss;
+  const Span c = span_of<ONE>(q, i);
+  const int r = 4 * (threadIdx.x & 63);
+  const float g = c.seq >= 0 ? slope[c.seq] * all : 0.f;
+  const int in = inside4(c, r), on = live4(in, in ? mask4(q, c, r) : 0);
+  float x[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = on >> j & 1 ? g : 0.f;
+  store4(grad, c, r, x);
 }
 
 // ---------------------------------------------------------------- clipped policy
+// e^q - q - 1, of q and e = e^q. The terms cancel near 0: there a series, q^2 (1/2 + q/6 + ..), good to 1e-9 of
+// its value at |q| = 1/2.
+__device__ __forceinline__ float exp_excess(float q, float e) {
+  float s = 1.f / 3628800.f;
+  s = fmaf(s, q, 1.f / 362880.f);
+  s = fmaf(s, q, 1.f / 40320.f);
+  s = fmaf(s, q, 1.f / 5040.f);
+  s = fmaf(s, q, 1.f / 720.f);
+  s = fmaf(s, q, 1.f / 120.f);
+  s = fmaf(s, q, 1.f / 24.f);
+  s = fmaf(s, q, 1.f / 6.f);
+  s = fmaf(s, q, 0.5f);
+  return fabsf(q) < 0.5f ? s * q * q : e - 1.f - q;
+}
+// e^q by the hardware's 2^x: the product's rounding, and what log2 e has beyond fp32, are put back to first order.
+__device__ __forceinline__ float exp_of(float q) {
+  constexpr float A = 1.44269504088896340736f, B = (float)(1.44269504088896340736 - (double)A), LN2 = 0.693147180559945309f;
+  const float t = q * A, e = __builtin_amdgcn_exp2f(t), r = fmaf(q, B, fmaf(q, A, -t));
+  return fabsf(t) < 128.f ? fmaf(e, r * LN2, e) : e;
+}
+
 // A token's terms. d and the comparison with the bounds are 64 bits: a ratio next to a bound falls on the side
 // that the difference of the two fp32 log-probabilities says.
 struct Token { float gain, slope, kl, dkl, excess; bool clipped; };
 __device__ __forceinline__ Token policy_token(const PolicyParams& p, float logp, float old, float ref, float a) {
   Token t;
   const double d = p.old ? (double)logp - (double)old : 0.0;
-  const float ratio = expf((float)d);
+  const float df = (float)d, ratio = exp_of(df), q = p.ref ? (float)((double)ref - (double)logp) : 0.f, e = exp_of(q);
   const bool up = d > p.high && a > 0, down = d < p.low && a < 0;
   t.clipped = up || down;
   t.gain = (up ? p.at_high : down ? p.at_low : ratio) * a;
   t.slope = t.clipped ? 0.f : -ratio * a;
-  t.excess = p.old ? exp_excess((float)d) : 0.f;
-  t.kl = t.dkl = 0.f;
-  if (p.ref) {
-    const float q = (float)((double)ref - (double)logp);
-    t.kl = p.kl == 0 ? exp_excess(q) : p.kl == 1 ? -q : 0.5f * q * q;
-    t.dkl = p.kl == 0 ? -expm1f(q) : p.kl == 1 ? 1.f : -q;
-  }
+  t.excess = exp_excess(df, ratio);
+  const float far = exp_excess(q, e), dfar = fabsf(q) < 0.5f ? q + far : e - 1.f;
+  t.kl = p.kl == 0 ? far : p.kl == 1 ? -q : 0.5f * q * q;
+  t.dkl = p.kl == 0 ? -dfar : p.kl == 1 ? 1.f : -q;
   return t;
 }
+struct Four { float logp[4], old[4], ref[4], a[4]; };
+__device__ __forceinline__ void fetch(const PolicyParams& p, const Span& c, int r, float each, Four& x) {
+  load4(p.logp, c, r, x.logp);
+  if (p.old) load4(p.old, c, r, x.old); else zero4(x.old);
+  if (p.ref) load4(p.ref, c, r, x.ref); else zero4(x.ref);
+  if (!p.sequence_advantages) load4(p.advantages, c, r, x.a);
+  else
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x.a[j] = each;
+}
 
-__device__ __forceinline__ void policy_cell(const PolicyParams& p, int64_t i) {
-  const Cell c = cell_at(p.q, i, LOSS_CELL);
-  double sum[POLICY_SUMS] = {};
+template <int SHIFT, int W>
+__device__ __forceinline__ void policy_cell(const PolicyParams& p, int64_t i, CellSums<POLICY_SUMS, W>& s) {
+  constexpr int TURNS = 1 << (SHIFT - ONE);
+  const Span c = span_of<SHIFT>(p.q, i);
   const float each = p.sequence_advantages && c.seq >= 0 ? p.advantages[c.seq] : 0.f;
-#pragma unroll 2
-  for (int64_t t = c.begin + (threadIdx.x & 63); t < c.end; t += 64) {
-    const bool on = !p.q.mask || p.q.mask[t];
-    const Token x = policy_token(p, p.logp[t], p.old ? p.old[t] : 0.f, p.ref ? p.ref[t] : 0.f,
-                                 p.sequence_advantages ? each : p.advantages[t]);
-    const float entropy = p.entropy ? p.entropy[t] : 0.f;
-    if (on) {
-      sum[0] += 1;
-      sum[1] -= (double)x.gain;
-      sum[2] += (double)x.kl;
-      sum[3] += (double)entropy;
-      sum[4] += x.clipped ? 1 : 0;
-      sum[5] += (double)x.excess;
-    }
+  double sum[POLICY_SUMS] = {};
+  int count = 0, clipped = 0;
+  Four x[TURNS];
+  float entropy[TURNS][4];
+  uint32_t mask[TURNS];
+  int in[TURNS];
+#pragma unroll
+  for (int v = 0; v < TURNS; ++v) {     // all of a lane's loads are on their way before the first is used
+    const int r = 4 * (threadIdx.x & 63) + 256 * v;
+    in[v] = inside4(c, r);
+    if (!in[v]) continue;
+    mask[v] = mask4(p.q, c, r);
+    fetch(p, c, r, each, x[v]);
+    if (p.entropy) load4(p.entropy, c, r, entropy[v]); else zero4(entropy[v]);
   }
 #pragma unroll
-  for (int k = 0; k < POLICY_SUMS; ++k) {
-    const double s = wave_sum_d(sum[k]);
-    if ((threadIdx.x & 63) == 0) p.sums[POLICY_SUMS * i + k] = s;
+  for (int v = 0; v < TURNS; ++v) {
+    if (!in[v]) continue;
+    const int on = live4(in[v], mask[v]);
+    count += __popc(on);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const Token y = policy_token(p, x[v].logp[j], x[v].old[j], x[v].ref[j], x[v].a[j]);
+      const bool live = on >> j & 1;
+      sum[1] -= live ? (double)y.gain : 0.0;
+      sum[2] += live ? (double)y.kl : 0.0;
+      sum[3] += live ? (double)entropy[v][j] : 0.0;
+      clipped += live && y.clipped;
+      sum[5] += live ? (double)y.excess : 0.0;
+    }
+  }
+  sum[0] = count;
+  sum[4] = clipped;
+#pragma unroll
+  for (int k = 0; k < POLICY_SUMS; ++k) sum[k] = sum_of<64>(sum[k]);
+  if ((threadIdx.x & 63) == 0) {
+    const int w = threadIdx.x >> 6;
+#pragma unroll
+    for (int k = 0; k < POLICY_SUMS; ++k) s.sum[w][k] = sum[k];
+    s.seq[w] = c.seq;
   }
 }
 
-__device__ __forceinline__ void policy_end(const PolicyParams& p) {
-  __shared__ double part[END_THREADS / 64];
+template <int SHIFT, int W> __device__ __forceinline__ void policy_end(const PolicyParams& p, const double* sums) {
+  constexpr int N = POLICY_SUMS + 1;
+  __shared__ double part[END_THREADS / 64][N];
   const int64_t S = p.q.sequences;
   const int lanes = lanes_of_each(S), lane = threadIdx.x & (lanes - 1);
-  double sum[POLICY_SUMS] = {}, live = 0;
+  double all[N] = {};           // the cells' sums, by sequence over its tokens, and the sequences with tokens
   for (int64_t s = threadIdx.x / lanes; s < S; s += END_THREADS / lanes) {
     int64_t first, last;
-    cells_of(p.q, s, LOSS_CELL, first, last);
-    double own[POLICY_SUMS] = {};
-    for (int64_t i = first + lane; i < last; i += lanes)
+    cells_of(p.q, s, SHIFT, first, last);
+    double own[POLICY_SUMS];
+    gather<W>(sums, first, last, lane, lanes, own);
+    // a sum over the lanes waits for the others' sums below, except where it divides them
+    const double n = over_lanes(own[0], lanes), per = !p.by_sequence ? 1 : n > 0 ? 1 / n : 0;
+    all[0] += own[0];
 #pragma unroll
-      for (int k = 0; k < POLICY_SUMS; ++k) own[k] += p.sums[POLICY_SUMS * i + k];
-#pragma unroll
-    for (int k = 0; k < POLICY_SUMS; ++k) own[k] = over_lanes(own[k], lanes);
-    if (lane) continue;
-    const double per = !p.by_sequence ? 1 : own[0] > 0 ? 1 / own[0] : 0;
-    live += own[0] > 0 ? 1 : 0;
-    sum[0] += own[0];
-#pragma unroll
-    for (int k = 1; k < POLICY_SUMS; ++k) sum[k] += own[k] * per;
-    p.weight[s] = own[0] > 0 ? (float)per : 0.f;
+    for (int k = 1; k < POLICY_SUMS; ++k) all[k] += own[k] * per;
+    if (lane == 0) {
+      all[POLICY_SUMS] += n > 0 ? 1 : 0;
+      p.weight[s] = n > 0 ? (float)per : 0.f;
+    }
   }
-  live = group_sum<END_THREADS>(live, part);
-#pragma unroll
-  for (int k = 0; k < POLICY_SUMS; ++k) sum[k] = group_sum<END_THREADS>(sum[k], part);
-  const double over = p.divisor > 0 ? p.divisor : p.by_sequence ? live : sum[0], share = over > 0 ? 1 / over : 0;
-  for (int64_t s = threadIdx.x / lanes; s < S; s += END_THREADS / lanes)
-    if (!lane) p.weight[s] = (float)(p.weight[s] * share);      // the thread that wrote it
+  group_sums<END_THREADS>(all, part);
   if (threadIdx.x == 0) {
-    const double policy = sum[1] * share, kl = sum[2] * share, entropy = sum[3] * share;
+    const double over = p.divisor > 0 ? p.divisor : p.by_sequence ? all[POLICY_SUMS] : all[0], share = over > 0 ? 1 / over : 0;
+    const double policy = all[1] * share, kl = all[2] * share, entropy = all[3] * share;
     p.out[0] = (float)(policy + (p.ref ? p.kl_coef * kl : 0) - (p.entropy ? p.entropy_coef * entropy : 0));
     p.out[1] = (float)policy;
     p.out[2] = (float)kl;
     p.out[3] = (float)entropy;
-    p.out[4] = (float)(sum[4] * share);
-    p.out[5] = (float)(sum[5] * share);
+    p.out[4] = (float)(all[4] * share);
+    p.out[5] = (float)(all[5] * share);
+    p.weight[S] = (float)share;
   }
 }
 
-__global__ __launch_bounds__(256) void k_policy_cells(PolicyParams p, int64_t cells) {
-  const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (i < cells) policy_cell(p, i);
+template <int SHIFT> __global__ __launch_bounds__(64 * GROUP) void k_policy_cells(PolicyParams p, int64_t cells) {
+  __shared__ CellSums<POLICY_SUMS, GROUP> s;
+  const int64_t i0 = (int64_t)blockIdx.x * GROUP, i = i0 + (threadIdx.x >> 6);
+  if (i < cells) policy_cell<SHIFT>(p, i, s);
+  leave(s, i0, cells, p.sums);
 }
-__global__ __launch_bounds__(END_THREADS) void k_policy_end(PolicyParams p) { policy_end(p); }
+template <int SHIFT> __global__ __launch_bounds__(END_THREADS) void k_policy_end(PolicyParams p) { policy_end<SHIFT, GROUP>(p, p.sums); }
+// All cells in one workgroup.
+__global__ __launch_bounds__(END_THREADS) void k_policy_small(PolicyParams p, int64_t cells) {
+  __shared__ CellSums<POLICY_SUMS, FEW> s;
+  __shared__ double sums[FEW * POLICY_SUMS];
+  const int64_t i = threadIdx.x >> 6;
+  if (i < cells) policy_cell<ONE>(p, i, s);
+  leave(s, 0, cells, sums);
+  __syncthreads();
+  policy_end<ONE, FEW>(p, sums);
+}
 
 __global__ __launch_bounds__(256) void k_policy_backward(PolicyParams p, int64_t cells) {
   const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (i >= cells) return;
-  const int lane = threadIdx.x & 63;
-  const Cell c = cell_at(p.q, i, LOSS_CELL);
+  const float all = p.weight[p.q.sequences] * *p.grad_loss;
+  const Span c = span_of<ONE>(p.q, i);
+  const int r = 4 * (threadIdx.x & 63);
   const float each = p.sequence_advantages && c.seq >= 0 ? p.advantages[c.seq] : 0.f;
-  const float w = c.seq >= 0 ? p.weight[c.seq] * *p.grad_loss : 0.f;
+  const float w = c.seq >= 0 ? p.weight[c.seq] * all : 0.f;
   const float kl_coef = (float)p.kl_coef, bonus = -(float)p.entropy_coef * w;
-#pragma unroll 2
-  for (int64_t t = c.begin + lane; t < c.end; t += 64) {
-    const bool on = !p.q.mask || p.q.mask[t];
-    const Token x = policy_token(p, p.logp[t], p.old ? p.old[t] : 0.f, p.ref ? p.ref[t] : 0.f,
-                                 p.sequence_advantages ? each : p.advantages[t]);
-    p.grad_logp[t] = on ? (x.slope + (p.ref ? kl_coef * x.dkl : 0.f)) * w : 0.f;
-    if (p.grad_entropy) p.grad_entropy[t] = on ? bonus : 0.f;
-  }
-  auto clear = [&](int64_t from, int64_t to) {
-    for (int64_t t = from + lane; t < to; t += 64) {
-      p.grad_logp[t] = 0.f;
-      if (p.grad_entropy) p.grad_entropy[t] = 0.f;
+  const int in = inside4(c, r);
+  float g[4] = {}, h[4] = {};
+  if (in) {
+    Four x;
+    const uint32_t mask = mask4(p.q, c, r);
+    fetch(p, c, r, each, x);
+    const int on = live4(in, mask);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const Token y = policy_token(p, x.logp[j], x.old[j], x.ref[j], x.a[j]);
+      const bool live = on >> j & 1;
+      g[j] = live ? (y.slope + (p.ref ? kl_coef * y.dkl : 0.f)) * w : 0.f;
+      h[j] = live ? bonus : 0.f;
     }
-  };
-  clear(c.fill0, c.fill1);
-  clear(c.fill2, c.fill3);
+  }
+  store4(p.grad_logp, c, r, g);
+  if (p.grad_entropy) store4(p.grad_entropy, c, r, h);
 }
 
 }  // namespace
 
-#define ON_CELLS(kernel, q, st, ...)                                                                                   \
-  do {                                                                                                                 \
-    const int64_t cells = cells_of_all(q, LOSS_CELL);                                                                  \
-    if (cells > 0) hipLaunchKernelGGL(kernel, dim3((uint32_t)((cells + 3) / 4)), dim3(256), 0, st, __VA_ARGS__, cells); \
+#define ON_CELLS(kernel, st, ...) \
+  hipLaunchKernelGGL(kernel, dim3((uint32_t)((cells + 3) / 4)), dim3(256), 0, st, __VA_ARGS__, cells)
+// Both steps of a forward pass over cells of 2^SHIFT tokens: two launches, or one where there are few cells.
+#define FORWARD(name, SHIFT)                                                                                \
+  do {                                                                                                      \
+    const int64_t cells = cells_of_all(p.q, SHIFT);                                                         \
+    if (SHIFT == ONE && cells <= FEW)   {                                                                   \
+      hipLaunchKernelGGL(k_##name##_small, dim3(1), dim3(END_THREADS), 0, st, p, cells);                    \
+      return hipGetLastError();                                                                             \
+    }                                                                                                       \
+    hipLaunchKernelGGL(k_##name##_cells<SHIFT>, dim3((uint32_t)((cells + GROUP - 1) / GROUP)), dim3(64 * GROUP), 0, st, p, \
+                       cells);                                                                              \
+    const hipError_t e = hipGetLastError();                                                                 \
+    if (e != hipSuccess) return e;                                                                          \
+    hipLaunchKernelGGL(k_##name##_end<SHIFT>, dim3(1), dim3(END_THREADS), 0, st, p);                        \
+    return hipGetLastError();                                                                               \
   } while (0)
 
 hipError_t launch_preference(const PreferenceParams& p, hipStream_t st) {
-  ON_CELLS(k_preference_cells, p.q, st, p);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_preference_end, dim3(1), dim3(END_THREADS), 0, st, p);
-  return hipGetLastError();
+  if (p.q.tokens > LOSS_FEW_TOKENS) FORWARD(preference, LOSS_CELL_SHIFT); else FORWARD(preference, ONE);
 }
 hipError_t launch_preference_backward(const Packed& q, const float* slope, const float* grad_loss, float* grad, hipStream_t st) {
-  ON_CELLS(k_preference_backward, q, st, q, slope, grad_loss, grad);
+  const int64_t cells = cells_of_all(q, ONE);
+  ON_CELLS(k_preference_backward, st, q, slope, grad_loss, grad);
   return hipGetLastError();
 }
 hipError_t launch_policy(const PolicyParams& p, hipStream_t st) {
-  ON_CELLS(k_policy_cells, p.q, st, p);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_policy_end, dim3(1), dim3(END_THREADS), 0, st, p);
-  return hipGetLastError();
+  if (p.q.tokens > LOSS_FEW_TOKENS) FORWARD(policy, LOSS_CELL_SHIFT); else FORWARD(policy, ONE);
 }
 hipError_t launch_policy_backward(const PolicyParams& p, hipStream_t st) {
-  ON_CELLS(k_policy_backward, p.q, st, p);
+  const int64_t cells = cells_of_all(p.q, ONE);
+  ON_CELLS(k_policy_backward, st, p);
   return hipGetLastError();
 }

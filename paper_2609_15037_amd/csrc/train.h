@@ -101,10 +101,11 @@ struct Packed {
   const uint8_t* mask;
   int64_t tokens, sequences, length;
 };
-// Sequences and tiles of CELL tokens cut the tokens into cells. Along the tokens either the sequence or the tile
+// Sequences and tiles of 512 (or 256) tokens cut the tokens into cells. Along the tokens either the sequence or the tile
 // advances, so sequence + tile numbers the cells: at most sequences + tiles - 1 of them.
-constexpr int LOSS_CELL = 1024;
-constexpr int64_t MAX_LOSS_TOKENS = (int64_t)1 << 33, MAX_SEQUENCES = (int64_t)1 << 22;
+constexpr int LOSS_CELL_SHIFT = 9;
+constexpr int64_t LOSS_FEW_TOKENS = 1 << 16;   // up to these tiles of 256
+constexpr int64_t MAX_LOSS_TOKENS = (int64_t)1 << 33, MAX_SEQUENCES = (int64_t)1 << 21;
 struct PreferenceParams {
   Packed q;
   const float *logp, *ref;
@@ -147,6 +148,6 @@ struct BalanceParams {
   const float* grad_loss;
   void* grad;
 };
-constexpr int BALANCE_LEAST_TILE = 32;
+constexpr int BALANCE_LEAST_SHIFT = 5;
 hipError_t launch_balance(const BalanceParams& p, hipStream_t st);
 hipError_t launch_balance_backward(const BalanceParams& p, hipStream_t st);

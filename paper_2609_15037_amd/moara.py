@@ -877,7 +877,7 @@ def _like(t, logp, dev, what: str):
 
 def _loss_workspace(logp, tokens: int, sequences: int):
     import torch
-    return torch.empty(7 * (max(sequences, 0) + tokens // 1024 + 2), dtype=torch.float64, device=logp.device)
+    return torch.empty(6 * (max(sequences, 0) + tokens // 512 + 130), dtype=torch.float64, device=logp.device)
 
 
 def moara_preference_default_config(**overrides) -> moara_preference_config:
@@ -899,7 +899,7 @@ def moara_preference_loss(cfg: moara_preference_config, logp, ref_logp=None, off
     ref = _like(ref_logp, logp, dev, "ref_logp")
     out = logp.new_empty(3)
     rewards = logp.new_empty(max(n, 0))
-    slope = torch.empty_like(rewards)
+    slope = logp.new_empty(max(n, 0) + 1)
     workspace = _loss_workspace(logp, tokens, n)
     _call(dev, lib().moara_preference_loss, cfg, at, ref, m, tokens, o, n, out.data_ptr(), rewards.data_ptr(), slope.data_ptr(),
           workspace.data_ptr())
@@ -912,7 +912,7 @@ def moara_preference_loss_backward(cfg: moara_preference_config, logp, slope, gr
     a float32 tensor of one element on the GPU; the others as they were."""
     import torch
     dev, tokens, _, m, o, n = _packed(logp, offsets, mask)
-    s, g = _vector(slope, dev, torch.float32, n, "slope"), _vector(grad_loss, dev, torch.float32, 1, "grad_loss")
+    s, g = _vector(slope, dev, torch.float32, n + 1, "slope"), _vector(grad_loss, dev, torch.float32, 1, "grad_loss")
     grad = torch.empty_like(logp)
     _call(dev, lib().moara_preference_loss_backward, s, g, m, tokens, o, n, grad.data_ptr())
     return grad
@@ -944,7 +944,7 @@ def moara_policy_loss(cfg: moara_policy_config, logp, advantages, old_logp=None,
     old, ref, bits = (_like(t, logp, dev, w) for t, w in ((old_logp, "old_logp"), (ref_logp, "ref_logp"), (entropy, "entropy")))
     a = _advantages(cfg, advantages, logp, n, dev)
     out = logp.new_empty(6)
-    weight = logp.new_empty(max(n, 0))
+    weight = logp.new_empty(max(n, 0) + 1)
     workspace = _loss_workspace(logp, tokens, n)
     _call(dev, lib().moara_policy_loss, cfg, at, old, ref, bits, a, m, tokens, o, n, out.data_ptr(), weight.data_ptr(),
           workspace.data_ptr())
@@ -960,7 +960,7 @@ def moara_policy_loss_backward(cfg: moara_policy_config, logp, advantages, weigh
     dev, tokens, at, m, o, n = _packed(logp, offsets, mask)
     old, ref = _like(old_logp, logp, dev, "old_logp"), _like(ref_logp, logp, dev, "ref_logp")
     a = _advantages(cfg, advantages, logp, n, dev)
-    w, g = _vector(weight, dev, torch.float32, n, "weight"), _vector(grad_loss, dev, torch.float32, 1, "grad_loss")
+    w, g = _vector(weight, dev, torch.float32, n + 1, "weight"), _vector(grad_loss, dev, torch.float32, 1, "grad_loss")
     grad = torch.empty_like(logp)
     bits = None if entropy is None else torch.empty_like(logp)
     _call(dev, lib().moara_policy_loss_backward, cfg, at, old, ref, a, m, tokens, o, n, w, g, grad.data_ptr(),

@@ -59,7 +59,7 @@ def test_logps_outputs_are_refused(lib):
 
 
 PACKED = [(dict(tokens=-1), SHAPE), (dict(tokens=(1 << 33) + 1, sequences=1), SHAPE), (dict(sequences=0), SHAPE),
-          (dict(sequences=-2), SHAPE), (dict(sequences=(1 << 22) + 2), SHAPE), (dict(tokens=9), SHAPE), (dict(offsets=P + 4), ARG)]
+          (dict(sequences=-2), SHAPE), (dict(sequences=(1 << 21) + 2), SHAPE), (dict(tokens=9), SHAPE), (dict(offsets=P + 4), ARG)]
 
 
 @pytest.mark.parametrize("kw,status", PACKED + [
