@@ -522,8 +522,9 @@ int moara_token_logps_backward(const void* logits, int32_t logits_dtype, int64_t
                                int64_t grad_stride, void* stream);
 
 /* Bytes of the workspace of moara_preference_loss and moara_policy_loss: device memory, 8-byte
- * aligned, of any contents, for one call at a time. */
-#define MOARA_LOSS_WORKSPACE(tokens, sequences) (48 * ((sequences) + (tokens) / 512 + 130))
+ * aligned, of any contents, for one call at a time. 0 for a few tokens: it may be null. */
+#define MOARA_LOSS_WORKSPACE(tokens, sequences) \
+  ((sequences) + ((tokens) + 255) / 256 <= 17 ? 0 : 48 * ((sequences) + (tokens) / 512 + 130))
 
 enum { MOARA_PREF_SIGMOID = 0, MOARA_PREF_HINGE = 1, MOARA_PREF_SQUARE = 2 };
 

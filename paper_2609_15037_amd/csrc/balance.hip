@@ -26,10 +26,11 @@ __device__ __forceinline__ double* about_sequences(const BalanceParams& p, int64
 
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
 
-// A token's scores s (of a sigmoid over their sum, which exists where they underflow); for the gradient w = s times 1 -
-// sigmoid, or s; with z the softmax and the logits' log-sum-exp. False where it has no scores.
+// A token's scores s[j] y, as parts of their sum (of a sigmoid too, which so exist where they underflow); for the gradient
+// w = 1 - sigmoid; with z the softmax and the logits' log-sum-exp. False where it has no scores.
 template <int LANES, int V, bool SIGMOID, bool Z, bool BACKWARD>
-__device__ __forceinline__ bool token_scores(const float (&l)[V], float (&s)[V], float (&w)[V], float (&soft)[V], float& lse) {
+__device__ __forceinline__ bool token_scores(const float (&l)[V], float (&s)[V], float& y, float (&w)[V], float (&soft)[V],
+                                             float& lse) {
   float top = 0, sum = 0;
   auto find_top = [&] {
     top = l[0];
@@ -39,62 +40,53 @@ __device__ __forceinline__ bool token_scores(const float (&l)[V], float (&s)[V],
   };
   if (Z || !SIGMOID) find_top();
   lse = 0;
-  if (SIGMOID) {
-    // e^min(l, 0) / (1 + e^-|l|): e^min(l, 0) is the other exponential or 1
+  if (!SIGMOID) {
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const float q = exp_of(-fabsf(l[j])), r = __builtin_amdgcn_rcpf(1.f + q);
-      const float low = q * r;
-      s[j] = l[j] < 0 ? low : r;
-      if (BACKWARD) w[j] = l[j] < 0 ? r : low;
+      s[j] = exp_of(l[j] - top);
       sum += s[j];
     }
     sum = sum_of<LANES>(sum);
-    if (!(sum > 0x1p-30f)) {            // where they are small, or underflow, their quotients from the logits less the largest
-      if (!Z) find_top();
-      const float shift = fminf(top, 0.f);
-      sum = 0;
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const float q = exp_of(-fabsf(l[j])), r = __builtin_amdgcn_rcpf(1.f + q);
-        s[j] = exp_of(fminf(l[j], 0.f) - shift) * r;
-        if (BACKWARD) w[j] = l[j] < 0 ? r : q * r;
-        sum += s[j];
-      }
-      sum = sum_of<LANES>(sum);
-    }
-    const float y = __builtin_amdgcn_rcpf(sum);
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      s[j] *= y;
-      if (BACKWARD) w[j] *= s[j];
-    }
-    if (Z) {
-      float total = 0;
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        soft[j] = exp_of(l[j] - top);
-        total += soft[j];
-      }
-      total = sum_of<LANES>(total);
-      lse = top + logf(total);
-      const float v = __builtin_amdgcn_rcpf(total);
-#pragma unroll
-      for (int j = 0; j < V; ++j) soft[j] *= v;
-    }
-    return sum > 0;                     // not NaN, not a row of -infinity
+    y = __builtin_amdgcn_rcpf(sum);
+    if (Z) lse = top + logf(sum);
+    return sum > 0;                     // not NaN: a row of -infinity, one with a NaN or +infinity
   }
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    s[j] = exp_of(l[j] - top);
+  for (int j = 0; j < V; ++j) {         // 1 / (1 + q), and q / (1 + q); q may overflow where the score is 0
+    const float q = exp_of(-l[j]);
+    s[j] = __builtin_amdgcn_rcpf(1.f + q);
+    if (BACKWARD) w[j] = fminf(q, 0x1p126f) * s[j];
     sum += s[j];
   }
   sum = sum_of<LANES>(sum);
-  const float y = __builtin_amdgcn_rcpf(sum);
+  if (!(sum > 0x1p-30f)) {              // small ones, or none: their quotients from the logits less the largest
+    if (!Z) find_top();
+    const float shift = fminf(top, 0.f);
+    sum = 0;
 #pragma unroll
-  for (int j = 0; j < V; ++j) s[j] *= y;
-  if (Z) lse = top + logf(sum);
-  return sum > 0;                       // not NaN: a row of -infinity, one with a NaN or +infinity
+    for (int j = 0; j < V; ++j) {
+      const float q = exp_of(-fabsf(l[j])), r = __builtin_amdgcn_rcpf(1.f + q);
+      s[j] = exp_of(fminf(l[j], 0.f) - shift) * r;
+      if (BACKWARD) w[j] = l[j] < 0 ? r : q * r;
+      sum += s[j];
+    }
+    sum = sum_of<LANES>(sum);
+  }
+  y = __builtin_amdgcn_rcpf(sum);
+  if (Z) {
+    float total = 0;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      soft[j] = exp_of(l[j] - top);
+      total += soft[j];
+    }
+    total = sum_of<LANES>(total);
+    lse = top + logf(total);
+    const float v = __builtin_amdgcn_rcpf(total);
+#pragma unroll
+    for (int j = 0; j < V; ++j) soft[j] *= v;
+  }
+  return sum > 0;                       // not NaN, not a row of -infinity
 }
 
 template <int LANES, int V> __device__ __forceinline__ void fetch(const BalanceParams& p, int64_t t, int lane, float (&l)[V]) {
@@ -137,16 +129,17 @@ template <int LANES, int V, bool SIGMOID, bool Z> struct Sums {
     for (int64_t t = begin + slot; t < end; t += TOK) {
       const bool live = !p.q.mask || p.q.mask[t];
       int e = lane < p.k ? p.index[t * p.k + lane] : -1;
-      float s[V], w[V], soft[V], lse;
-      const bool on = token_scores<LANES, V, SIGMOID, Z, false>(l, s, w, soft, lse) && live;
+      float s[V], y, w[V], soft[V], lse;
+      const bool on = token_scores<LANES, V, SIGMOID, Z, false>(l, s, y, w, soft, lse) && live;
       if (t + TOK < end) fetch<LANES, V>(p, t + TOK, lane, l);
+      if (!on) continue;
 #pragma unroll
-      for (int j = 0; j < V; ++j) sum[j] += on ? s[j] : 0.f;
-      if (on && lane == 0) {
+      for (int j = 0; j < V; ++j) sum[j] = fmaf(s[j], y, sum[j]);
+      if (lane == 0) {
         about[0] += (double)lse * (double)lse;
         about[1] += 1;
       }
-      for (int j = lane; on && j < p.k; j += LANES) {
+      for (int j = lane; j < p.k; j += LANES) {
         if (j != lane) e = p.index[t * p.k + j];
         if (e >= 0 && e < p.E) atomicAdd(&hist[e], 1u);
       }
@@ -300,21 +293,21 @@ __global__ __launch_bounds__(BACKWARD_THREADS) void k_balance_backward(BalancePa
   }
   for (int64_t t = c.begin + slot; t < c.end; t += TOK) {
     const bool live = !p.q.mask || p.q.mask[t];
-    float s[V], w[V], soft[V], lse;
-    const bool on = token_scores<LANES, V, SIGMOID, Z, true>(l, s, w, soft, lse) && live;
+    float s[V], y, w[V], soft[V], lse;
+    const bool on = token_scores<LANES, V, SIGMOID, Z, true>(l, s, y, w, soft, lse) && live;
     if (t + TOK < c.end) fetch<LANES, V>(p, t + TOK, lane, l);
     float mean = 0;
 #pragma unroll
     for (int j = 0; j < V; ++j) mean = fmaf(f[j], s[j], mean);
-    mean = sum_of<LANES>(mean);
+    mean = sum_of<LANES>(mean) * y;
     const float zl = b * lse;
 #pragma unroll
     for (int j = 0; j < V; j += 4) {
       float x[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float d = (SIGMOID ? w[j + i] : s[j + i]) * (f[j + i] - mean);
-        if (Z) d = fmaf(zl, SIGMOID ? soft[j + i] : s[j + i], d);
+        float d = (f[j + i] - mean) * (SIGMOID ? w[j + i] * y : y) * s[j + i];
+        if (Z) d = fmaf(zl, SIGMOID ? soft[j + i] : s[j + i] * y, d);
         x[i] = on ? d : 0.f;
       }
       const int e = expert_of<LANES>(j, lane);

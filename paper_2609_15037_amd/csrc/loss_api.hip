@@ -184,7 +184,8 @@ int moara_preference_loss(const moara_preference_config* cfg, const float* logp,
   if (rc == MOARA_OK) rc = check_preference(p.q);
   if (rc != MOARA_OK) return rc;
   if (tokens > 0 && !logp) return moara_fail(MOARA_E_ARG, "null logp");
-  if (!out || !out_rewards || !out_slope || !workspace) return moara_fail(MOARA_E_ARG, "null output or workspace");
+  if (!out || !out_rewards || !out_slope || (!workspace && MOARA_LOSS_WORKSPACE(tokens, sequences) > 0))
+    return moara_fail(MOARA_E_ARG, "null output or workspace");
   if (misaligned(logp, 4) || misaligned(ref_logp, 4) || misaligned(out, 4) || misaligned(out_rewards, 4) ||
       misaligned(out_slope, 4) || misaligned(workspace, 8))
     return moara_fail(MOARA_E_ARG, "pointer not aligned");
@@ -229,7 +230,8 @@ int moara_policy_loss(const moara_policy_config* cfg, const float* logp, const f
   const int rc = check_policy(cfg, p, logp, old_logp, ref_logp, advantages, mask, tokens, offsets, sequences);
   if (rc != MOARA_OK) return rc;
   if (tokens > 0 && cfg->entropy_coef != 0 && !entropy) return moara_fail(MOARA_E_ARG, "an entropy term needs entropy");
-  if (!out || !out_weight || !workspace) return moara_fail(MOARA_E_ARG, "null output or workspace");
+  if (!out || !out_weight || (!workspace && MOARA_LOSS_WORKSPACE(tokens, sequences) > 0))
+    return moara_fail(MOARA_E_ARG, "null output or workspace");
   if (misaligned(entropy, 4) || misaligned(out, 4) || misaligned(out_weight, 4) || misaligned(workspace, 8))
     return moara_fail(MOARA_E_ARG, "pointer not aligned");
   p.entropy = entropy;

@@ -876,8 +876,11 @@ def _like(t, logp, dev, what: str):
 
 
 def _loss_workspace(logp, tokens: int, sequences: int):
+    """The workspace of MOARA_LOSS_WORKSPACE's bytes; None where a call needs none."""
     import torch
-    return torch.empty(6 * (max(sequences, 0) + tokens // 512 + 130), dtype=torch.float64, device=logp.device)
+    if sequences + (tokens + 255) // 256 <= 17:
+        return None
+    return logp.new_empty(6 * (sequences + tokens // 512 + 130), dtype=torch.float64)
 
 
 def moara_preference_default_config(**overrides) -> moara_preference_config:
@@ -902,7 +905,7 @@ def moara_preference_loss(cfg: moara_preference_config, logp, ref_logp=None, off
     slope = logp.new_empty(max(n, 0) + 1)
     workspace = _loss_workspace(logp, tokens, n)
     _call(dev, lib().moara_preference_loss, cfg, at, ref, m, tokens, o, n, out.data_ptr(), rewards.data_ptr(), slope.data_ptr(),
-          workspace.data_ptr())
+          None if workspace is None else workspace.data_ptr())
     return out, rewards, slope
 
 
@@ -947,7 +950,7 @@ def moara_policy_loss(cfg: moara_policy_config, logp, advantages, old_logp=None,
     weight = logp.new_empty(max(n, 0) + 1)
     workspace = _loss_workspace(logp, tokens, n)
     _call(dev, lib().moara_policy_loss, cfg, at, old, ref, bits, a, m, tokens, o, n, out.data_ptr(), weight.data_ptr(),
-          workspace.data_ptr())
+          None if workspace is None else workspace.data_ptr())
     return out, weight
 
 

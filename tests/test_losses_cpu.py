@@ -64,7 +64,7 @@ PACKED = [(dict(tokens=-1), SHAPE), (dict(tokens=(1 << 33) + 1, sequences=1), SH
 
 @pytest.mark.parametrize("kw,status", PACKED + [
     (dict(sequences=3, tokens=9), SHAPE), (dict(logp=None), ARG), (dict(logp=P + 1), ARG), (dict(ref=P + 2), ARG),
-    (dict(out=None), ARG), (dict(rewards=None), ARG), (dict(slope=None), ARG), (dict(work=None), ARG), (dict(work=P + 4), ARG),
+    (dict(out=None), ARG), (dict(rewards=None), ARG), (dict(slope=None), ARG), (dict(work=None, tokens=8000), ARG), (dict(work=P + 4), ARG),
     (dict(beta=0.0), ARG), (dict(beta=-1.0), ARG), (dict(beta=math.inf), ARG), (dict(margin=math.nan), ARG), (dict(kind=3), ARG),
     (dict(kind=-1), ARG), (dict(smoothing=1.5), ARG), (dict(smoothing=-0.1), ARG), (dict(smoothing=0.1, kind=1), ARG),
     (dict(margin=0.5, kind=2), ARG)])
@@ -86,7 +86,7 @@ def test_preference_backward_arguments_are_refused(lib):
 
 @pytest.mark.parametrize("kw,status", PACKED + [
     (dict(logp=None), ARG), (dict(adv=None), ARG), (dict(logp=P + 1), ARG), (dict(old=P + 2), ARG), (dict(ref=P + 2), ARG),
-    (dict(adv=P + 2), ARG), (dict(entropy=P + 2), ARG), (dict(out=None), ARG), (dict(weight=None), ARG), (dict(work=None), ARG),
+    (dict(adv=P + 2), ARG), (dict(entropy=P + 2), ARG), (dict(out=None), ARG), (dict(weight=None), ARG), (dict(work=None, tokens=8000), ARG),
     (dict(work=P + 4), ARG), (dict(clip_low=-0.1), ARG), (dict(clip_low=1.1), ARG), (dict(clip_high=-0.1), ARG),
     (dict(clip_high=math.nan), ARG), (dict(kl_coef=0.1, ref=None), ARG), (dict(entropy_coef=0.1, entropy=None), ARG),
     (dict(kl_coef=math.inf), ARG), (dict(entropy_coef=math.nan), ARG), (dict(divisor=-1.0), ARG), (dict(divisor=math.inf), ARG),
