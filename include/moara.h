@@ -615,7 +615,7 @@ int moara_balance_default_config(moara_balance_config* out);
 
 /* Bytes of the workspace of moara_balance_loss: device memory, 8-byte aligned, of any contents, for
  * one call at a time. */
-#define MOARA_BALANCE_WORKSPACE(experts, tokens, sequences) ((8 * (experts) + 64) * ((sequences) + (tokens) / 32 + 2))
+#define MOARA_BALANCE_WORKSPACE(experts, tokens, sequences) ((8 * (experts) + 64) * (2 * (sequences) + (tokens) / 32 + 2))
 
 /* Load-balancing loss of routed tokens. For each sequence with tokens, c_e the number of its tokens that
  * index gives to expert e, f_e = E c_e / sum_e c_e (0 where nothing is given), P_e the mean of its tokens'

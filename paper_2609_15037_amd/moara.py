@@ -1017,7 +1017,7 @@ def moara_balance_loss(cfg: moara_balance_config, logits, index, offsets=None, m
     out = logits.new_empty(3, dtype=torch.float32)
     counts = out.new_empty((s, E), dtype=torch.int64)
     slope = out.new_empty(s * E + 2)
-    workspace = out.new_empty((E + 8) * (s + tokens // 32 + 2), dtype=torch.float64)
+    workspace = out.new_empty((E + 8) * (2 * s + tokens // 32 + 2), dtype=torch.float64)
     _call(dev, lib().moara_balance_loss, cfg, logits.data_ptr(), tokens, ld, i, m, o, n, load, out.data_ptr(), counts.data_ptr(),
           slope.data_ptr(), workspace.data_ptr())
     return out, counts, slope
