@@ -2,7 +2,7 @@
 a training step: expert routing, MoARa on the projection and expert matrices, AdamW with 8-bit moments on
 the embedding, norms, head and routers, clipping by the norm of all gradients.
 
-    python examples/train_moe.py [--steps 40] [--bits 8|32]
+    python examples/train_moe.py [--steps 40] [--bits 8|32] [--balance-loss 0.01]
 """
 import argparse
 import os
@@ -43,10 +43,13 @@ class Layer(torch.nn.Module):
         y = F.scaled_dot_product_attention(q, k, v, is_causal=True)
         return self.o_proj(y.transpose(1, 2).reshape(b, t, d))
 
-    def mixture(self, x):
-        """Every token's experts on its row, weighted; experts without tokens are not called."""
+    def mixture(self, x, balance=None, losses=None):
+        """Every token's experts on its row, weighted; experts without tokens are not called. With the configuration of a
+        balance loss, the layer's is appended to `losses`."""
         rows = x.reshape(-1, x.shape[-1])
-        index, weight = self.router(rows)
+        index, weight, *loss = self.router(rows, balance=balance)
+        if losses is not None:
+            losses += loss
         out = torch.zeros_like(rows)
         for e in index[index >= 0].unique().tolist():
             token, slot = (index == e).nonzero(as_tuple=True)
@@ -54,9 +57,9 @@ class Layer(torch.nn.Module):
             out = out.index_add(0, token, y)
         return out.view_as(x)
 
-    def forward(self, x):
+    def forward(self, x, balance=None, losses=None):
         x = x + self.attention(self.norm1(x))
-        return x + self.mixture(self.norm2(x))
+        return x + self.mixture(self.norm2(x), balance, losses)
 
 
 class Model(torch.nn.Module):
@@ -67,16 +70,16 @@ class Model(torch.nn.Module):
         self.norm = torch.nn.RMSNorm(d)
         self.head = torch.nn.Linear(d, vocab, bias=False)
 
-    def forward(self, tokens):
+    def forward(self, tokens, balance=None, losses=None):
         x = self.embed(tokens)
         for layer in self.layers:
-            x = layer(x)
+            x = layer(x, balance, losses)
         return self.head(self.norm(x))
 
 
-def train(steps=40, bits=8, seed=0, rate=1e-2, say=print):
+def train(steps=40, bits=8, seed=0, rate=1e-2, say=print, balance_loss=0.0):
     """Losses of the steps and the largest share of the tokens an expert had in the last one (layer by layer).
-    rate: of the balancing bias."""
+    rate: of the balancing bias; balance_loss: coefficient of the routers' balance loss beside it."""
     torch.manual_seed(seed)
     model = Model().cuda()
     targets, others = moara_targets(model)
@@ -87,9 +90,11 @@ def train(steps=40, bits=8, seed=0, rate=1e-2, say=print):
     tokens = torch.randint(0, 512, (8, 65), generator=torch.Generator().manual_seed(seed)).cuda()
     losses, share = [], []
     for step in range(steps):
-        logits = model(tokens[:, :-1])
+        aux = []
+        balance = model.layers[0].router.balance_config(balance_coef=balance_loss) if balance_loss else None
+        logits = model(tokens[:, :-1], balance, aux)
         loss = F.cross_entropy(logits.flatten(0, 1).float(), tokens[:, 1:].flatten())
-        loss.backward()
+        (sum(aux, loss) if aux else loss).backward()
         opt.step()
         sched.step()
         opt.zero_grad()
@@ -107,5 +112,6 @@ if __name__ == "__main__":
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--steps", type=int, default=40)
     ap.add_argument("--bits", type=int, choices=(8, 32), default=8)
+    ap.add_argument("--balance-loss", type=float, default=0.0)
     a = ap.parse_args()
-    train(a.steps, a.bits)
+    train(a.steps, a.bits, balance_loss=a.balance_loss)

@@ -245,7 +245,7 @@ __global__ __launch_bounds__(256) void k_logps_backward(LogpsParams p, uint32_t 
 // 369; where the logits alone would fit, gradients only: 16384 x 4096 fp32 80 and 94, with the logits past them too 86.
 constexpr double CACHE = 256 << 20;
 template <typename T> double bytes_of(const LogpsParams& p) { return (double)p.tokens * (double)p.vocab * sizeof(T); }
-constexpr int64_t MOST_GROUPS = 1 << 22;        // workgroups of a launch: fewer than 2^32 threads
+constexpr int64_t MOST_GROUPS = 1 << 21;        // workgroups of a launch: fewer than 2^32 threads
 
 template <typename T, int THREADS, int U, bool ONCE> void forward(const LogpsParams& p, hipStream_t st) {
   constexpr int block = THREADS < 256 ? 256 : THREADS, rows = block / THREADS;

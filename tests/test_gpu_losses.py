@@ -952,3 +952,66 @@ def test_a_router_with_a_balance_loss(score):
     torch.testing.assert_close(grad.cpu().double(), torch.autograd.grad(want, W)[0], rtol=1e-4, atol=1e-6)
     _, _, loss = r(x, balance=r.balance_config(), load=torch.arange(12, device="cuda"))
     loss.backward()
+
+
+# ---------------------------------------------------------------- the example
+
+def _align():
+    import importlib.util
+    import os
+    from tests.conftest import ROOT
+    spec = importlib.util.spec_from_file_location("align_moe", os.path.join(ROOT, "examples", "align_moe.py"))
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    return ex
+
+
+@pytest.mark.parametrize("name", ["preference", "policy"])
+def test_the_alignment_example(name):
+    """It runs, and the gradients of one of its batches are those of torch's own log-softmax and elementary operations on the
+    same model (its products in fp32, whose sums torch may take in any order from pass to pass)."""
+    ex = _align()
+    about = ex.train(name, steps=6, say=lambda s: print("[align]", s, flush=True))
+    assert about.shape == (6, 3 if name == "preference" else 6) and torch.isfinite(about).all()
+    torch.manual_seed(1)
+    model, reference = ex.Model().cuda(), ex.Model().cuda()
+    tokens, answer = ex.batch(6, torch.Generator().manual_seed(2))
+    with torch.no_grad():
+        old = ex.logps(model, tokens, answer) + 0.1 * torch.randn(answer.shape, device="cuda")
+        ref = ex.logps(reference, tokens, answer)
+    loss, _ = ex.objective(name, model, reference, old, tokens, answer)
+    loss.backward()
+    got = {n: None if p.grad is None else p.grad.clone() for n, p in model.named_parameters()}
+    model.zero_grad()
+    aux = []
+    logits = model(tokens, model.layers[0].router.balance_config(balance_coef=1e-2, z_coef=1e-4), aux)
+    log = torch.log_softmax(logits[:, :-1].double(), dim=-1)
+    logp = torch.where(answer, log.gather(2, tokens[:, 1:, None])[..., 0], 0.0)
+    if name == "preference":
+        d = (logp - ref).sum(dim=1)
+        want = torch.nn.functional.softplus(-0.2 * (d[0::2] - d[1::2])).mean()
+    else:
+        H = torch.where(answer, -(log.exp() * log).sum(dim=-1), 0.0)
+        even = ((tokens[:, 1:] % 2 == 0) & answer).sum(dim=1) / answer.sum(dim=1)
+        a = ((even - even.mean()) / (even.std() + 1e-6))[:, None]
+        r, q = (logp - old).exp(), ref - logp
+        each = -torch.minimum(r * a, r.clamp(0.8, 1.2) * a) + 0.02 * (q.expm1() - q) - 1e-3 * H
+        want = (each * answer).sum() / answer.sum()
+    want = want + sum(aux)
+    assert float(loss.detach()) == pytest.approx(float(want.detach()), rel=1e-4)
+    want.backward()
+    for n, p in model.named_parameters():
+        assert (p.grad is None) == (got[n] is None), n
+        if p.grad is not None:
+            torch.testing.assert_close(got[n], p.grad, rtol=2e-3, atol=2e-3 * float(p.grad.abs().max()) + 1e-8, msg=n)
+
+
+def test_the_training_example_with_a_balance_loss():
+    import importlib.util
+    import os
+    from tests.conftest import ROOT
+    spec = importlib.util.spec_from_file_location("train_moe", os.path.join(ROOT, "examples", "train_moe.py"))
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    losses, share = ex.train(steps=3, balance_loss=0.1, say=lambda s: print("[moe]", s, flush=True))
+    assert all(math.isfinite(x) for x in losses) and len(share) == 2
