@@ -491,6 +491,7 @@ int moara_route_balance(int32_t experts, int64_t* counts, float* bias, float rat
  * left out, as are tokens before the first and behind the last sequence: whatever values they
  * have, they add nothing, and their gradients are 0. What is outside [0, tokens) is never read
  * or written, whatever the offsets are; offsets that fall give sums of some of the tokens.
+ * out_loss: one float, or null: the loss, out[0], once more, for callers that keep it by itself.
  * ------------------------------------------------------------------------------------ */
 
 /* Log-probabilities of labels. With x = scale logits[t] and p = softmax(x):
@@ -553,8 +554,8 @@ int moara_preference_default_config(moara_preference_config* out);
  * Sums are 64 bits. Errors: MOARA_E_ARG, MOARA_E_SHAPE (an odd number of sequences, tokens no
  * multiple of them without offsets, over 2^33 tokens or 2^21 sequences), MOARA_E_HIP. */
 int moara_preference_loss(const moara_preference_config* cfg, const float* logp, const float* ref_logp, const uint8_t* mask,
-                          int64_t tokens, const int64_t* offsets, int64_t sequences, float* out, float* out_rewards,
-                          float* out_slope, void* workspace, void* stream);
+                          int64_t tokens, const int64_t* offsets, int64_t sequences, float* out, float* out_loss,
+                          float* out_rewards, float* out_slope, void* workspace, void* stream);
 
 /* out_grad[t] = *grad_loss slope[sequences] slope[sequence of t], 0 where t is left out. grad_loss: one
  * float of device memory, the gradient of out[0]. Errors as moara_preference_loss. */
@@ -592,8 +593,8 @@ int moara_policy_default_config(moara_policy_config* out);
  * Errors: MOARA_E_ARG, MOARA_E_SHAPE (as moara_preference_loss), MOARA_E_HIP. */
 int moara_policy_loss(const moara_policy_config* cfg, const float* logp, const float* old_logp, const float* ref_logp,
                       const float* entropy, const float* advantages, const uint8_t* mask, int64_t tokens,
-                      const int64_t* offsets, int64_t sequences, float* out, float* out_weight, void* workspace,
-                      void* stream);
+                      const int64_t* offsets, int64_t sequences, float* out, float* out_loss, float* out_weight,
+                      void* workspace, void* stream);
 
 /* Gradients of logp and (or null) of the entropies: *grad_loss times the derivatives of out[0], 0
  * where a token is left out. weight: as moara_policy_loss gave it. Errors as moara_policy_loss. */
@@ -634,7 +635,8 @@ int moara_balance_default_config(moara_balance_config* out);
  * overlapping rows), MOARA_E_UNSUPPORTED (over the limits above), MOARA_E_HIP. */
 int moara_balance_loss(const moara_balance_config* cfg, const void* logits, int64_t tokens, int64_t row_stride,
                        const int32_t* index, const uint8_t* mask, const int64_t* offsets, int64_t sequences,
-                       const int64_t* load, float* out, int64_t* out_counts, float* out_slope, void* workspace, void* stream);
+                       const int64_t* load, float* out, float* out_loss, int64_t* out_counts, float* out_slope, void* workspace,
+                       void* stream);
 
 /* Gradient of the logits (tokens x experts, contiguous, their type): *grad_loss times the derivative of
  * out[0], 0 where a token is left out. Errors as moara_balance_loss. */

@@ -181,7 +181,9 @@ __global__ __launch_bounds__(FORWARD_THREADS) void k_balance(BalanceParams p, in
 // out and the factors of the gradient, from the sums over the sequences.
 __device__ __forceinline__ void balance_out(const BalanceParams& p, double balance, double live, double z, double n) {
   const double each = live > 0 ? 1 / live : 0, per = n > 0 ? 1 / n : 0;
-  p.out[0] = (float)(p.balance_coef * balance * each + p.z_coef * z * per);
+  const float loss = (float)(p.balance_coef * balance * each + p.z_coef * z * per);
+  p.out[0] = loss;
+  if (p.loss) *p.loss = loss;
   p.out[1] = (float)(balance * each);
   p.out[2] = (float)(z * per);
   float* tail = p.slope + p.q.sequences * p.E;

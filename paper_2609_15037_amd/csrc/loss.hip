@@ -221,6 +221,7 @@ template <int SHIFT, int W> __device__ __forceinline__ void preference_end(const
     const double share = all[3] > 0 ? 1 / all[3] : 0;
 #pragma unroll
     for (int k = 0; k < 3; ++k) p.out[k] = (float)(all[k] * share);
+    if (p.loss) *p.loss = (float)(all[0] * share);
     p.slope[p.q.sequences] = (float)share;
   }
 }
@@ -383,7 +384,9 @@ template <int SHIFT, int W> __device__ __forceinline__ void policy_end(const Pol
   if (threadIdx.x == 0) {
     const double over = p.divisor > 0 ? p.divisor : p.by_sequence ? all[POLICY_SUMS] : all[0], share = over > 0 ? 1 / over : 0;
     const double policy = all[1] * share, kl = all[2] * share, entropy = all[3] * share;
-    p.out[0] = (float)(policy + (p.ref ? p.kl_coef * kl : 0) - (p.entropy ? p.entropy_coef * entropy : 0));
+    const float loss = (float)(policy + (p.ref ? p.kl_coef * kl : 0) - (p.entropy ? p.entropy_coef * entropy : 0));
+    p.out[0] = loss;
+    if (p.loss) *p.loss = loss;
     p.out[1] = (float)policy;
     p.out[2] = (float)kl;
     p.out[3] = (float)entropy;

@@ -170,8 +170,8 @@ int moara_preference_default_config(moara_preference_config* out) {
 }
 
 int moara_preference_loss(const moara_preference_config* cfg, const float* logp, const float* ref_logp, const uint8_t* mask,
-                          int64_t tokens, const int64_t* offsets, int64_t sequences, float* out, float* out_rewards,
-                          float* out_slope, void* workspace, void* stream) {
+                          int64_t tokens, const int64_t* offsets, int64_t sequences, float* out, float* out_loss,
+                          float* out_rewards, float* out_slope, void* workspace, void* stream) {
   if (!cfg) return moara_fail(MOARA_E_ARG, "null config");
   if (!(cfg->beta > 0) || !isfinite(cfg->beta)) return moara_fail(MOARA_E_ARG, "beta must be positive");
   if (cfg->kind < MOARA_PREF_SIGMOID || cfg->kind > MOARA_PREF_SQUARE) return moara_fail(MOARA_E_ARG, "bad kind");
@@ -186,7 +186,7 @@ int moara_preference_loss(const moara_preference_config* cfg, const float* logp,
   if (tokens > 0 && !logp) return moara_fail(MOARA_E_ARG, "null logp");
   if (!out || !out_rewards || !out_slope || (!workspace && MOARA_LOSS_WORKSPACE(tokens, sequences) > 0))
     return moara_fail(MOARA_E_ARG, "null output or workspace");
-  if (misaligned(logp, 4) || misaligned(ref_logp, 4) || misaligned(out, 4) || misaligned(out_rewards, 4) ||
+  if (misaligned(logp, 4) || misaligned(ref_logp, 4) || misaligned(out, 4) || misaligned(out_loss, 4) || misaligned(out_rewards, 4) ||
       misaligned(out_slope, 4) || misaligned(workspace, 8))
     return moara_fail(MOARA_E_ARG, "pointer not aligned");
   p.logp = logp;
@@ -197,6 +197,7 @@ int moara_preference_loss(const moara_preference_config* cfg, const float* logp,
   p.kind = cfg->kind;
   p.average = cfg->average != 0;
   p.out = out;
+  p.loss = out_loss;
   p.rewards = out_rewards;
   p.slope = out_slope;
   p.sums = (double*)workspace;
@@ -224,18 +225,19 @@ int moara_policy_default_config(moara_policy_config* out) {
 
 int moara_policy_loss(const moara_policy_config* cfg, const float* logp, const float* old_logp, const float* ref_logp,
                       const float* entropy, const float* advantages, const uint8_t* mask, int64_t tokens,
-                      const int64_t* offsets, int64_t sequences, float* out, float* out_weight, void* workspace,
-                      void* stream) {
+                      const int64_t* offsets, int64_t sequences, float* out, float* out_loss, float* out_weight,
+                      void* workspace, void* stream) {
   PolicyParams p;
   const int rc = check_policy(cfg, p, logp, old_logp, ref_logp, advantages, mask, tokens, offsets, sequences);
   if (rc != MOARA_OK) return rc;
   if (tokens > 0 && cfg->entropy_coef != 0 && !entropy) return moara_fail(MOARA_E_ARG, "an entropy term needs entropy");
   if (!out || !out_weight || (!workspace && MOARA_LOSS_WORKSPACE(tokens, sequences) > 0))
     return moara_fail(MOARA_E_ARG, "null output or workspace");
-  if (misaligned(entropy, 4) || misaligned(out, 4) || misaligned(out_weight, 4) || misaligned(workspace, 8))
+  if (misaligned(entropy, 4) || misaligned(out, 4) || misaligned(out_loss, 4) || misaligned(out_weight, 4) || misaligned(workspace, 8))
     return moara_fail(MOARA_E_ARG, "pointer not aligned");
   p.entropy = entropy;
   p.out = out;
+  p.loss = out_loss;
   p.weight = out_weight;
   p.sums = (double*)workspace;
   LOSS_TRY(launch_policy(p, (hipStream_t)stream));
@@ -268,18 +270,20 @@ int moara_balance_default_config(moara_balance_config* out) {
 
 int moara_balance_loss(const moara_balance_config* cfg, const void* logits, int64_t tokens, int64_t row_stride,
                        const int32_t* index, const uint8_t* mask, const int64_t* offsets, int64_t sequences,
-                       const int64_t* load, float* out, int64_t* out_counts, float* out_slope, void* workspace, void* stream) {
+                       const int64_t* load, float* out, float* out_loss, int64_t* out_counts, float* out_slope, void* workspace,
+                       void* stream) {
   BalanceParams p;
   const int rc = check_balance(cfg, p, logits, tokens, row_stride, mask, offsets, sequences);
   if (rc != MOARA_OK) return rc;
   if (tokens > 0 && !index) return moara_fail(MOARA_E_ARG, "null index");
   if (!out || !out_counts || !out_slope || !workspace) return moara_fail(MOARA_E_ARG, "null output or workspace");
-  if (misaligned(index, 4) || misaligned(load, 8) || misaligned(out, 4) || misaligned(out_counts, 8) ||
+  if (misaligned(index, 4) || misaligned(load, 8) || misaligned(out, 4) || misaligned(out_loss, 4) || misaligned(out_counts, 8) ||
       misaligned(out_slope, 4) || misaligned(workspace, 8))
     return moara_fail(MOARA_E_ARG, "pointer not aligned");
   p.index = index;
   p.load = load;
   p.out = out;
+  p.loss = out_loss;
   p.counts = (long long*)out_counts;
   p.slope = out_slope;
   p.workspace = workspace;

@@ -111,7 +111,7 @@ struct PreferenceParams {
   const float *logp, *ref;
   double beta, margin, smoothing;
   int kind, average;
-  float *out, *rewards, *slope;
+  float *out, *loss, *rewards, *slope;
   double* sums;                 // workspace: sum and number of a cell's tokens
 };
 hipError_t launch_preference(const PreferenceParams& p, hipStream_t st);
@@ -123,7 +123,7 @@ struct PolicyParams {
   float at_low, at_high;        // the bounds themselves
   double kl_coef, entropy_coef, divisor;
   int kl, by_sequence, sequence_advantages;
-  float *out, *weight;
+  float *out, *loss, *weight;
   double* sums;                 // workspace: a cell's number of tokens and five sums
   const float* grad_loss;
   float *grad_logp, *grad_entropy;
@@ -141,7 +141,7 @@ struct BalanceParams {
   const int64_t* load;
   int E, k, sigmoid, bf16, want_z;
   double balance_coef, z_coef;
-  float* out;
+  float *out, *loss;
   long long* counts;
   float* slope;
   void* workspace;

@@ -23,7 +23,11 @@ from . import moara as M
 
 def _plain(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
     """A tensor without a gradient, float32 and contiguous."""
-    return None if t is None else t.detach().float().contiguous()
+    return None if t is None else _rows(t.detach() if t.requires_grad else t)
+
+
+def _rows(t: torch.Tensor) -> torch.Tensor:
+    return t if t.dtype is torch.float32 and t.is_contiguous() else t.float().contiguous()
 
 
 class _TokenLogps(torch.autograd.Function):
@@ -56,7 +60,9 @@ def token_logps(logits: torch.Tensor, labels: torch.Tensor, temperature: float =
     if labels.shape != logits.shape[:-1]:
         raise ValueError(f"labels: shape {tuple(labels.shape)}, the logits have {tuple(logits.shape)}")
     flat = logits if logits.dim() in (2, 3) else logits.reshape(-1, logits.shape[-1])
-    at = labels.to(torch.int64).reshape(flat.shape[:-1]).contiguous()
+    at = labels
+    if at.dtype is not torch.int64 or flat is not logits or not at.is_contiguous():
+        at = at.to(torch.int64).reshape(flat.shape[:-1]).contiguous()
     out = _TokenLogps.apply(flat, at, 1.0 / temperature, entropy)
     if flat is logits:
         return out
@@ -67,11 +73,12 @@ class _Preference(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logp, cfg, ref_logp, offsets, mask):
         cfg = M.moara_preference_config.from_buffer_copy(cfg)       # the caller may change its own before the backward pass
-        out, rewards, slope = M.moara_preference_loss(cfg, logp, ref_logp, offsets=offsets, mask=mask)
+        loss = logp.new_empty(())           # by itself: callers may change it in place
+        out, rewards, slope = M.moara_preference_loss(cfg, logp, ref_logp, offsets=offsets, mask=mask, loss=loss)
         ctx.cfg = cfg
         ctx.save_for_backward(logp, slope, offsets, mask)
         ctx.mark_non_differentiable(rewards, out)
-        return out[0].clone(), rewards, out
+        return loss, rewards, out
 
     @staticmethod
     @torch.autograd.function.once_differentiable
@@ -87,19 +94,20 @@ def preference_loss(cfg: M.moara_preference_config, logp: torch.Tensor, ref_logp
     """(loss, rewards, about) of pairs of responses, sequences 2p (chosen) and 2p + 1 (rejected); differentiable in logp.
     rewards: one for each sequence; about: loss, share of the pairs with the chosen one ahead, mean difference of their
     rewards. logp, ref_logp, mask: sequences x length, or flat with offsets."""
-    return _Preference.apply(logp.float().contiguous(), cfg, _plain(ref_logp), offsets, mask)
+    return _Preference.apply(_rows(logp), cfg, _plain(ref_logp), offsets, mask)
 
 
 class _Policy(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logp, entropy, cfg, advantages, old_logp, ref_logp, offsets, mask):
         cfg = M.moara_policy_config.from_buffer_copy(cfg)
+        loss = logp.new_empty(())
         out, weight = M.moara_policy_loss(cfg, logp, advantages, old_logp=old_logp, ref_logp=ref_logp, entropy=entropy,
-                                          offsets=offsets, mask=mask)
+                                          offsets=offsets, mask=mask, loss=loss)
         ctx.cfg = cfg
         ctx.save_for_backward(logp, entropy, advantages, weight, old_logp, ref_logp, offsets, mask)
         ctx.mark_non_differentiable(out)
-        return out[0].clone(), out
+        return loss, out
 
     @staticmethod
     @torch.autograd.function.once_differentiable
@@ -120,20 +128,21 @@ def policy_loss(cfg: M.moara_policy_config, logp: torch.Tensor, advantages: torc
     reference, entropy, share of clipped tokens, distance to the old policy. logp, old_logp (None: the policy is the one
     that sampled), ref_logp, entropy, mask: sequences x length, or flat with offsets; advantages alike, or one for each
     sequence where cfg.sequence_advantages."""
-    entropy = None if entropy is None else entropy.float().contiguous()
-    return _Policy.apply(logp.float().contiguous(), entropy, cfg, _plain(advantages), _plain(old_logp), _plain(ref_logp),
-                         offsets, mask)
+    return _Policy.apply(_rows(logp), None if entropy is None else _rows(entropy), cfg, _plain(advantages), _plain(old_logp),
+                         _plain(ref_logp), offsets, mask)
 
 
 class _Balance(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, cfg, index, offsets, mask, load, sequences):
         cfg = M.moara_balance_config.from_buffer_copy(cfg)
-        out, counts, slope = M.moara_balance_loss(cfg, logits, index, offsets=offsets, mask=mask, load=load, sequences=sequences)
+        loss = logits.new_empty((), dtype=torch.float32)
+        out, counts, slope = M.moara_balance_loss(cfg, logits, index, offsets=offsets, mask=mask, load=load, sequences=sequences,
+                                                  loss=loss)
         ctx.cfg, ctx.sequences = cfg, sequences
         ctx.save_for_backward(logits, slope, offsets, mask)
         ctx.mark_non_differentiable(counts, out)
-        return out[0].clone(), counts, out
+        return loss, counts, out
 
     @staticmethod
     @torch.autograd.function.once_differentiable

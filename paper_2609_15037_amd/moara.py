@@ -171,14 +171,14 @@ def lib():
         "moara_token_logps_backward": (ctypes.c_int, [vp, i32, i64, i64, i64, i64, i64, ctypes.c_float, vp, vp, vp, vp, vp,
                                                       vp, i64, vp]),
         "moara_preference_default_config": (ctypes.c_int, [P(moara_preference_config)]),
-        "moara_preference_loss": (ctypes.c_int, [P(moara_preference_config), vp, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp]),
+        "moara_preference_loss": (ctypes.c_int, [P(moara_preference_config), vp, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp]),
         "moara_preference_loss_backward": (ctypes.c_int, [vp, vp, vp, i64, vp, i64, vp, vp]),
         "moara_policy_default_config": (ctypes.c_int, [P(moara_policy_config)]),
-        "moara_policy_loss": (ctypes.c_int, [P(moara_policy_config), vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, vp]),
+        "moara_policy_loss": (ctypes.c_int, [P(moara_policy_config), vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp]),
         "moara_policy_loss_backward": (ctypes.c_int, [P(moara_policy_config), vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp,
                                                       vp, vp]),
         "moara_balance_default_config": (ctypes.c_int, [P(moara_balance_config)]),
-        "moara_balance_loss": (ctypes.c_int, [P(moara_balance_config), vp, i64, i64, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp]),
+        "moara_balance_loss": (ctypes.c_int, [P(moara_balance_config), vp, i64, i64, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp]),
         "moara_balance_loss_backward": (ctypes.c_int, [P(moara_balance_config), vp, i64, i64, vp, vp, i64, vp, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
@@ -875,6 +875,12 @@ def _like(t, logp, dev, what: str):
     return _vector(t, dev, torch.float32, t.numel(), what)
 
 
+def _one(loss, dev: int):
+    """Address of the tensor that gets the loss by itself; None for None."""
+    import torch
+    return None if loss is None else _vector(loss, dev, torch.float32, 1, "loss")
+
+
 def _loss_workspace(logp, tokens: int, sequences: int):
     """The workspace of MOARA_LOSS_WORKSPACE's bytes; None where a call needs none."""
     import torch
@@ -892,11 +898,11 @@ def moara_preference_default_config(**overrides) -> moara_preference_config:
 
 
 @_streamed
-def moara_preference_loss(cfg: moara_preference_config, logp, ref_logp=None, offsets=None, mask=None):
+def moara_preference_loss(cfg: moara_preference_config, logp, ref_logp=None, offsets=None, mask=None, loss=None):
     """moara_preference_loss of the C ABI: (out, rewards, slope), float32; out: loss, share of the pairs with the chosen
     response ahead, mean of beta h; rewards: one for each sequence; slope is for the backward call. logp (and ref_logp):
     float32, sequences x length, or flat with offsets (int64, sequences + 1); sequences 2p and 2p + 1 are a pair, the
-    chosen one first. mask: bool or uint8, of logp's shape."""
+    chosen one first. mask: bool or uint8, of logp's shape. loss: a float32 tensor of one element that gets the loss too."""
     import torch
     dev, tokens, at, m, o, n = _packed(logp, offsets, mask)
     ref = _like(ref_logp, logp, dev, "ref_logp")
@@ -904,8 +910,8 @@ def moara_preference_loss(cfg: moara_preference_config, logp, ref_logp=None, off
     rewards = logp.new_empty(max(n, 0))
     slope = logp.new_empty(max(n, 0) + 1)
     workspace = _loss_workspace(logp, tokens, n)
-    _call(dev, lib().moara_preference_loss, cfg, at, ref, m, tokens, o, n, out.data_ptr(), rewards.data_ptr(), slope.data_ptr(),
-          None if workspace is None else workspace.data_ptr())
+    _call(dev, lib().moara_preference_loss, cfg, at, ref, m, tokens, o, n, out.data_ptr(), _one(loss, dev), rewards.data_ptr(),
+          slope.data_ptr(), None if workspace is None else workspace.data_ptr())
     return out, rewards, slope
 
 
@@ -938,19 +944,20 @@ def _advantages(cfg, advantages, logp, sequences: int, dev: int) -> int:
 
 @_streamed
 def moara_policy_loss(cfg: moara_policy_config, logp, advantages, old_logp=None, ref_logp=None, entropy=None, offsets=None,
-                      mask=None):
+                      mask=None, loss=None):
     """moara_policy_loss of the C ABI: (out, weight), float32; out: loss, policy term, distance to the reference, entropy,
     share of clipped tokens, distance to the old policy; weight is for the backward call. logp: float32, sequences x
     length, or flat with offsets (int64, sequences + 1); old_logp, ref_logp, entropy, mask (bool or uint8) of its shape or
-    None; advantages of its shape, or one for each sequence where cfg.sequence_advantages."""
+    None; advantages of its shape, or one for each sequence where cfg.sequence_advantages. loss: a float32 tensor of one
+    element that gets the loss too."""
     dev, tokens, at, m, o, n = _packed(logp, offsets, mask)
     old, ref, bits = (_like(t, logp, dev, w) for t, w in ((old_logp, "old_logp"), (ref_logp, "ref_logp"), (entropy, "entropy")))
     a = _advantages(cfg, advantages, logp, n, dev)
     out = logp.new_empty(6)
     weight = logp.new_empty(max(n, 0) + 1)
     workspace = _loss_workspace(logp, tokens, n)
-    _call(dev, lib().moara_policy_loss, cfg, at, old, ref, bits, a, m, tokens, o, n, out.data_ptr(), weight.data_ptr(),
-          None if workspace is None else workspace.data_ptr())
+    _call(dev, lib().moara_policy_loss, cfg, at, old, ref, bits, a, m, tokens, o, n, out.data_ptr(), _one(loss, dev),
+          weight.data_ptr(), None if workspace is None else workspace.data_ptr())
     return out, weight
 
 
@@ -1002,12 +1009,13 @@ def _balance_args(cfg, logits, offsets, sequences, mask):
 
 @_streamed
 def moara_balance_loss(cfg: moara_balance_config, logits, index, offsets=None, mask=None, load=None,
-                       sequences: Optional[int] = None):
+                       sequences: Optional[int] = None, loss=None):
     """moara_balance_loss of the C ABI: (out, counts, slope); out: loss, mean balance, z (float32); counts: int64, sequences
     x experts; slope is for the backward call. logits: tokens x experts, float32 or bfloat16, rows any distance apart
     (whatever cfg.logits_dtype says); index: as moara_route gives it; offsets: int64, of packed sequences, each balanced
     for itself, or `sequences`, a number of equal ones (1: all tokens together); mask: bool or uint8, one for each token;
-    load: int64, one for each expert, for f in place of the counts."""
+    load: int64, one for each expert, for f in place of the counts. loss: a float32 tensor of one element that gets the loss
+    too."""
     import torch
     cfg, dev, tokens, ld, m, o, n = _balance_args(cfg, logits, offsets, sequences, mask)
     i = _vector(index, dev, torch.int32, tokens * cfg.top_k, "index")
@@ -1018,8 +1026,8 @@ def moara_balance_loss(cfg: moara_balance_config, logits, index, offsets=None, m
     counts = out.new_empty((s, E), dtype=torch.int64)
     slope = out.new_empty(s * E + 2)
     workspace = out.new_empty((E + 8) * (2 * s + tokens // 32 + 2), dtype=torch.float64)
-    _call(dev, lib().moara_balance_loss, cfg, logits.data_ptr(), tokens, ld, i, m, o, n, load, out.data_ptr(), counts.data_ptr(),
-          slope.data_ptr(), workspace.data_ptr())
+    _call(dev, lib().moara_balance_loss, cfg, logits.data_ptr(), tokens, ld, i, m, o, n, load, out.data_ptr(), _one(loss, dev),
+          counts.data_ptr(), slope.data_ptr(), workspace.data_ptr())
     return out, counts, slope
 
 

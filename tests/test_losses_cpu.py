@@ -64,14 +64,14 @@ PACKED = [(dict(tokens=-1), SHAPE), (dict(tokens=(1 << 33) + 1, sequences=1), SH
 
 @pytest.mark.parametrize("kw,status", PACKED + [
     (dict(sequences=3, tokens=9), SHAPE), (dict(logp=None), ARG), (dict(logp=P + 1), ARG), (dict(ref=P + 2), ARG),
-    (dict(out=None), ARG), (dict(rewards=None), ARG), (dict(slope=None), ARG), (dict(work=None, tokens=8000), ARG), (dict(work=P + 4), ARG),
+    (dict(out=None), ARG), (dict(loss=P + 2), ARG), (dict(rewards=None), ARG), (dict(slope=None), ARG), (dict(work=None, tokens=8000), ARG), (dict(work=P + 4), ARG),
     (dict(beta=0.0), ARG), (dict(beta=-1.0), ARG), (dict(beta=math.inf), ARG), (dict(margin=math.nan), ARG), (dict(kind=3), ARG),
     (dict(kind=-1), ARG), (dict(smoothing=1.5), ARG), (dict(smoothing=-0.1), ARG), (dict(smoothing=0.1, kind=1), ARG),
     (dict(margin=0.5, kind=2), ARG)])
 def test_preference_calls_are_refused(lib, kw, status):
     cfg = M.moara_preference_default_config(**{k: v for k, v in kw.items() if k in ("beta", "margin", "smoothing", "kind")})
-    a = {**dict(logp=P, ref=None, mask=None, tokens=8, offsets=None, sequences=4, out=P, rewards=P, slope=P, work=P), **kw}
-    call = [a[k] for k in ("logp", "ref", "mask", "tokens", "offsets", "sequences", "out", "rewards", "slope", "work")]
+    a = {**dict(logp=P, ref=None, mask=None, tokens=8, offsets=None, sequences=4, out=P, loss=None, rewards=P, slope=P, work=P), **kw}
+    call = [a[k] for k in ("logp", "ref", "mask", "tokens", "offsets", "sequences", "out", "loss", "rewards", "slope", "work")]
     assert lib.moara_preference_loss(ctypes.byref(cfg), *call, None) == status
     if (kw, status) in PACKED:
         assert lib.moara_preference_loss_backward(P, P, None, a["tokens"], a["offsets"], a["sequences"], P, None) == status
@@ -81,12 +81,12 @@ def test_preference_backward_arguments_are_refused(lib):
     for a in ((None, P, P), (P, None, P), (P, P, None), (P + 1, P, P), (P, P + 2, P), (P, P, P + 2)):
         assert lib.moara_preference_loss_backward(a[0], a[1], None, 8, None, 4, a[2], None) == ARG, a
     assert lib.moara_preference_loss_backward(P, P, None, 9, None, 3, P, None) == SHAPE
-    assert lib.moara_preference_loss(None, P, None, None, 8, None, 4, P, P, P, P, None) == ARG
+    assert lib.moara_preference_loss(None, P, None, None, 8, None, 4, P, None, P, P, P, None) == ARG
 
 
 @pytest.mark.parametrize("kw,status", PACKED + [
     (dict(logp=None), ARG), (dict(adv=None), ARG), (dict(logp=P + 1), ARG), (dict(old=P + 2), ARG), (dict(ref=P + 2), ARG),
-    (dict(adv=P + 2), ARG), (dict(entropy=P + 2), ARG), (dict(out=None), ARG), (dict(weight=None), ARG), (dict(work=None, tokens=8000), ARG),
+    (dict(adv=P + 2), ARG), (dict(entropy=P + 2), ARG), (dict(out=None), ARG), (dict(loss=P + 2), ARG), (dict(weight=None), ARG), (dict(work=None, tokens=8000), ARG),
     (dict(work=P + 4), ARG), (dict(clip_low=-0.1), ARG), (dict(clip_low=1.1), ARG), (dict(clip_high=-0.1), ARG),
     (dict(clip_high=math.nan), ARG), (dict(kl_coef=0.1, ref=None), ARG), (dict(entropy_coef=0.1, entropy=None), ARG),
     (dict(kl_coef=math.inf), ARG), (dict(entropy_coef=math.nan), ARG), (dict(divisor=-1.0), ARG), (dict(divisor=math.inf), ARG),
@@ -94,10 +94,11 @@ def test_preference_backward_arguments_are_refused(lib):
 def test_policy_calls_are_refused(lib, kw, status):
     names = [n for n, _ in M.moara_policy_config._fields_]
     cfg = M.moara_policy_default_config(**{k: v for k, v in kw.items() if k in names})
-    a = {**dict(logp=P, old=P, ref=P, entropy=P, adv=P, mask=None, tokens=8, offsets=None, sequences=4, out=P, weight=P, work=P), **kw}
-    order = ("logp", "old", "ref", "entropy", "adv", "mask", "tokens", "offsets", "sequences", "out", "weight", "work")
+    a = {**dict(logp=P, old=P, ref=P, entropy=P, adv=P, mask=None, tokens=8, offsets=None, sequences=4, out=P, loss=None, weight=P,
+           work=P), **kw}
+    order = ("logp", "old", "ref", "entropy", "adv", "mask", "tokens", "offsets", "sequences", "out", "loss", "weight", "work")
     assert lib.moara_policy_loss(ctypes.byref(cfg), *[a[k] for k in order], None) == status
-    if not {"entropy", "entropy_coef", "out", "weight", "work"} & set(kw) or kw.get("entropy_coef") != kw.get("entropy_coef"):
+    if not {"entropy", "entropy_coef", "out", "loss", "weight", "work"} & set(kw) or kw.get("entropy_coef") != kw.get("entropy_coef"):
         back = [a[k] for k in ("logp", "old", "ref", "adv", "mask", "tokens", "offsets", "sequences")]
         assert lib.moara_policy_loss_backward(ctypes.byref(cfg), *back, P, P, P, None, None) == status
     assert lib.moara_policy_loss(None, *[a[k] for k in order], None) == ARG
@@ -114,16 +115,16 @@ def test_policy_backward_arguments_are_refused(lib):
     (dict(experts=0), ARG), (dict(top_k=0), ARG), (dict(score=2), ARG), (dict(logits_dtype=2), ARG),
     (dict(balance_coef=math.nan), ARG), (dict(z_coef=math.inf), ARG), (dict(experts=1025, row=1025), UNS), (dict(top_k=65), UNS),
     (dict(logits=None), ARG), (dict(logits=P + 2), ARG), (dict(row=63), SHAPE), (dict(index=None), ARG), (dict(index=P + 2), ARG),
-    (dict(load=P + 4), ARG), (dict(out=None), ARG), (dict(counts=None), ARG), (dict(counts=P + 4), ARG), (dict(slope=None), ARG),
+    (dict(load=P + 4), ARG), (dict(out=None), ARG), (dict(loss=P + 2), ARG), (dict(counts=None), ARG), (dict(counts=P + 4), ARG), (dict(slope=None), ARG),
     (dict(work=None), ARG), (dict(work=P + 4), ARG)])
 def test_balance_calls_are_refused(lib, kw, status):
     names = [n for n, _ in M.moara_balance_config._fields_]
     cfg = M.moara_balance_default_config(**{k: v for k, v in kw.items() if k in names})
-    a = {**dict(logits=P, tokens=8, row=64, index=P, mask=None, offsets=None, sequences=4, load=None, out=P, counts=P, slope=P,
-                work=P), **kw}
-    order = ("logits", "tokens", "row", "index", "mask", "offsets", "sequences", "load", "out", "counts", "slope", "work")
+    a = {**dict(logits=P, tokens=8, row=64, index=P, mask=None, offsets=None, sequences=4, load=None, out=P, loss=None, counts=P,
+                slope=P, work=P), **kw}
+    order = ("logits", "tokens", "row", "index", "mask", "offsets", "sequences", "load", "out", "loss", "counts", "slope", "work")
     assert lib.moara_balance_loss(ctypes.byref(cfg), *[a[k] for k in order], None) == status
-    if not {"index", "load", "out", "counts", "slope", "work"} & set(kw):
+    if not {"index", "load", "out", "loss", "counts", "slope", "work"} & set(kw):
         back = [a[k] for k in ("logits", "tokens", "row", "mask", "offsets", "sequences")]
         assert lib.moara_balance_loss_backward(ctypes.byref(cfg), *back, P, P, P, None) == status
     assert lib.moara_balance_loss(None, *[a[k] for k in order], None) == ARG
@@ -379,11 +380,17 @@ def calls(monkeypatch):
     ones = lambda t: torch.ones(t.shape, dtype=torch.float32)  # noqa: E731
     record("moara_token_logps", lambda x, lab, scale, entropy: (ones(lab), 2 * ones(lab) if entropy else None, torch.zeros(lab.numel(), 4)))
     record("moara_token_logps_backward", lambda x, lab, stats, g, scale, entropy, grad_entropy: torch.ones_like(x) * g[..., None])
-    record("moara_preference_loss", lambda cfg, x, ref, offsets, mask: (torch.tensor([7.0, 0.5, 0.1]), torch.zeros(4), torch.zeros(4)))
+
+    def filled(loss, value, *rest):
+        loss.fill_(value)
+        return rest
+    record("moara_preference_loss", lambda cfg, x, ref, offsets, mask, loss: filled(
+        loss, 7.0, torch.tensor([7.0, 0.5, 0.1]), torch.zeros(4), torch.zeros(5)))
     record("moara_preference_loss_backward", lambda cfg, x, slope, g, offsets, mask: ones(x) * g)
-    record("moara_policy_loss", lambda cfg, x, a, **kw: (torch.arange(6.0) + 3, torch.zeros(4)))
+    record("moara_policy_loss", lambda cfg, x, a, loss, **kw: filled(loss, 3.0, torch.arange(6.0) + 3, torch.zeros(5)))
     record("moara_policy_loss_backward", lambda cfg, x, a, w, g, entropy=None, **kw: (ones(x) * g, None if entropy is None else -ones(x) * g))
-    record("moara_balance_loss", lambda cfg, x, i, **kw: (torch.tensor([5.0, 1.0, 0.0]), torch.zeros(1, 3, dtype=torch.int64), torch.zeros(5)))
+    record("moara_balance_loss", lambda cfg, x, i, loss, **kw: filled(
+        loss, 5.0, torch.tensor([5.0, 1.0, 0.0]), torch.zeros(1, 3, dtype=torch.int64), torch.zeros(5)))
     record("moara_balance_loss_backward", lambda cfg, x, slope, g, **kw: torch.ones_like(x) * g)
     return seen
 
@@ -415,7 +422,7 @@ def test_losses_are_scalars_of_their_own(calls):
     loss, rewards, about = L.preference_loss(cfg, x)
     cfg.beta = 9.0
     loss /= 4
-    assert float(about[0]) == 7 and not about.requires_grad and not rewards.requires_grad
+    assert float(about[0]) == 7 and float(loss.detach()) == 1.75 and not about.requires_grad and not rewards.requires_grad
     loss.backward()
     assert calls[-1][1][0].beta == 0.1 and torch.equal(x.grad, torch.full_like(x, 0.25))
     cfg = M.moara_policy_config(clip_low=0.2)
