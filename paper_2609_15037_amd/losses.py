@@ -10,7 +10,9 @@ of paired responses and of a clipped policy over them, and the load-balancing lo
     loss, about = policy_loss(cfg, logp, advantages, old_logp=old, ref_logp=ref, entropy=entropy, mask=mask)
 
 Sequences are rows, or packed one after another with their offsets (int64, sequences + 1). Losses are scalars on the
-GPU; nothing is copied to the host.
+GPU; nothing is copied to the host, and a step can be captured into a graph, its backward pass too. As with any torch
+operator, first drop what was computed eagerly from the same parameters (losses of warm-up steps that are still held): their
+gradients' accumulation belongs to the stream of that time, which a capture cannot wait for.
 """
 from __future__ import annotations
 
@@ -45,7 +47,7 @@ class _TokenLogps(torch.autograd.Function):
         if grad_logp is None and grad_entropy is None:
             return None, None, None, None
         logits, labels, stats, bits = ctx.saved_tensors
-        g = torch.zeros(labels.shape, device=logits.device) if grad_logp is None else grad_logp.contiguous()
+        g = stats.new_zeros(labels.shape) if grad_logp is None else grad_logp.contiguous()
         h = None if grad_entropy is None else grad_entropy.contiguous()
         grad = M.moara_token_logps_backward(logits, labels, stats, g, scale=ctx.scale, entropy=None if h is None else bits,
                                             grad_entropy=h)
@@ -56,7 +58,8 @@ def token_logps(logits: torch.Tensor, labels: torch.Tensor, temperature: float =
     """Log-probabilities (float32) of the labels under logits / temperature, and with `entropy` the distributions'
     entropies: both of the labels' shape, the logits' without the last axis. Differentiable in the logits (float32 or
     bfloat16; a view such as `logits[:, :-1]` is not copied). A label outside the vocabulary, e.g. -100, has 0 and no
-    gradient."""
+    gradient: all the logits with such labels where a token is not wanted spare the copy that a view's gradient is put
+    into the whole logits' with."""
     if labels.shape != logits.shape[:-1]:
         raise ValueError(f"labels: shape {tuple(labels.shape)}, the logits have {tuple(logits.shape)}")
     flat = logits if logits.dim() in (2, 3) else logits.reshape(-1, logits.shape[-1])

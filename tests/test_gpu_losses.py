@@ -864,6 +864,26 @@ def _every_call(x, lab, o, old, ref, adv):
     return [logp, H, out, g, h, grad, p_out, rewards, p_grad, b_out, counts, b_grad]
 
 
+@pytest.mark.parametrize("T,S,E", [(40, 4, 8), (6000, 4, 40), (200000, 10, 40), (40000, 1, 256)])
+def test_the_loss_by_itself_is_the_first_output(T, S, E):
+    """A scalar of its own, the same bits as out[0]; what a caller does to it stays out of the others."""
+    M, L = _M(), _L()
+    r = np.random.default_rng(T)
+    logp, ref = (_gpu(-r.random(T), F32) for _ in range(2))
+    o = _gpu(np.linspace(0, T, S + 1).astype(np.int64), torch.int64)
+    logits = _gpu(r.normal(size=(T, E)), F32)
+    index = M.moara_route(M.moara_route_default_config(experts=E, top_k=2), logits)[0]
+    taken = [L.policy_loss(M.moara_policy_default_config(), logp, ref, old_logp=ref, offsets=o),
+             L.balance_loss(M.moara_balance_default_config(experts=E, top_k=2, z_coef=0.1), logits, index, offsets=o)]
+    if S % 2 == 0:
+        taken.append(L.preference_loss(M.moara_preference_default_config(), logp, ref, offsets=o))
+    for loss, *_, about in taken:
+        assert loss.shape == () and float(loss) != 0 and torch.equal(loss, about[0])
+        kept = about.clone()
+        loss += 1
+        assert torch.equal(about, kept)
+
+
 def test_losses_on_another_stream():
     M = _M()
     args = _policy_inputs(T=4000, V=700)

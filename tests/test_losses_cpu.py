@@ -378,7 +378,8 @@ def calls(monkeypatch):
             return answer(*a, **kw)
         monkeypatch.setattr(M, name, f)
     ones = lambda t: torch.ones(t.shape, dtype=torch.float32)  # noqa: E731
-    record("moara_token_logps", lambda x, lab, scale, entropy: (ones(lab), 2 * ones(lab) if entropy else None, torch.zeros(lab.numel(), 4)))
+    record("moara_token_logps", lambda x, lab, scale, entropy: (ones(lab), 2 * ones(lab) if entropy else None,
+                                                              torch.zeros(lab.numel(), 4, dtype=torch.float32)))
     record("moara_token_logps_backward", lambda x, lab, stats, g, scale, entropy, grad_entropy: torch.ones_like(x) * g[..., None])
 
     def filled(loss, value, *rest):
@@ -412,6 +413,18 @@ def test_logps_of_any_axes_and_gradients_of_one_output(calls):
     view = torch.randn(2, 4, 5)
     L.token_logps(view[:, :-1], torch.zeros(2, 3, dtype=torch.int64))
     assert calls[-1][1][0].data_ptr() == view.data_ptr()         # not copied
+
+
+def test_a_gradient_of_the_entropies_alone_whatever_the_default_type(calls):
+    """The log-probabilities' gradient is then made here: of float32, as the library takes it."""
+    from paper_2609_15037_amd import losses as L
+    x = torch.zeros(4, 7, requires_grad=True)
+    torch.set_default_dtype(torch.bfloat16)
+    try:
+        L.token_logps(x, torch.zeros(4, dtype=torch.int64), entropy=True)[1].sum().backward()
+    finally:
+        torch.set_default_dtype(torch.float32)
+    assert calls[-1][1][3].dtype == torch.float32 and not calls[-1][1][3].any()
 
 
 def test_losses_are_scalars_of_their_own(calls):
