@@ -14,6 +14,7 @@ constexpr int GROUP = 8;                // else cells of a workgroup
 
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32u __attribute__((aligned(1)));
+typedef double f64x2u __attribute__((ext_vector_type(2), aligned(8)));
 // A cell's tokens counted from its tile's first: its own [begin, end), those it clears, and how many there are at all.
 struct Span {
   int64_t seq, tile;
@@ -110,21 +111,42 @@ template <int N, int W> __device__ __forceinline__ void leave(const CellSums<N, 
   for (int v = w; v < W && i0 + v < cells && s.seq[v] == s.seq[w]; ++v) x += s.sum[v][k];
   sums[(i0 + w) * N + k] = x;
 }
-// Adds up a sequence's sums, of cells [first, last), by `lanes` lanes: those at its first cell and at each workgroup's
-// first. Four at a time, past the end the last one without weight.
-template <int W, int N> __device__ __forceinline__ void gather(const double* sums, int64_t first, int64_t last, int lane, int lanes,
-                                                        double (&own)[N]) {
+// Adds up the sums of K sequences, of cells [first, last), by `lanes` lanes: those at its first cell and at each workgroup's
+// first. The loads of several turns are on their way together, 16 bytes each, and only for sums that there are: one workgroup's
+// scattered addresses are what this costs.
+template <int W, int K, int N> __device__ __forceinline__ void gather(const double* sums, const int64_t (&first)[K],
+                                                               const int64_t (&last)[K], int lane, int lanes, double (&own)[K][N]) {
+  constexpr int TURNS = 4 / K;
+  int64_t group[K], n[K], most = 0;
 #pragma unroll
-  for (int k = 0; k < N; ++k) own[k] = 0;
-  const int64_t group = first / W, n = last > first ? (last - 1) / W - group + 1 : 0;
-  for (int64_t j = lane; j < n; j += 4 * lanes)
+  for (int s = 0; s < K; ++s) {
+    group[s] = first[s] / W;
+    n[s] = last[s] > first[s] ? (last[s] - 1) / W - group[s] + 1 : 0;
+    most = n[s] > most ? n[s] : most;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int64_t at = j + u * lanes, e = at < n ? at : n - 1;
-      const double* x = sums + N * (e ? (group + e) * W : first);
+    for (int k = 0; k < N; ++k) own[s][k] = 0;
+  }
+  for (int64_t j = lane; j < most; j += TURNS * lanes) {
+    f64x2u x[K][TURNS][N / 2];
 #pragma unroll
-      for (int k = 0; k < N; ++k) own[k] += at < n ? x[k] : 0.0;
-    }
+    for (int s = 0; s < K; ++s)
+#pragma unroll
+      for (int u = 0; u < TURNS; ++u) {
+        const int64_t at = j + u * lanes;
+        const f64x2u* q = reinterpret_cast<const f64x2u*>(sums + N * (at ? (group[s] + at) * W : first[s]));
+#pragma unroll
+        for (int k = 0; k < N / 2; ++k) x[s][u][k] = f64x2u{0, 0};
+        if (at < n[s])
+#pragma unroll
+          for (int k = 0; k < N / 2; ++k) x[s][u][k] = q[k];
+      }
+#pragma unroll
+    for (int s = 0; s < K; ++s)
+#pragma unroll
+      for (int u = 0; u < TURNS; ++u)
+#pragma unroll
+        for (int k = 0; k < N; ++k) own[s][k] += x[s][u][k / 2][k % 2];
+  }
 }
 
 // ---------------------------------------------------------------- pairs of responses
@@ -174,15 +196,15 @@ template <int SHIFT, int W> __device__ __forceinline__ void preference_end(const
   const int lanes = lanes_of_each(pairs), lane = threadIdx.x & (lanes - 1);
   double all[4] = {};           // loss, pairs ahead, margin, pairs with a token
   for (int64_t pair = threadIdx.x / lanes; pair < pairs; pair += END_THREADS / lanes) {
-    double d[2], n[2];
+    int64_t first[2], last[2];
+    double own[2][PREFERENCE_SUMS], d[2], n[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) cells_of(p.q, 2 * pair + k, SHIFT, first[k], last[k]);
+    gather<W>(sums, first, last, lane, lanes, own);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      int64_t first, last;
-      cells_of(p.q, 2 * pair + k, SHIFT, first, last);
-      double own[PREFERENCE_SUMS];
-      gather<W>(sums, first, last, lane, lanes, own);
-      d[k] = over_lanes(own[0], lanes);
-      n[k] = over_lanes(own[1], lanes);
+      d[k] = over_lanes(own[k][0], lanes);
+      n[k] = over_lanes(own[k][1], lanes);
     }
     if (lane == 0) {
       const double per0 = p.average && n[0] > 0 ? 1 / n[0] : 1, per1 = p.average && n[1] > 0 ? 1 / n[1] : 1;
@@ -366,10 +388,11 @@ template <int SHIFT, int W> __device__ __forceinline__ void policy_end(const Pol
   const int lanes = lanes_of_each(S), lane = threadIdx.x & (lanes - 1);
   double all[N] = {};           // the cells' sums, by sequence over its tokens, and the sequences with tokens
   for (int64_t s = threadIdx.x / lanes; s < S; s += END_THREADS / lanes) {
-    int64_t first, last;
-    cells_of(p.q, s, SHIFT, first, last);
-    double own[POLICY_SUMS];
-    gather<W>(sums, first, last, lane, lanes, own);
+    int64_t first[1], last[1];
+    cells_of(p.q, s, SHIFT, first[0], last[0]);
+    double sum[1][POLICY_SUMS];
+    gather<W>(sums, first, last, lane, lanes, sum);
+    const double (&own)[POLICY_SUMS] = sum[0];
     // a sum over the lanes waits for the others' sums below, except where it divides them
     const double n = over_lanes(own[0], lanes), per = !p.by_sequence ? 1 : n > 0 ? 1 / n : 0;
     all[0] += own[0];
