@@ -83,6 +83,10 @@ template <int LANES, bool ENTROPY> __device__ __forceinline__ Part together(cons
 
 // THREADS threads take a row. The label is left out of the sum, which is then small where the label has nearly all of
 // the probability: log p = a - log1p(sum + (e_label - 1)) with a = scale (x_label - top) keeps its relative accuracy.
+// A lane's sum is fp32, rescaled when its maximum grows (once for U vectors), the lanes' are joined in 64 bits. Bound by
+// reads: 4096 x 131072 bf16 in 168 us, 6.4 TB/s; 2039 x 50021 fp32 with entropies 72 us, 5.7 TB/s (rows that start and end
+// within a vector); 8 x 32000 4.6 us, a launch and the latencies of a row. One vector more in flight for each lane, a fetch
+// ahead of the next turn, or registers held down for more waves (64: 120 us instead of 96 at 8192 x 32000) gained nothing.
 template <typename T, int THREADS, int U, bool ENTROPY, bool ONCE>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void k_logps(LogpsParams p) {
   constexpr int N = 16 / sizeof(T), BLOCK = THREADS < 256 ? 256 : THREADS, ROWS = BLOCK / THREADS;
@@ -178,7 +182,9 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void k_logps(LogpsPa
 }
 
 // 2^((x - top) k - log2 sum) is p; GROUP threads take U vectors a lane of a row. The label's own value has 1 - p and
-// log p from the forward pass.
+// log p from the forward pass: no difference of values near 1. Parts of rows, not rows, so that a large vocabulary's few rows
+// fill the GPU. The gradient is rounded once, to its type. Bound by memory: 4096 x 131072 bf16 in 320 us, 2.1 GB at 6.7 TB/s;
+// 2039 x 50021 fp32 with entropies 139 us, 5.9 TB/s.
 template <typename T, int GROUP, bool ENTROPY, bool ONCE_IN, bool ONCE_OUT>
 __global__ __launch_bounds__(256) void k_logps_backward(LogpsParams p, uint32_t parts) {
   constexpr int N = 16 / sizeof(T), U = 4, SPAN = GROUP * N * U, GROUPS = 256 / GROUP;
