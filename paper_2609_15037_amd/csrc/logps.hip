@@ -83,16 +83,17 @@ template <int LANES, bool ENTROPY> __device__ __forceinline__ Part together(cons
 
 // THREADS threads take a row. The label is left out of the sum, which is then small where the label has nearly all of
 // the probability: log p = a - log1p(sum + (e_label - 1)) with a = scale (x_label - top) keeps its relative accuracy.
-// A lane's sum is fp32, rescaled when its maximum grows (once for U vectors), the lanes' are joined in 64 bits. Bound by
-// reads: 4096 x 131072 bf16 in 168 us, 6.4 TB/s; 2039 x 50021 fp32 with entropies 72 us, 5.7 TB/s (rows that start and end
-// within a vector); 8 x 32000 4.6 us, a launch and the latencies of a row. One vector more in flight for each lane, a fetch
-// ahead of the next turn, or registers held down for more waves (64: 120 us instead of 96 at 8192 x 32000) gained nothing.
+// A lane's sum is fp32, rescaled when its maximum grows (once for U vectors), the lanes' are joined in 64 bits. Of its last
+// turn a wave skips the vectors that it has nothing of (2039 x 50021 fp32 on 512 threads 75 us with them, 67 without). Bound
+// by reads: 4096 x 131072 bf16 in 167 us, 6.4 TB/s; 2039 x 50021 fp32 with entropies, rows 50048 apart, 60 us, 6.8 TB/s; 8 x
+// 32000 4.7 us, a launch and the latencies of a row. One vector more in flight for each lane, a fetch ahead of the next turn,
+// or registers held down for more waves (64: 120 us instead of 96 at 8192 x 32000) gained nothing.
 template <typename T, int THREADS, int U, bool ENTROPY, bool ONCE>
-__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void k_logps(LogpsParams p) {
-  constexpr int N = 16 / sizeof(T), BLOCK = THREADS < 256 ? 256 : THREADS, ROWS = BLOCK / THREADS;
+__global__ __launch_bounds__(THREADS <= 64 ? 256 : THREADS) void k_logps(LogpsParams p) {
+  constexpr int N = 16 / sizeof(T), BLOCK = THREADS <= 64 ? 256 : THREADS, ROWS = BLOCK / THREADS;
   constexpr int WAVES = THREADS < 64 ? 1 : THREADS / 64, LANES = THREADS < 64 ? THREADS : 64;
   __shared__ Part parts[2][WAVES];
-  const int lane = threadIdx.x % THREADS;
+  const int lane = threadIdx.x % THREADS, first = THREADS > 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x & -64) : 0;
   const float k = p.log2_scale;
   int turn = 0;
   for (int64_t r = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS; r < p.tokens; r += (int64_t)gridDim.x * ROWS) {
@@ -110,8 +111,11 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void k_logps(LogpsPa
     const float xl = value(row + own);
     float top = -FLT_MAX, sum = 0, bits = 0;
     // U vectors a lane; in the last ones (whole: false) those that there are, and of the row's last V % N elements one a lane
-    auto take = [&](int base, auto whole) {
+    auto take = [&](int at, auto whole) {
       constexpr bool WHOLE = decltype(whole)::value;
+      const int base = at + N * lane;
+      // whether the wave has any of its u-th vectors
+      auto some = [&](int u) { return WHOLE || at + N * (first + u * THREADS) < V; };
       u32x4 raw[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -123,18 +127,20 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void k_logps(LogpsPa
       const float more = !WHOLE && rag < V && rag != own ? value(row + rag) : -__builtin_inff();
       float x[U][N];
 #pragma unroll
-      for (int u = 0; u < U; ++u) apart(raw[u], x[u]);
-      const unsigned at = own - base;
-      if (at < N * THREADS * U && at % (N * THREADS) < N)
+      for (int u = 0; u < U; ++u)
+        if (some(u)) apart(raw[u], x[u]);
+      const unsigned hit = own - base;
+      if (hit < N * THREADS * U && hit % (N * THREADS) < N)
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-          for (int j = 0; j < N; ++j) x[u][j] = at == u * N * THREADS + j ? -__builtin_inff() : x[u][j];
+          for (int j = 0; j < N; ++j) x[u][j] = hit == u * N * THREADS + j ? -__builtin_inff() : x[u][j];
       float most = WHOLE ? top : fmaxf(top, more);
 #pragma unroll
       for (int u = 0; u < U; ++u)
+        if (some(u))
 #pragma unroll
-        for (int j = 0; j < N; ++j) most = fmaxf(most, x[u][j]);
+          for (int j = 0; j < N; ++j) most = fmaxf(most, x[u][j]);
       const float d = fmaxf((top - most) * k, LEAST), f = __builtin_amdgcn_exp2f(d);
       if (ENTROPY) bits = f * fmaf(d, sum, bits);
       sum *= f;
@@ -146,13 +152,14 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void k_logps(LogpsPa
       };
 #pragma unroll
       for (int u = 0; u < U; ++u)
+        if (some(u))
 #pragma unroll
-        for (int j = 0; j < N; ++j) add(x[u][j]);
+          for (int j = 0; j < N; ++j) add(x[u][j]);
       if (!WHOLE) add(more);
     };
     int at = 0;
-    for (; at + N * THREADS * U <= V; at += N * THREADS * U) take(at + N * lane, std::true_type{});
-    if (at < V) take(at + N * lane, std::false_type{});
+    for (; at + N * THREADS * U <= V; at += N * THREADS * U) take(at, std::true_type{});
+    if (at < V) take(at, std::false_type{});
     Part a = together<LANES, ENTROPY>(Part{top, sum, bits}, k);
     if (WAVES > 1) {
       // one barrier a row: the next row's parts go to the other half, and the first wave has read this one's when it
@@ -188,7 +195,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void k_logps(LogpsPa
 template <typename T, int GROUP, bool ENTROPY, bool ONCE_IN, bool ONCE_OUT>
 __global__ __launch_bounds__(256) void k_logps_backward(LogpsParams p, uint32_t parts) {
   constexpr int N = 16 / sizeof(T), U = 4, SPAN = GROUP * N * U, GROUPS = 256 / GROUP;
-  const int lane = threadIdx.x % GROUP;
+  const int lane = threadIdx.x % GROUP, first = GROUP > 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x & -64) : 0;
   const int64_t units = p.tokens * parts;
   for (int64_t i = (int64_t)blockIdx.x * GROUPS + threadIdx.x / GROUP; i < units; i += (int64_t)gridDim.x * GROUPS) {
     const int64_t r = parts == 1 ? i : i <= 0xFFFFFFFF ? (uint32_t)i / parts : i / parts;
@@ -229,6 +236,7 @@ __global__ __launch_bounds__(256) void k_logps_backward(LogpsParams p, uint32_t 
     };
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+      if (!whole && at + N * (first + u * GROUP) >= V) break;         // nothing for the whole wave
       const int e = base + u * N * GROUP;
       float x[N];
       apart(raw[u], x);
@@ -254,7 +262,7 @@ template <typename T> double bytes_of(const LogpsParams& p) { return (double)p.t
 constexpr int64_t MOST_GROUPS = 1 << 21;        // workgroups of a launch: fewer than 2^32 threads
 
 template <typename T, int THREADS, int U, bool ONCE> void forward(const LogpsParams& p, hipStream_t st) {
-  constexpr int block = THREADS < 256 ? 256 : THREADS, rows = block / THREADS;
+  constexpr int block = THREADS <= 64 ? 256 : THREADS, rows = block / THREADS;
   const int64_t n = (p.tokens + rows - 1) / rows;
   const dim3 g((uint32_t)(n < MOST_GROUPS ? n : MOST_GROUPS)), b(block);
   if (p.entropy) hipLaunchKernelGGL((k_logps<T, THREADS, U, true, ONCE>), g, b, 0, st, p);
@@ -280,28 +288,32 @@ template <typename T, int GROUP> void backward(const LogpsParams& p, hipStream_t
 
 }  // namespace
 
-// Threads of a row. Many rows, bf16 (fp32), us, from the caches: 65536 x 512 (x 256) 15 (13) on 16 lanes, 44 (33) on a wave;
-// 32768 x 2048 28 on a wave, 87 on 256 threads; 8192 x 8192 26 and 27 (16384 x 4096 43 and 41); 8192 x 32000 95 (174) on 256,
-// 128 (169) on 1024; 4096 x 131072 190 (351) and 174 (339). Few rows: 64 x 131072 11.4 and 9.0, 256 x 32000 5.6 and 5.0, 512 x
-// 32000 7.8 and 8.9.
+// Threads of a row: a turn of all of them takes 4 vectors each, and what a row's last turn lacks is lost. Many rows, us, on
+// 64, 256, 512 and 1024 threads: bf16 16384 x 3000 21, 37, 75 and 127; 16384 x 9000 52, 65, 97 and 174; 8192 x 20000 61, 56, 77
+// and 107; 4096 x 65536 102, 87, 85 and 96; 4096 x 100000 139, 140, 135 and 145; fp32 16384 x 4096 45, 41, 60 and 128; 8192 x
+// 20000 102, 101, 98 and 127; 4096 x 131072 329, 323, 318 and 314. Few rows: bf16 64 x 4096 4.2, 3.8, 3.7 and 3.9; 1024 x 4096
+// 4.2, 4.9, 6.6 and 9.8; 1024 x 8192 5.7, 5.2, 7.0 and 10.6; 256, 512 and 1024 threads: 256 x 50021 7.7, 6.8 and 6.9; 300 x
+// 50021 10.0, 10.6 and 12.1. 65536 x 512 15 on 16 lanes, 44 on a wave.
 hipError_t launch_logps(const LogpsParams& p, hipStream_t st) {
   const int64_t vectors = (p.vocab + (p.bf16 ? 7 : 3)) / (p.bf16 ? 8 : 4);
 #define LOGPS(THREADS, U) p.bf16 ? forward<bf16, THREADS, U>(p, st) : forward<float, THREADS, U>(p, st)
   if (vectors <= 128) LOGPS(16, 2);
-  else if (vectors <= 512) LOGPS(64, 4);
-  else if (vectors <= 8192 && (vectors < 2048 || p.tokens > 256)) LOGPS(256, 4);
-  else LOGPS(1024, 4);
+  else if (p.tokens <= 256 && vectors >= 1280) LOGPS(512, 4);
+  else if ((p.tokens > 512 && vectors <= 512) || (p.tokens >= 2048 && vectors <= 1280)) LOGPS(64, 4);
+  else if (vectors <= (p.bf16 ? 8192 : 4096)) LOGPS(256, 4);
+  else LOGPS(512, 4);
 #undef LOGPS
   return hipGetLastError();
 }
 
-// Threads of a row's part, by the same cases: 65536 x 512 bf16 22 us on 16 lanes, 35 on a wave, 114 on 256 threads; 32768 x 2048
-// 44, 44 and 67.
+// Threads of a row's part. bf16, us: 65536 x 512 22 on 16 lanes, 35 on a wave, 114 on 256 threads; on a wave and on 256 threads:
+// 16384 x 2100 26 and 31, x 9000 103 and 129, 8192 x 32000 186 and 181, 4096 x 131072 342 and 339; fp32 16384 x 5000 111 and 133,
+// 8192 x 16384 175 and 169.
 hipError_t launch_logps_backward(const LogpsParams& p, hipStream_t st) {
   const int64_t vectors = (p.vocab + (p.bf16 ? 7 : 3)) / (p.bf16 ? 8 : 4);
 #define LOGPS(GROUP) p.bf16 ? backward<bf16, GROUP>(p, st) : backward<float, GROUP>(p, st)
   if (vectors <= 128) LOGPS(16);
-  else if (vectors <= 512) LOGPS(64);
+  else if (vectors <= 2048) LOGPS(64);
   else LOGPS(256);
 #undef LOGPS
   return hipGetLastError();

@@ -52,7 +52,7 @@ def _close(got, want, tol, what=""):
 # ---------------------------------------------------------------- log-probabilities of tokens
 # With a = scale (x - max): the difference, the factor and their product are rounded (3 u |a| in the exponent), the
 # exponential is good to a step (2 u), and a sum adds u for each of the terms that one lane adds up (a row is on at least 16
-# lanes, on 64 above a vocabulary of 1024, on 256 above 4096) and two for each 16 of them where its maximum moves. So e_j is good to
+# lanes, on 64 above a vocabulary of 1024, on 256 above 4096, or from 2048 rows on above 10240) and two for each 16 of them where its maximum moves. So e_j is good to
 # (3 |a_j| + 2) u, their sum to s = (3 sum p_j |a_j| + 2 + n) u; log1p to two steps (4 u).
 # The label is apart from the others' sum R, whose own error over the whole sum S is that of its terms alone: with d e_j <=
 # (3 |a_j| + 2 + n) u e_j, d R / S <= sum over j != label of p_j (3 |a_j| + 2 + n) u =: o. It is what log S = log1p(R + e - 1)
@@ -62,13 +62,14 @@ def _close(got, want, tol, what=""):
 # All this holds for numbers that fp32 holds to 24 bits. An exponential under 2^-126 may be taken as 0 or have fewer: V of
 # them are off by at most V 2^-126 in R, and so in log p, which is as small there.
 
-def _adds(V):
-    return V / (16 if V <= 1024 else 64 if V <= 4096 else 256) * 1.125 + 12
+def _adds(shape):
+    V, rows = shape[-1], np.prod(shape[:-1])
+    return V / (16 if V <= 1024 else 64 if V <= 4096 or (V <= 10240 and rows >= 2048) else 256) * 1.125 + 12
 
 
 def _others(a, p, lab):
     """o of the text above, for each row."""
-    each = np.where(np.arange(a.shape[-1]) == lab[..., None], 0, p) * (3 * np.where(p > 0, np.abs(a), 0) + 2 + _adds(a.shape[-1]))
+    each = np.where(np.arange(a.shape[-1]) == lab[..., None], 0, p) * (3 * np.where(p > 0, np.abs(a), 0) + 2 + _adds(a.shape))
     return each.sum(axis=-1) * U
 
 
@@ -79,7 +80,7 @@ def _terms(x, scale):
         a = scale * (x - x.max(axis=-1, keepdims=True))
         log = O.log_softmax(scale * x)
         p = np.exp(log)
-    n = _adds(V)
+    n = _adds(x.shape)
     s = (3 * np.abs(O.xlogy(p, a)).sum(axis=-1) + 2 + n) * U
     return a, log, p, s
 
@@ -174,7 +175,7 @@ def test_logps_of_every_size(V, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("T,V", [(3, 50021), (2, 131073), (33, 32000), (1, 131072), (600, 12289)])
+@pytest.mark.parametrize("T,V", [(3, 50021), (2, 131073), (33, 32000), (1, 131072), (600, 12289), (300, 70001)])
 def test_logps_of_large_vocabularies(T, V, dtype):
     x, lab, g, h = _case(1, T, V, dtype, 1.0)
     _check_logps(x, lab, g, h)
