@@ -501,7 +501,7 @@ int moara_route_balance(int32_t experts, int64_t* counts, float* bias, float rat
  *   logits: tokens rows of vocab consecutive elements; row r starts at element
  *           (r / inner) outer_stride + (r % inner) row_stride (inner = tokens: rows row_stride apart;
  *           otherwise e.g. a batch whose last positions are left out).
- *   scale:  > 0, e.g. the reciprocal of a temperature.
+ *   scale:  > 0 and below 2.3e38, e.g. the reciprocal of a temperature.
  *   out_stats: 4 floats for each token, 16-byte aligned, for moara_token_logps_backward.
  * Sums are fp32 within a lane and 64 bits across them; log-probabilities near 0 keep their
  * relative accuracy (the others' exponentials are summed apart from the label's).

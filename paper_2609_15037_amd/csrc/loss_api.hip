@@ -32,7 +32,8 @@ int check_logps(LogpsParams& p, const void* logits, int32_t dtype, int64_t token
   if (dtype != MOARA_F32 && dtype != MOARA_BF16) return moara_fail(MOARA_E_ARG, "bad logits dtype");
   if (tokens < 0 || tokens > (int64_t)1 << 40 || vocab < 1 || vocab > (int64_t)1 << 30)
     return moara_fail(MOARA_E_SHAPE, "%lld tokens, vocabulary of %lld", (long long)tokens, (long long)vocab);
-  if (!(scale > 0) || !isfinite(scale)) return moara_fail(MOARA_E_ARG, "scale must be positive");
+  const float log2_scale = (float)(scale * 1.4426950408889634);
+  if (!(scale > 0) || !isfinite(log2_scale)) return moara_fail(MOARA_E_ARG, "scale must be positive, below 2.3e38");
   if (tokens == 0) return MOARA_OK;
   if (inner < 1 || (inner > 1 && tokens > 1 && row_stride < vocab) || (inner < tokens && outer_stride < vocab) ||
       row_stride > MAX_STRIDE || outer_stride > MAX_STRIDE)
@@ -49,7 +50,7 @@ int check_logps(LogpsParams& p, const void* logits, int32_t dtype, int64_t token
   p.outer = outer_stride;
   p.labels = labels;
   p.scale = scale;
-  p.log2_scale = (float)(scale * 1.4426950408889634);
+  p.log2_scale = log2_scale;
   p.bf16 = dtype == MOARA_BF16;
   return MOARA_OK;
 }

@@ -13,9 +13,11 @@ Sequences are rows, or packed one after another with their offsets (int64, seque
 GPU; nothing is copied to the host, and a step can be captured into a graph, its backward pass too. As with any torch
 operator, first drop what was computed eagerly from the same parameters (losses of warm-up steps that are still held): their
 gradients' accumulation belongs to the stream of that time, which a capture cannot wait for.
+Gradients of the gradients are refused.
 """
 from __future__ import annotations
 
+import functools
 from typing import Optional, Tuple
 
 import torch
@@ -32,6 +34,32 @@ def _rows(t: torch.Tensor) -> torch.Tensor:
     return t if t.dtype is torch.float32 and t.is_contiguous() else t.float().contiguous()
 
 
+class _Last(torch.autograd.Function):
+    """A gradient that may be used, but not differentiated again."""
+    @staticmethod
+    def forward(ctx, grad, source):
+        return grad.view_as(grad)
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("the library's losses have no gradient of their gradient")
+
+
+def _once(backward):
+    """For a backward pass that has none of its own. Where a second one may be asked for (create_graph), asking is an error,
+    also if what came in is a constant: the gradient is none."""
+    @functools.wraps(backward)
+    def call(ctx, *grads):
+        if not torch.is_grad_enabled():
+            return backward(ctx, *grads)
+        with torch.no_grad():
+            out = backward(ctx, *grads)
+        source = torch.zeros((), requires_grad=True)
+        last = lambda g: None if g is None else _Last.apply(g, source)      # noqa: E731
+        return tuple(map(last, out)) if isinstance(out, tuple) else last(out)
+    return call
+
+
 class _TokenLogps(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, labels, scale, entropy):
@@ -42,7 +70,7 @@ class _TokenLogps(torch.autograd.Function):
         return (logp, bits) if entropy else logp
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, grad_logp, grad_entropy=None):
         if grad_logp is None and grad_entropy is None:
             return None, None, None, None
@@ -84,7 +112,7 @@ class _Preference(torch.autograd.Function):
         return loss, rewards, out
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, grad, *_):
         logp, slope, offsets, mask = ctx.saved_tensors
         return M.moara_preference_loss_backward(ctx.cfg, logp, slope, grad.contiguous(), offsets=offsets, mask=mask), \
@@ -113,7 +141,7 @@ class _Policy(torch.autograd.Function):
         return loss, out
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, grad, _):
         logp, entropy, advantages, weight, old_logp, ref_logp, offsets, mask = ctx.saved_tensors
         if not ctx.needs_input_grad[1]:
@@ -148,7 +176,7 @@ class _Balance(torch.autograd.Function):
         return loss, counts, out
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, grad, *_):
         logits, slope, offsets, mask = ctx.saved_tensors
         return M.moara_balance_loss_backward(ctx.cfg, logits, slope, grad.contiguous(), offsets=offsets, mask=mask,

@@ -32,7 +32,7 @@ LOGITS = dict(logits=P, dtype=0, tokens=4, vocab=10, row=10, inner=4, outer=0, s
 @pytest.mark.parametrize("kw,status", [
     (dict(dtype=2), ARG), (dict(tokens=-1), SHAPE), (dict(tokens=(1 << 40) + 1), SHAPE), (dict(vocab=0), SHAPE),
     (dict(vocab=(1 << 30) + 1), SHAPE), (dict(scale=0.0), ARG), (dict(scale=-1.0), ARG), (dict(scale=math.nan), ARG),
-    (dict(scale=math.inf), ARG), (dict(row=9), SHAPE), (dict(row=0), SHAPE), (dict(row=-10), SHAPE), (dict(inner=0), SHAPE),
+    (dict(scale=math.inf), ARG), (dict(scale=3e38), ARG), (dict(row=9), SHAPE), (dict(row=0), SHAPE), (dict(row=-10), SHAPE), (dict(inner=0), SHAPE),
     (dict(inner=2, outer=9), SHAPE), (dict(inner=2, outer=0), SHAPE), (dict(inner=2, outer=1 << 45), SHAPE),
     (dict(row=1 << 45), SHAPE), (dict(logits=None), ARG), (dict(labels=None), ARG),
     (dict(logits=P + 2), ARG), (dict(logits=P + 1, dtype=1), ARG), (dict(labels=P + 4), ARG),
@@ -425,6 +425,18 @@ def test_a_gradient_of_the_entropies_alone_whatever_the_default_type(calls):
     finally:
         torch.set_default_dtype(torch.float32)
     assert calls[-1][1][3].dtype == torch.float32 and not calls[-1][1][3].any()
+
+
+def test_a_gradient_of_a_gradient_is_refused(calls):
+    """Not given as if the first gradient did not depend on its inputs; the first one itself may be had in that way."""
+    from paper_2609_15037_amd import losses as L
+    x = torch.zeros(4, 7, requires_grad=True)
+    loss, about = L.policy_loss(M.moara_policy_default_config(), L.token_logps(x, torch.zeros(4, dtype=torch.int64))[None],
+                                torch.ones(1, 4))
+    g, = torch.autograd.grad(loss, x, create_graph=True)
+    assert torch.equal(g, torch.ones(4, 7))
+    with pytest.raises(RuntimeError, match="no gradient of their gradient"):
+        (loss + g.square().sum()).backward()
 
 
 def test_losses_are_scalars_of_their_own(calls):
