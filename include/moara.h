@@ -485,7 +485,7 @@ int moara_route_balance(int32_t experts, int64_t* counts, float* bias, float rat
  * pointers of their element type's alignment, and give the same bits for the same arguments.
  *
  * Packed tokens. The losses over sequences take `tokens` values one after another. Sequence s
- * of `sequences` is [offsets[s], offsets[s + 1]) (int64 device memory, sequences + 1 values that do
+ * of `sequences` (at least 1) is [offsets[s], offsets[s + 1]) (int64 device memory, sequences + 1 values that do
  * not fall, from 0 to tokens; sequences may be empty), or, without offsets, the s-th of equal
  * parts (tokens is a multiple of sequences). mask (tokens bytes, or null): a token with 0 is
  * left out, as are tokens before the first and behind the last sequence: whatever values they

@@ -427,8 +427,9 @@ template <int SHIFT, int W> __device__ __forceinline__ void policy_end(const Pol
   }
 }
 
-// 16 us for 42 MB, 2.6 TB/s: about 100 vector instructions a token (two exponentials, two series, sums in 64 bits) take 6 us
-// of it, the rest is the latencies of one set of waves as above.
+// 16 us for 42 MB, 2.6 TB/s: all waves are resident, and their phases follow one another: the search, the loads (8 us at a copy's
+// rate), two exponentials and two series a token, the sums. A third fewer instructions (bounds checks kept out of all tiles but
+// the last, inputs masked instead of terms) took as long.
 template <int SHIFT> __global__ __launch_bounds__(64 * GROUP) void k_policy_cells(PolicyParams p, int64_t cells) {
   __shared__ CellSums<POLICY_SUMS, GROUP> s;
   const int64_t i0 = (int64_t)blockIdx.x * GROUP, i = i0 + (threadIdx.x >> 6);

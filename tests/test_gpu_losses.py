@@ -1,5 +1,6 @@
 """The losses on the GPU, against the 64-bit oracle. Tolerances count roundings: u = 2^-24 is half a step of fp32."""
 import math
+import threading
 
 import numpy as np
 import pytest
@@ -899,6 +900,28 @@ def test_losses_on_another_stream():
     also = M.moara_token_logps(args[0], args[1], stream=s.cuda_stream)[0]
     s.synchronize()
     assert torch.equal(logp, want[0]) and torch.equal(also, want[0])
+
+
+def test_losses_from_two_threads_at_once():
+    """Each on its own stream and its own inputs, whose sizes take other kernels: as one call after another."""
+    inputs = [_policy_inputs(T=4000, V=700), _policy_inputs(T=300, V=9000, dtype=F32)]
+    want = [_every_call(*a) for a in inputs]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            for _ in range(20):
+                got = _every_call(*inputs[i])
+                s.synchronize()
+                wrong.extend((i, n) for n, (a, b) in enumerate(zip(got, want[i])) if not torch.equal(a, b))
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
 
 
 @pytest.mark.parametrize("T", [300, 9000])
