@@ -33,10 +33,11 @@ template <int SHIFT> __device__ __forceinline__ Span span_of(const Packed& q, in
               from_tile(c.fill3), from_tile(q.tokens)};
 }
 __device__ __forceinline__ int within(int r, int from, int to) { return r >= from && r < to; }
-// Four tokens from the r-th of a tile: all in one access where they exist.
-__device__ __forceinline__ void load4(const float* q, const Span& c, int r, float (&x)[4]) {
+// Four tokens from the r-th of a tile, in one access. Only in the last tile (WHOLE: not that one) may some not exist: what
+// asks for that, lane by lane and load by load, is kept out of all other cells.
+template <bool WHOLE> __device__ __forceinline__ void load4(const float* q, const Span& c, int r, float (&x)[4]) {
   q += c.tile;
-  if (r + 4 <= c.left) {
+  if (WHOLE || r + 4 <= c.left) {
     const f32x4u a = *reinterpret_cast<const f32x4u*>(q + r);
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[j] = a[j];
@@ -54,10 +55,10 @@ __device__ __forceinline__ int inside4(const Span& c, int r) {
   for (int j = 0; j < 4; ++j) in |= within(r + j, c.begin, c.end) << j;
   return in;
 }
-__device__ __forceinline__ uint32_t mask4(const Packed& q, const Span& c, int r) {
+template <bool WHOLE> __device__ __forceinline__ uint32_t mask4(const Packed& q, const Span& c, int r) {
   if (!q.mask) return 0x01010101u;
   const uint8_t* m = q.mask + c.tile;
-  if (r + 4 <= c.left) return *reinterpret_cast<const u32u*>(m + r);
+  if (WHOLE || r + 4 <= c.left) return *reinterpret_cast<const u32u*>(m + r);
   uint32_t x = 0;
 #pragma unroll
   for (int j = 0; j < 4; ++j)
@@ -155,34 +156,41 @@ template <int W, int K, int N> __device__ __forceinline__ void gather(const doub
 // ---------------------------------------------------------------- pairs of responses
 constexpr int PREFERENCE_SUMS = 2;      // of logp - ref, and the number of tokens
 
-template <int SHIFT, int W>
-__device__ __forceinline__ void preference_cell(const PreferenceParams& p, int64_t i, CellSums<PREFERENCE_SUMS, W>& s) {
+// A token that does not count has zeros for its inputs, and so for its terms; here and below.
+template <int SHIFT, bool WHOLE>
+__device__ __forceinline__ void preference_sums(const PreferenceParams& p, const Span& c, double& sum, int& count) {
   constexpr int TURNS = 1 << (SHIFT - ONE);
-  const Span c = span_of<SHIFT>(p.q, i);
-  double sum = 0;
-  int count = 0, in[TURNS];
+  int in[TURNS];
   uint32_t mask[TURNS];
   float x[TURNS][4], y[TURNS][4];
 #pragma unroll
   for (int v = 0; v < TURNS; ++v) {     // all of a lane's loads are on their way before the first is used
     const int r = 4 * (threadIdx.x & 63) + 256 * v;
     in[v] = inside4(c, r);
-    mask[v] = 0;
-    zero4(x[v]);
-    zero4(y[v]);
-    if (in[v]) {
-      mask[v] = mask4(p.q, c, r);
-      load4(p.logp, c, r, x[v]);
-      if (p.ref) load4(p.ref, c, r, y[v]);
-    }
+    if (!in[v]) continue;
+    mask[v] = mask4<WHOLE>(p.q, c, r);
+    load4<WHOLE>(p.logp, c, r, x[v]);
+    if (p.ref) load4<WHOLE>(p.ref, c, r, y[v]); else zero4(y[v]);
   }
 #pragma unroll
   for (int v = 0; v < TURNS; ++v) {
+    if (!in[v]) continue;
     const int on = live4(in[v], mask[v]);
     count += __popc(on);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sum += on >> j & 1 ? (double)x[v][j] - (double)y[v][j] : 0.0;
+    for (int j = 0; j < 4; ++j) {
+      const bool live = on >> j & 1;
+      sum += (double)(live ? x[v][j] : 0.f) - (double)(live ? y[v][j] : 0.f);
+    }
   }
+}
+template <int SHIFT, int W>
+__device__ __forceinline__ void preference_cell(const PreferenceParams& p, int64_t i, CellSums<PREFERENCE_SUMS, W>& s) {
+  const Span c = span_of<SHIFT>(p.q, i);
+  double sum = 0;
+  int count = 0;
+  if (c.left >= 1 << SHIFT) preference_sums<SHIFT, true>(p, c, sum, count);
+  else preference_sums<SHIFT, false>(p, c, sum, count);
   sum = sum_of<64>(sum);
   const double n = sum_of<64>((double)count);
   if ((threadIdx.x & 63) == 0) {
@@ -284,7 +292,7 @@ __global__ __launch_bounds__(256) void k_preference_backward(Packed q, const flo
   const Span c = span_of<ONE>(q, i);
   const int r = 4 * (threadIdx.x & 63);
   const float g = c.seq >= 0 ? slope[c.seq] * all : 0.f;
-  const int in = inside4(c, r), on = live4(in, in ? mask4(q, c, r) : 0);
+  const int in = inside4(c, r), on = live4(in, !in ? 0 : c.left >= 1 << ONE ? mask4<true>(q, c, r) : mask4<false>(q, c, r));
   float x[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) x[j] = on >> j & 1 ? g : 0.f;
@@ -314,39 +322,39 @@ __device__ __forceinline__ float exp_of(float q) {
 }
 
 // A token's terms. d and the comparison with the bounds are 64 bits: a ratio next to a bound falls on the side
-// that the difference of the two fp32 log-probabilities says.
+// that the difference of the two fp32 log-probabilities says. KL: the kind of the distance, or NO_REF.
+constexpr int NO_REF = -1;
 struct Token { float gain, slope, kl, dkl, excess; bool clipped; };
-__device__ __forceinline__ Token policy_token(const PolicyParams& p, float logp, float old, float ref, float a) {
+template <int KL> __device__ __forceinline__ Token policy_token(const PolicyParams& p, float logp, float old, float ref, float a) {
   Token t;
   const double d = p.old ? (double)logp - (double)old : 0.0;
-  const float df = (float)d, ratio = exp_of(df), q = p.ref ? (float)((double)ref - (double)logp) : 0.f, e = exp_of(q);
+  const float df = (float)d, ratio = exp_of(df);
   const bool up = d > p.high && a > 0, down = d < p.low && a < 0;
   t.clipped = up || down;
   t.gain = (up ? p.at_high : down ? p.at_low : ratio) * a;
   t.slope = t.clipped ? 0.f : -ratio * a;
   t.excess = exp_excess(df, ratio);
-  const float far = exp_excess(q, e), dfar = fabsf(q) < 0.5f ? q + far : e - 1.f;
-  t.kl = p.kl == 0 ? far : p.kl == 1 ? -q : 0.5f * q * q;
-  t.dkl = p.kl == 0 ? -dfar : p.kl == 1 ? 1.f : -q;
+  const float q = KL == NO_REF ? 0.f : (float)((double)ref - (double)logp), e = KL == 0 ? exp_of(q) : 0.f;
+  const float far = KL == 0 ? exp_excess(q, e) : 0.f;
+  t.kl = KL == 0 ? far : KL == 1 ? -q : 0.5f * q * q;
+  t.dkl = KL == 0 ? -(fabsf(q) < 0.5f ? q + far : e - 1.f) : KL == 1 ? 1.f : -q;
   return t;
 }
 struct Four { float logp[4], old[4], ref[4], a[4]; };
+template <int KL, bool WHOLE>
 __device__ __forceinline__ void fetch(const PolicyParams& p, const Span& c, int r, float each, Four& x) {
-  load4(p.logp, c, r, x.logp);
-  if (p.old) load4(p.old, c, r, x.old); else zero4(x.old);
-  if (p.ref) load4(p.ref, c, r, x.ref); else zero4(x.ref);
-  if (!p.sequence_advantages) load4(p.advantages, c, r, x.a);
+  load4<WHOLE>(p.logp, c, r, x.logp);
+  if (p.old) load4<WHOLE>(p.old, c, r, x.old); else zero4(x.old);
+  if (KL != NO_REF) load4<WHOLE>(p.ref, c, r, x.ref); else zero4(x.ref);
+  if (!p.sequence_advantages) load4<WHOLE>(p.advantages, c, r, x.a);
   else
 #pragma unroll
     for (int j = 0; j < 4; ++j) x.a[j] = each;
 }
-
-template <int SHIFT, int W>
-__device__ __forceinline__ void policy_cell(const PolicyParams& p, int64_t i, CellSums<POLICY_SUMS, W>& s) {
+template <int KL, int SHIFT, bool WHOLE>
+__device__ __forceinline__ void policy_sums(const PolicyParams& p, const Span& c, double (&sum)[POLICY_SUMS]) {
   constexpr int TURNS = 1 << (SHIFT - ONE);
-  const Span c = span_of<SHIFT>(p.q, i);
   const float each = p.sequence_advantages && c.seq >= 0 ? p.advantages[c.seq] : 0.f;
-  double sum[POLICY_SUMS] = {};
   int count = 0, clipped = 0;
   Four x[TURNS];
   float entropy[TURNS][4];
@@ -357,9 +365,9 @@ __device__ __forceinline__ void policy_cell(const PolicyParams& p, int64_t i, Ce
     const int r = 4 * (threadIdx.x & 63) + 256 * v;
     in[v] = inside4(c, r);
     if (!in[v]) continue;
-    mask[v] = mask4(p.q, c, r);
-    fetch(p, c, r, each, x[v]);
-    if (p.entropy) load4(p.entropy, c, r, entropy[v]); else zero4(entropy[v]);
+    mask[v] = mask4<WHOLE>(p.q, c, r);
+    fetch<KL, WHOLE>(p, c, r, each, x[v]);
+    if (p.entropy) load4<WHOLE>(p.entropy, c, r, entropy[v]); else zero4(entropy[v]);
   }
 #pragma unroll
   for (int v = 0; v < TURNS; ++v) {
@@ -368,17 +376,24 @@ __device__ __forceinline__ void policy_cell(const PolicyParams& p, int64_t i, Ce
     count += __popc(on);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const Token y = policy_token(p, x[v].logp[j], x[v].old[j], x[v].ref[j], x[v].a[j]);
       const bool live = on >> j & 1;
-      sum[1] -= live ? (double)y.gain : 0.0;
-      sum[2] += live ? (double)y.kl : 0.0;
-      sum[3] += live ? (double)entropy[v][j] : 0.0;
-      clipped += live && y.clipped;
-      sum[5] += live ? (double)y.excess : 0.0;
+      auto of = [&](const float (&y)[4]) { return live ? y[j] : 0.f; };
+      const Token y = policy_token<KL>(p, of(x[v].logp), of(x[v].old), of(x[v].ref), of(x[v].a));
+      sum[1] -= (double)y.gain;
+      if (KL != NO_REF) sum[2] += (double)y.kl;
+      sum[3] += (double)of(entropy[v]);
+      clipped += y.clipped;
+      sum[5] += (double)y.excess;
     }
   }
   sum[0] = count;
   sum[4] = clipped;
+}
+template <int KL, int SHIFT, int W>
+__device__ __forceinline__ void policy_cell(const PolicyParams& p, int64_t i, CellSums<POLICY_SUMS, W>& s) {
+  const Span c = span_of<SHIFT>(p.q, i);
+  double sum[POLICY_SUMS] = {};
+  if (c.left >= 1 << SHIFT) policy_sums<KL, SHIFT, true>(p, c, sum); else policy_sums<KL, SHIFT, false>(p, c, sum);
 #pragma unroll
   for (int k = 0; k < POLICY_SUMS; ++k) sum[k] = sum_of<64>(sum[k]);
   if ((threadIdx.x & 63) == 0) {
@@ -427,31 +442,31 @@ template <int SHIFT, int W> __device__ __forceinline__ void policy_end(const Pol
   }
 }
 
-// 16 us for 42 MB, 2.6 TB/s: all waves are resident, and their phases follow one another: the search, the loads (8 us at a copy's
-// rate), two exponentials and two series a token, the sums. A third fewer instructions (bounds checks kept out of all tiles but
-// the last, inputs masked instead of terms) took as long.
-template <int SHIFT> __global__ __launch_bounds__(64 * GROUP) void k_policy_cells(PolicyParams p, int64_t cells) {
+// 15.5 us for 42 MB, 2.7 TB/s: all waves are resident, and their phases follow one another: the search, the loads, some 80
+// vector instructions a token, the sums; of its 10 us a wave waits 6.4 for memory and the workgroup. A kernel for each kind of
+// distance: as branches of each token, though alike for all, 16.2 (backward 13.4 for 12.3).
+template <int SHIFT, int KL> __global__ __launch_bounds__(64 * GROUP) void k_policy_cells(PolicyParams p, int64_t cells) {
   __shared__ CellSums<POLICY_SUMS, GROUP> s;
   const int64_t i0 = (int64_t)blockIdx.x * GROUP, i = i0 + (threadIdx.x >> 6);
-  if (i < cells) policy_cell<SHIFT>(p, i, s);
+  if (i < cells) policy_cell<KL, SHIFT>(p, i, s);
   leave(s, i0, cells, p.sums);
 }
 // 5.7 us, one workgroup's latencies; 7 with loads of 8 bytes, also of sums that are not there.
 template <int SHIFT> __global__ __launch_bounds__(END_THREADS) void k_policy_end(PolicyParams p) { policy_end<SHIFT, GROUP>(p, p.sums); }
 // All cells in one workgroup.
-__global__ __launch_bounds__(END_THREADS) void k_policy_small(PolicyParams p, int64_t cells) {
+template <int KL> __global__ __launch_bounds__(END_THREADS) void k_policy_small(PolicyParams p, int64_t cells) {
   __shared__ CellSums<POLICY_SUMS, FEW> s;
   __shared__ double sums[FEW * POLICY_SUMS];
   const int64_t i = threadIdx.x >> 6;
-  if (i < cells) policy_cell<ONE>(p, i, s);
+  if (i < cells) policy_cell<KL, ONE>(p, i, s);
   leave(s, 0, cells, sums);
   __syncthreads();
   policy_end<ONE, FEW>(p, sums);
 }
 
 // The terms again (their inputs are half the bytes of what they would be stored as), the derivative in fp32, rounded once a
-// product. 13 us for 50 MB, 3.8 TB/s; tiles of 512 tokens took as long.
-__global__ __launch_bounds__(256) void k_policy_backward(PolicyParams p, int64_t cells) {
+// product. 12 us for 50 MB, 4.1 TB/s; tiles of 512 tokens took as long.
+template <int KL> __global__ __launch_bounds__(256) void k_policy_backward(PolicyParams p, int64_t cells) {
   const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (i >= cells) return;
   const float all = p.weight[p.q.sequences] * *p.grad_loss;
@@ -464,14 +479,20 @@ __global__ __launch_bounds__(256) void k_policy_backward(PolicyParams p, int64_t
   float g[4] = {}, h[4] = {};
   if (in) {
     Four x;
-    const uint32_t mask = mask4(p.q, c, r);
-    fetch(p, c, r, each, x);
+    uint32_t mask;
+    if (c.left >= 1 << ONE) {
+      mask = mask4<true>(p.q, c, r);
+      fetch<KL, true>(p, c, r, each, x);
+    } else {
+      mask = mask4<false>(p.q, c, r);
+      fetch<KL, false>(p, c, r, each, x);
+    }
     const int on = live4(in, mask);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const Token y = policy_token(p, x.logp[j], x.old[j], x.ref[j], x.a[j]);
+      const Token y = policy_token<KL>(p, x.logp[j], x.old[j], x.ref[j], x.a[j]);
       const bool live = on >> j & 1;
-      g[j] = live ? (y.slope + (p.ref ? kl_coef * y.dkl : 0.f)) * w : 0.f;
+      g[j] = live ? (y.slope + (KL != NO_REF ? kl_coef * y.dkl : 0.f)) * w : 0.f;
       h[j] = live ? bonus : 0.f;
     }
   }
@@ -484,23 +505,42 @@ __global__ __launch_bounds__(256) void k_policy_backward(PolicyParams p, int64_t
 #define ON_CELLS(kernel, st, ...) \
   hipLaunchKernelGGL(kernel, dim3((uint32_t)((cells + 3) / 4)), dim3(256), 0, st, __VA_ARGS__, cells)
 // Both steps of a forward pass over cells of 2^SHIFT tokens: two launches, or one where there are few cells.
-#define FORWARD(name, SHIFT)                                                                                \
+#define FORWARD(SMALL, CELLS, END, SHIFT)                                                                   \
   do {                                                                                                      \
     const int64_t cells = cells_of_all(p.q, SHIFT);                                                         \
-    if (SHIFT == ONE && cells <= FEW)   {                                                                   \
-      hipLaunchKernelGGL(k_##name##_small, dim3(1), dim3(END_THREADS), 0, st, p, cells);                    \
+    if (SHIFT == ONE && cells <= FEW) {                                                                     \
+      SMALL(dim3(1), dim3(END_THREADS), 0, st, p, cells);                                                   \
       return hipGetLastError();                                                                             \
     }                                                                                                       \
-    hipLaunchKernelGGL(k_##name##_cells<SHIFT>, dim3((uint32_t)((cells + GROUP - 1) / GROUP)), dim3(64 * GROUP), 0, st, p, \
-                       cells);                                                                              \
+    CELLS(SHIFT, dim3((uint32_t)((cells + GROUP - 1) / GROUP)), dim3(64 * GROUP), 0, st, p, cells);         \
     const hipError_t e = hipGetLastError();                                                                 \
     if (e != hipSuccess) return e;                                                                          \
-    hipLaunchKernelGGL(k_##name##_end<SHIFT>, dim3(1), dim3(END_THREADS), 0, st, p);                        \
+    hipLaunchKernelGGL(END<SHIFT>, dim3(1), dim3(END_THREADS), 0, st, p);                                   \
     return hipGetLastError();                                                                               \
+  } while (0)
+#define PREFERENCE_SMALL(...) hipLaunchKernelGGL(k_preference_small, __VA_ARGS__)
+#define PREFERENCE_CELLS(SHIFT, ...) hipLaunchKernelGGL(k_preference_cells<SHIFT>, __VA_ARGS__)
+// A kernel for each kind of distance: decided for each token, even alike for all, the branches were a third of the work.
+#define POLICY_SMALL(...)                                                                \
+  do {                                                                                   \
+    if (!p.ref) hipLaunchKernelGGL(k_policy_small<NO_REF>, __VA_ARGS__);                 \
+    else if (p.kl == 0) hipLaunchKernelGGL(k_policy_small<0>, __VA_ARGS__);              \
+    else if (p.kl == 1) hipLaunchKernelGGL(k_policy_small<1>, __VA_ARGS__);              \
+    else hipLaunchKernelGGL(k_policy_small<2>, __VA_ARGS__);                             \
+  } while (0)
+#define POLICY_CELLS(SHIFT, ...)                                                         \
+  do {                                                                                   \
+    if (!p.ref) hipLaunchKernelGGL((k_policy_cells<SHIFT, NO_REF>), __VA_ARGS__);        \
+    else if (p.kl == 0) hipLaunchKernelGGL((k_policy_cells<SHIFT, 0>), __VA_ARGS__);     \
+    else if (p.kl == 1) hipLaunchKernelGGL((k_policy_cells<SHIFT, 1>), __VA_ARGS__);     \
+    else hipLaunchKernelGGL((k_policy_cells<SHIFT, 2>), __VA_ARGS__);                    \
   } while (0)
 
 hipError_t launch_preference(const PreferenceParams& p, hipStream_t st) {
-  if (p.q.tokens > LOSS_FEW_TOKENS) FORWARD(preference, LOSS_CELL_SHIFT); else FORWARD(preference, ONE);
+  if (p.q.tokens > LOSS_FEW_TOKENS)
+    FORWARD(PREFERENCE_SMALL, PREFERENCE_CELLS, k_preference_end, LOSS_CELL_SHIFT);
+  else
+    FORWARD(PREFERENCE_SMALL, PREFERENCE_CELLS, k_preference_end, ONE);
 }
 hipError_t launch_preference_backward(const Packed& q, const float* slope, const float* grad_loss, float* grad, hipStream_t st) {
   const int64_t cells = cells_of_all(q, ONE);
@@ -508,10 +548,16 @@ hipError_t launch_preference_backward(const Packed& q, const float* slope, const
   return hipGetLastError();
 }
 hipError_t launch_policy(const PolicyParams& p, hipStream_t st) {
-  if (p.q.tokens > LOSS_FEW_TOKENS) FORWARD(policy, LOSS_CELL_SHIFT); else FORWARD(policy, ONE);
+  if (p.q.tokens > LOSS_FEW_TOKENS)
+    FORWARD(POLICY_SMALL, POLICY_CELLS, k_policy_end, LOSS_CELL_SHIFT);
+  else
+    FORWARD(POLICY_SMALL, POLICY_CELLS, k_policy_end, ONE);
 }
 hipError_t launch_policy_backward(const PolicyParams& p, hipStream_t st) {
   const int64_t cells = cells_of_all(p.q, ONE);
-  ON_CELLS(k_policy_backward, st, p);
+  if (!p.ref) ON_CELLS(k_policy_backward<NO_REF>, st, p);
+  else if (p.kl == 0) ON_CELLS(k_policy_backward<0>, st, p);
+  else if (p.kl == 1) ON_CELLS(k_policy_backward<1>, st, p);
+  else ON_CELLS(k_policy_backward<2>, st, p);
   return hipGetLastError();
 }
