@@ -254,10 +254,11 @@ __global__ __launch_bounds__(256) void k_logps_backward(LogpsParams p, uint32_t 
   }
 }
 
-// Logits that do not fit the memory-side cache go past the caches: forward 8192 x 32000 bf16 84 us instead of 96, 4096 x
-// 131072 fp32 312 and 340 (8192 x 16384 bf16, 268 MB, 45 and 43); backward 8192 x 32000 bf16 173 and 208, 4096 x 131072 340 and
-// 369; where the logits alone would fit, gradients only: 16384 x 4096 fp32 80 and 94, with the logits past them too 86.
-constexpr double CACHE = 256 << 20;
+// Logits that are well over the memory-side cache (256 MiB) go past the caches, gradients where both are. Rows of 32000 bf16,
+// both ways one after another, us, through the caches and past them: 250 MiB 122 and 134, 280 MiB 141 and 150, 300 MiB 160 and
+// 160, 330 MiB 186 and 176, 420 MiB 236 and 219; 8192 x 32000 96 + 208 and 84 + 173. Gradients only past them: 183 MiB 95 and
+// 99 through, 122 MiB 67 either way.
+constexpr double CACHE = 300 << 20;
 template <typename T> double bytes_of(const LogpsParams& p) { return (double)p.tokens * (double)p.vocab * sizeof(T); }
 constexpr int64_t MOST_GROUPS = 1 << 21;        // workgroups of a launch: fewer than 2^32 threads
 
