@@ -563,6 +563,8 @@ int moara_preference_loss_backward(const float* slope, const float* grad_loss, c
                                    const int64_t* offsets, int64_t sequences, float* out_grad, void* stream);
 
 enum { MOARA_KL_EXP = 0, MOARA_KL_LINEAR = 1, MOARA_KL_SQUARE = 2 };
+/* Another name of EXP: q^2 / 2 + q^3 / 6 + .., which leaves the SQUARE at the cubic term. */
+enum { MOARA_KL_CUBIC = MOARA_KL_EXP };
 enum { MOARA_MEAN_TOKENS = 0, MOARA_MEAN_SEQUENCES = 1 };
 
 typedef struct {

@@ -34,6 +34,7 @@ MOARA_SOFTMAX, MOARA_SIGMOID = 0, 1
 MOARA_GRAD_NORM_WORKSPACE = 16384
 MOARA_PREF_SIGMOID, MOARA_PREF_HINGE, MOARA_PREF_SQUARE = range(3)
 MOARA_KL_EXP, MOARA_KL_LINEAR, MOARA_KL_SQUARE = range(3)
+MOARA_KL_CUBIC = MOARA_KL_EXP      # another name of it: q^2 / 2 + q^3 / 6 + .., the square but for the cubic term on
 MOARA_MEAN_TOKENS, MOARA_MEAN_SEQUENCES = 0, 1
 
 EXPORTED = (

@@ -465,3 +465,37 @@ def test_losses_are_scalars_of_their_own(calls):
     (2 * loss).backward()
     with pytest.raises(RuntimeError):
         torch.autograd.grad(torch.autograd.grad(L.preference_loss(cfg, x)[0], x, create_graph=True)[0].sum(), x)
+
+
+# ---------------------------------------------------------------- the performance cases
+
+def _cases():
+    import importlib.util
+    import random
+    from tests.conftest import ROOT
+    spec = importlib.util.spec_from_file_location("more_operators", os.path.join(ROOT, "perf", "more_operators.py"))
+    cases = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(cases)
+    r = random.Random(5)
+    return cases, cases.listed() + [cases.draw(r) for _ in range(300)]
+
+
+def test_the_performance_cases_name_what_the_library_has(lib):
+    """Every listed case and drawn ones get the configuration that they describe."""
+    assert M.MOARA_KL_CUBIC == M.MOARA_KL_EXP
+    cases, every = _cases()
+    seen = set()
+    for case in every:
+        if case["op"] in ("logps",):
+            continue
+        cfg = cases._config(case)
+        if case["op"] in ("policy", "policy_step"):
+            kl = case.get("kl", "exp")
+            seen.add(kl)
+            assert cfg.kl == {"linear": M.MOARA_KL_LINEAR, "square": M.MOARA_KL_SQUARE}.get(kl, M.MOARA_KL_EXP)
+            assert cfg.kl_coef == (0 if kl == "none" else case.get("kl_coef", 0.04))
+        elif case["op"] == "preference":
+            assert (cfg.beta, cfg.margin, cfg.smoothing, cfg.average) == (case["beta"], case["margin"], case["smoothing"], case["average"])
+        else:
+            assert (cfg.experts, cfg.top_k, cfg.z_coef) == (case["experts"], case["top_k"], case["z_coef"])
+    assert len(seen) >= 4
