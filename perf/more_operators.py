@@ -47,9 +47,9 @@ def _preference(name, pairs, tokens, kind="sigmoid", average=False, smoothing=0.
                 margin=margin, beta=beta, reference=reference, mask=mask, padded=padded, tail=tail)
 
 
-def _policy(name, sequences, tokens, reduce="tokens", per_sequence=True, kl="exp", kl_coef=0.04, entropy_coef=0.0,
+def _policy(name, sequences, tokens, reduce="tokens", per_sequence=True, kl="cubic", kl_coef=0.04, entropy_coef=0.0,
             old=True, mask=True, padded=False, tail=0):
-    """kl: of the distance's estimators e^q - q - 1 (exp), logp - ref (linear), its half square (square), or none."""
+    """kl: of the distance's estimators e^q - q - 1 (cubic), logp - ref (linear), its half square (square), or none."""
     return dict(name=name, op="policy", sequences=sequences, tokens=tokens, reduce=reduce, per_sequence=per_sequence, kl=kl,
                 kl_coef=kl_coef, entropy_coef=entropy_coef, old=old, mask=mask, padded=padded, tail=tail)
 
@@ -129,7 +129,7 @@ def draw(rng):
     if padded:
         tokens = tokens // count * count
     return _policy("", count, tokens, rng.choice(["tokens", "sequences"]), rng.random() < 0.6,
-                   rng.choice(["exp", "linear", "square", "none"]), rng.choice([0.001, 0.04, 0.2]), rng.choice([0.0, 0.01]),
+                   rng.choice(["cubic", "linear", "square", "none"]), rng.choice([0.001, 0.04, 0.2]), rng.choice([0.0, 0.01]),
                    rng.random() < 0.8, padded or rng.random() < 0.6, padded, 0 if padded else rng.choice([0, 0, min(77, tokens // 4)]))
 
 
@@ -253,9 +253,9 @@ def _config(case):
         score = M.MOARA_SIGMOID if case["score"] == "sigmoid" else M.MOARA_SOFTMAX
         return M.moara_balance_default_config(experts=case["experts"], top_k=case["top_k"], score=score, balance_coef=0.01,
                                               z_coef=case["z_coef"])
-    kl = {"exp": M.MOARA_KL_EXP, "linear": M.MOARA_KL_LINEAR, "square": M.MOARA_KL_SQUARE, "none": M.MOARA_KL_EXP}
+    kl = {"cubic": M.MOARA_KL_CUBIC, "linear": M.MOARA_KL_LINEAR, "square": M.MOARA_KL_SQUARE, "none": M.MOARA_KL_CUBIC}
     reduce = M.MOARA_MEAN_SEQUENCES if case.get("reduce") == "sequences" else M.MOARA_MEAN_TOKENS
-    return M.moara_policy_default_config(clip_low=CLIP_LOW, clip_high=CLIP_HIGH, kl=kl[case.get("kl", "exp")],
+    return M.moara_policy_default_config(clip_low=CLIP_LOW, clip_high=CLIP_HIGH, kl=kl[case.get("kl", "cubic")],
                                          kl_coef=0.0 if case.get("kl") == "none" else case.get("kl_coef", 0.04),
                                          entropy_coef=case.get("entropy_coef", 0.01), reduce=reduce,
                                          sequence_advantages=int(case.get("per_sequence", True)))
@@ -442,7 +442,7 @@ def _policy_terms(case, logp, old, ref, entropy, advantages, seq, on, count, off
         far, dfar = torch.zeros_like(logp), torch.zeros_like(logp)
     else:
         q = ref.double() - logp.double()
-        if case.get("kl", "exp") == "exp":
+        if case.get("kl", "cubic") == "cubic":
             far, dfar = _low(q), -torch.expm1(q)
         elif case["kl"] == "linear":
             far, dfar = -q, torch.ones_like(q)
@@ -637,8 +637,8 @@ def _exact_policy_loss(case, st, logp, entropy, seq, live, count):
     far = torch.zeros_like(d)
     if st.ref is not None:
         q = st.ref.flatten().double() - logp
-        kind = case.get("kl", "exp")
-        far = q.expm1() - q if kind == "exp" else -q if kind == "linear" else q.square() / 2
+        kind = case.get("kl", "cubic")
+        far = q.expm1() - q if kind == "cubic" else -q if kind == "linear" else q.square() / 2
     n = _total(torch.ones_like(d), seq, live, count)
     if case.get("reduce") == "sequences":
         w = 1 / n.clamp(min=1)[seq] / max(1, int((n > 0).sum()))
