@@ -491,6 +491,7 @@ int moara_route_balance(int32_t experts, int64_t* counts, float* bias, float rat
  * left out, as are tokens before the first and behind the last sequence: whatever values they
  * have, they add nothing, and their gradients are 0. What is outside [0, tokens) is never read
  * or written, whatever the offsets are; offsets that fall give sums of some of the tokens.
+ * Without tokens (tokens 0) the inputs, the sequences' advantages among them, may be null.
  * out_loss: one float, or null: the loss, out[0], once more, for callers that keep it by itself.
  * ------------------------------------------------------------------------------------ */
 

@@ -354,7 +354,7 @@ __device__ __forceinline__ void fetch(const PolicyParams& p, const Span& c, int 
 template <int KL, int SHIFT, bool WHOLE>
 __device__ __forceinline__ void policy_sums(const PolicyParams& p, const Span& c, double (&sum)[POLICY_SUMS]) {
   constexpr int TURNS = 1 << (SHIFT - ONE);
-  const float each = p.sequence_advantages && c.seq >= 0 ? p.advantages[c.seq] : 0.f;
+  const float each = p.sequence_advantages && c.begin < c.end ? p.advantages[c.seq] : 0.f;    // there may be none of no tokens
   int count = 0, clipped = 0;
   Four x[TURNS];
   float entropy[TURNS][4];
@@ -472,7 +472,7 @@ template <int KL> __global__ __launch_bounds__(256) void k_policy_backward(Polic
   const float all = p.weight[p.q.sequences] * *p.grad_loss;
   const Span c = span_of<ONE>(p.q, i);
   const int r = 4 * (threadIdx.x & 63);
-  const float each = p.sequence_advantages && c.seq >= 0 ? p.advantages[c.seq] : 0.f;
+  const float each = p.sequence_advantages && c.begin < c.end ? p.advantages[c.seq] : 0.f;
   const float w = c.seq >= 0 ? p.weight[c.seq] * all : 0.f;
   const float kl_coef = (float)p.kl_coef, bonus = -(float)p.entropy_coef * w;
   const int in = inside4(c, r);

@@ -1059,3 +1059,24 @@ def test_the_training_example_with_a_balance_loss():
     spec.loader.exec_module(ex)
     losses, share = ex.train(steps=3, balance_loss=0.1, say=lambda s: print("[moe]", s, flush=True))
     assert all(math.isfinite(x) for x in losses) and len(share) == 2
+
+
+# ---------------------------------------------------------------- calls at the edges
+
+@pytest.mark.parametrize("S", [1, 2, 6, 600, 5000])
+@pytest.mark.parametrize("packed", [False, True])
+def test_policy_of_no_tokens_needs_no_inputs(S, packed):
+    """Sequences without a token: no pointer of an input is needed, that of the sequences' advantages neither; all is 0."""
+    import ctypes
+    M = _M()
+    offsets = torch.zeros(S + 1, dtype=torch.int64, device="cuda") if packed else None
+    out, loss, weight = (torch.full((n,), 7.0, device="cuda") for n in (6, 1, S + 1))
+    work = torch.full((6 * (S + 130),), math.nan, dtype=torch.float64, device="cuda")
+    for whole in (0, 1):
+        cfg = M.moara_policy_default_config(sequence_advantages=whole, reduce=whole)
+        status = M.lib().moara_policy_loss(ctypes.byref(cfg), None, None, None, None, None, None, 0, offsets.data_ptr() if packed else None,
+                                           S, out.data_ptr(), loss.data_ptr(), weight.data_ptr(), work.data_ptr(), None)
+        torch.cuda.synchronize()
+        assert status == M.MOARA_OK and not out.any() and not loss.any() and not weight.any()
+        for t in (out, loss, weight):
+            t.fill_(7.0)
