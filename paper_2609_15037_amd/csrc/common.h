@@ -8,6 +8,14 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
+// A load and a store through a pointer, past the caches (non-temporal) where `once`. Macros, as a function's template parameter
+// would drop the lower alignment that a typedef gives a vector, and the access be compiled for the vector's own.
+#define GET(once, q) ((once) ? __builtin_nontemporal_load(q) : *(q))
+#define PUT(once, q, x)                                             \
+  do {                                                              \
+    if (once) __builtin_nontemporal_store(x, q); else *(q) = (x);   \
+  } while (0)
+
 enum { SIDE_LEFT = 1, SIDE_RIGHT = 2 };
 
 // ---------------------------------------------------------------- descriptors

@@ -19,17 +19,11 @@ typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32x4h __attribute__((ext_vector_type(4), aligned(2)));
 // Sixteen bytes a lane, 4 fp32 or 8 bf16, of any alignment; ONCE: past the caches. A vector is loaded as it is and taken
 // apart later: taken apart where it may not exist, each load would be waited for before the next.
-template <bool ONCE, typename V> __device__ __forceinline__ u32x4 get(const V* q) {
-  return ONCE ? __builtin_nontemporal_load(q) : *q;
-}
-template <bool ONCE, typename V> __device__ __forceinline__ void put(V* q, const V& x) {
-  if (ONCE) __builtin_nontemporal_store(x, q); else *q = x;
-}
 template <bool ONCE> __device__ __forceinline__ u32x4 load(const float* q) {
-  return get<ONCE>(reinterpret_cast<const u32x4u*>(q));
+  return GET(ONCE, reinterpret_cast<const u32x4u*>(q));
 }
 template <bool ONCE> __device__ __forceinline__ u32x4 load(const bf16* q) {
-  return get<ONCE>(reinterpret_cast<const u32x4h*>(q));
+  return GET(ONCE, reinterpret_cast<const u32x4h*>(q));
 }
 template <typename T> __device__ __forceinline__ u32x4 nothing() {      // -inf
   const uint32_t x = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
@@ -47,14 +41,14 @@ template <bool ONCE> __device__ __forceinline__ void store(float* q, const float
   u32x4u a;
 #pragma unroll
   for (int j = 0; j < 4; ++j) a[j] = __float_as_uint(x[j]);
-  put<ONCE>(reinterpret_cast<u32x4u*>(q), a);
+  PUT(ONCE, reinterpret_cast<u32x4u*>(q), a);
 }
 template <bool ONCE> __device__ __forceinline__ void store(bf16* q, const float (&x)[8]) {
   u32x4h a;
 #pragma unroll
   for (int j = 0; j < 4; ++j)
     a[j] = (uint32_t)__builtin_bit_cast(uint16_t, f2bf(x[2 * j + 1])) << 16 | __builtin_bit_cast(uint16_t, f2bf(x[2 * j]));
-  put<ONCE>(reinterpret_cast<u32x4h*>(q), a);
+  PUT(ONCE, reinterpret_cast<u32x4h*>(q), a);
 }
 __device__ __forceinline__ void store1(float* q, float x) { *q = x; }
 __device__ __forceinline__ void store1(bf16* q, float x) { *q = f2bf(x); }

@@ -499,3 +499,19 @@ def test_the_performance_cases_name_what_the_library_has(lib):
         else:
             assert (cfg.experts, cfg.top_k, cfg.z_coef) == (case["experts"], case["top_k"], case["z_coef"])
     assert len(seen) >= 4
+
+
+# ---------------------------------------------------------------- alignment of vector accesses
+
+@pytest.mark.parametrize("source", ["logps.hip", "loss.hip", "balance.hip"])
+def test_vectors_are_accessed_with_the_alignment_they_are_declared_with(source):
+    """Rows begin at any element. An access that the compiler takes for more aligned than its pointer's type is an error."""
+    import subprocess
+    from paper_2609_15037_amd import build
+    try:
+        hipcc = build.hipcc()
+    except RuntimeError:
+        pytest.skip("no hipcc")
+    r = subprocess.run([hipcc, *build._flags(), "-Werror=align-mismatch", "--cuda-device-only", "-fsyntax-only",
+                        os.path.join(build.CSRC, source)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-2000:]
