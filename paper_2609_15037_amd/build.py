@@ -32,7 +32,7 @@ def hipcc() -> str:
 def _flags():
     return ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-            "-Wno-unused-result", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
+            "-Wno-unused-result", "-Werror=align-mismatch", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 
 
 def _compile(src: str, build_dir: str) -> str:

@@ -12,19 +12,12 @@ typedef uint32_t u32u __attribute__((aligned(1)));
 typedef uint16_t u16u __attribute__((aligned(1)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-// ONCE: the line is not needed again soon (non-temporal).
-template <bool ONCE, typename T> __device__ __forceinline__ T get(const T* q) {
-  return ONCE ? __builtin_nontemporal_load(q) : *q;
-}
-template <bool ONCE, typename T> __device__ __forceinline__ void put(T* q, T x) {
-  if (ONCE) __builtin_nontemporal_store(x, q); else *q = x;
-}
-
-// N consecutive elements (4, or 8 of bf16); `left` of them exist, the others read as zero and are not written.
+// N consecutive elements (4, or 8 of bf16); `left` of them exist, the others read as zero and are not written. ONCE: the line is
+// not needed again soon.
 template <bool ONCE, int N> __device__ __forceinline__ void load(const float* q, int64_t left, float (&x)[N]) {
   static_assert(N == 4);
   if (left >= N) {
-    const f32x4u a = get<ONCE>(reinterpret_cast<const f32x4u*>(q));
+    const f32x4u a = GET(ONCE, reinterpret_cast<const f32x4u*>(q));
 #pragma unroll
     for (int j = 0; j < N; ++j) x[j] = a[j];
   } else {
@@ -35,7 +28,7 @@ template <bool ONCE, int N> __device__ __forceinline__ void load(const float* q,
 template <bool ONCE, int N> __device__ __forceinline__ void load(const bf16* q, int64_t left, float (&x)[N]) {
   typedef uint16_t vec __attribute__((ext_vector_type(N), aligned(2)));
   if (left >= N) {
-    const vec a = get<ONCE>(reinterpret_cast<const vec*>(q));
+    const vec a = GET(ONCE, reinterpret_cast<const vec*>(q));
 #pragma unroll
     for (int j = 0; j < N; ++j) x[j] = __uint_as_float((uint32_t)a[j] << 16);
   } else {
@@ -46,7 +39,7 @@ template <bool ONCE, int N> __device__ __forceinline__ void load(const bf16* q, 
 template <bool ONCE, int N> __device__ __forceinline__ void store(float* q, int64_t left, const float (&x)[N]) {
   static_assert(N == 4);
   if (left >= N) {
-    put<ONCE>(reinterpret_cast<f32x4u*>(q), f32x4u{x[0], x[1], x[2], x[3]});
+    PUT(ONCE, reinterpret_cast<f32x4u*>(q), (f32x4u{x[0], x[1], x[2], x[3]}));
   } else {
 #pragma unroll
     for (int j = 0; j < N; ++j) if (j < left) q[j] = x[j];
@@ -58,7 +51,7 @@ template <bool ONCE, int N> __device__ __forceinline__ void store(bf16* q, int64
     vec a;
 #pragma unroll
     for (int j = 0; j < N; ++j) a[j] = __builtin_bit_cast(uint16_t, f2bf(x[j]));
-    put<ONCE>(reinterpret_cast<vec*>(q), a);
+    PUT(ONCE, reinterpret_cast<vec*>(q), a);
   } else {
 #pragma unroll
     for (int j = 0; j < N; ++j) if (j < left) q[j] = f2bf(x[j]);
@@ -286,8 +279,8 @@ __device__ __forceinline__ void chunk8(const AdamwTensor& T, const AdamwList& L,
     load<true>((const PT*)T.p + e, left, p);
     load<true>((const GT*)T.g + e, left, g);
     if (left >= 4) {
-      mc = get<true>(reinterpret_cast<const u32u*>(mq));
-      vc = get<true>(reinterpret_cast<const u32u*>(vq));
+      mc = GET(true, reinterpret_cast<const u32u*>(mq));
+      vc = GET(true, reinterpret_cast<const u32u*>(vq));
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -345,8 +338,8 @@ __device__ __forceinline__ void chunk8(const AdamwTensor& T, const AdamwList& L,
   if (left <= 0) return;
   store<true>((PT*)T.p + e, left, p);
   if (left >= 4) {
-    put<true>(reinterpret_cast<u32u*>(mq), (u32u)co);
-    put<true>(reinterpret_cast<u32u*>(vq), (u32u)cv);
+    PUT(true, reinterpret_cast<u32u*>(mq), (u32u)co);
+    PUT(true, reinterpret_cast<u32u*>(vq), (u32u)cv);
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j)

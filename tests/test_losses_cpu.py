@@ -503,7 +503,7 @@ def test_the_performance_cases_name_what_the_library_has(lib):
 
 # ---------------------------------------------------------------- alignment of vector accesses
 
-@pytest.mark.parametrize("source", ["logps.hip", "loss.hip", "balance.hip"])
+@pytest.mark.parametrize("source", ["logps.hip", "loss.hip", "balance.hip", "route.hip", "adamw.hip"])
 def test_vectors_are_accessed_with_the_alignment_they_are_declared_with(source):
     """Rows begin at any element. An access that the compiler takes for more aligned than its pointer's type is an error."""
     import subprocess
