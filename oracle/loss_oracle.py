@@ -106,8 +106,9 @@ def policy_terms(logp, old, ref, adv, low, high, kl="exp"):
         d = np.zeros_like(logp) if old is None else logp - old
         r = np.exp(d)
         clipped = ((r > 1 + high) & (adv > 0)) | ((r < 1 - low) & (adv < 0))
-        gain = np.where(clipped, np.where(adv > 0, 1 + high, 1 - low), r) * adv
-        slope = np.where(clipped, 0.0, r * adv)
+        none = (adv == 0) & ~np.isnan(r)        # no part, whatever the ratio
+        gain = np.where(none, 0.0, np.where(clipped, np.where(adv > 0, 1 + high, 1 - low), r) * adv)
+        slope = np.where(clipped | none, 0.0, r * adv)
         if ref is None:
             far = dfar = np.zeros_like(logp)
         else:

@@ -331,8 +331,9 @@ template <int KL> __device__ __forceinline__ Token policy_token(const PolicyPara
   const float df = (float)d, ratio = exp_of(df);
   const bool up = d > p.high && a > 0, down = d < p.low && a < 0;
   t.clipped = up || down;
-  t.gain = (up ? p.at_high : down ? p.at_low : ratio) * a;
-  t.slope = t.clipped ? 0.f : -ratio * a;
+  const bool none = a == 0 && df == df;         // an advantage of 0 has no part where the ratio overflows either; a NaN has
+  t.gain = none ? 0.f : (up ? p.at_high : down ? p.at_low : ratio) * a;
+  t.slope = t.clipped || none ? 0.f : -ratio * a;
   t.excess = exp_excess(df, ratio);
   const float q = KL == NO_REF ? 0.f : (float)((double)ref - (double)logp), e = KL == 0 ? exp_of(q) : 0.f;
   const float far = KL == 0 ? exp_excess(q, e) : 0.f;

@@ -1080,3 +1080,39 @@ def test_policy_of_no_tokens_needs_no_inputs(S, packed):
         assert status == M.MOARA_OK and not out.any() and not loss.any() and not weight.any()
         for t in (out, loss, weight):
             t.fill_(7.0)
+
+
+def _large(x, T):
+    """The tokens of a small case and, from there on, ones whose terms are all 0: of the sizes that take other kernels."""
+    y = torch.zeros(1, T, device="cuda")
+    y[:, :x.shape[-1]] = x
+    return y
+
+
+@pytest.mark.parametrize("T", [8, 3000, 70001])
+@pytest.mark.parametrize("reduce", [0, 1])
+def test_policy_of_an_advantage_of_zero(T, reduce):
+    """It has no part in the loss and no gradient, also where its ratio overflows, of the tokens' advantages and of a whole
+    sequence's; a NaN among its log-probabilities stays one."""
+    M = _M()
+    logp = _large(torch.tensor([0.0, 0.0, -200.0, 0.5, 100.0]), T)
+    old = _large(torch.tensor([-200.0, -math.inf, 0.0, 0.4, 0.0]), T)
+    adv = _large(torch.tensor([0.0, -0.0, 0.0, -2.0, 0.0]), T)
+    one = torch.ones(1, device="cuda")
+    cfg = M.moara_policy_default_config(reduce=reduce)
+    out, w = M.moara_policy_loss(cfg, logp, adv, old_logp=old)
+    grad, _ = M.moara_policy_loss_backward(cfg, logp, adv, w, one, old_logp=old)
+    d = float(logp[0, 3].double() - old[0, 3].double())
+    want = 2 * math.exp(d) / T          # one token with a part: its ratio (6 u and |d| u), product, weight, rounding
+    assert float(out[0]) == pytest.approx(want, rel=16 * U) and float(out[1]) == float(out[0])
+    assert float(grad[0, 3]) == pytest.approx(want, rel=16 * U)
+    grad[0, 3] = 0
+    assert not grad.any()
+    whole = M.moara_policy_default_config(reduce=reduce, sequence_advantages=1)
+    out, w = M.moara_policy_loss(whole, logp, torch.zeros(1, device="cuda"), old_logp=old)
+    grad, _ = M.moara_policy_loss_backward(whole, logp, torch.zeros(1, device="cuda"), w, one, old_logp=old)
+    assert float(out[0]) == 0 and float(out[1]) == 0 and not grad.any()
+    logp[0, 1] = math.nan
+    out, w = M.moara_policy_loss(cfg, logp, adv, old_logp=old)
+    grad, _ = M.moara_policy_loss_backward(cfg, logp, adv, w, one, old_logp=old)
+    assert out[0].isnan() and grad[0, 1].isnan() and torch.isfinite(grad[0, [0, 2, 3, 4]]).all()
