@@ -589,6 +589,7 @@ int moara_policy_default_config(moara_policy_config* out);
  * and with w its weight in the mean, the loss is sum w (-gain + kl_coef kl - entropy_coef entropy).
  * Whether a token is clipped (r beyond the bound on the side that A pushes to) is decided in 64 bits.
  * An advantage of 0 adds nothing, whatever the ratio (but for a NaN).
+ * A coefficient of 0 leaves its term out of the loss and the gradients, whatever out says of it.
  * out: 6 floats: the loss, sum -w gain, sum w kl, sum w entropy, sum w [clipped], sum w (e^d - d - 1)
  *      (the distance to the old policy). 0 where no token is left.
  * out_weight: sequences + 1 floats: w of a sequence's tokens (0 where it has none) is weight[s]

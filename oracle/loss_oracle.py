@@ -137,8 +137,9 @@ def policy(logp, old, ref, adv, entropy, seqs, low=0.2, high=0.2, kl="exp", kl_c
     on = w > 0
     mean = lambda x: math.fsum((w * np.where(on, x, 0.0))[on])  # noqa: E731
     policy_, kl_, ent = -mean(gain), mean(far), 0.0 if entropy is None else mean(entropy)
-    out = np.array([policy_ + kl_coef * kl_ - entropy_coef * ent, policy_, kl_, ent, mean(clipped), mean(moved)])
-    return out, weight, np.where(on, w * (kl_coef * np.where(on, dfar, 0) - np.where(on, slope, 0)), 0.0), \
+    times = lambda c, x: c * x if c else 0.0  # noqa: E731     a coefficient of 0 leaves its term out, whatever it is
+    out = np.array([policy_ + times(kl_coef, kl_) - times(entropy_coef, ent), policy_, kl_, ent, mean(clipped), mean(moved)])
+    return out, weight, np.where(on, w * (times(kl_coef, np.where(on, dfar, 0)) - np.where(on, slope, 0)), 0.0), \
         np.where(on, -entropy_coef * w, 0.0)
 
 

@@ -431,7 +431,9 @@ template <int SHIFT, int W> __device__ __forceinline__ void policy_end(const Pol
   if (threadIdx.x == 0) {
     const double over = p.divisor > 0 ? p.divisor : p.by_sequence ? all[POLICY_SUMS] : all[0], share = over > 0 ? 1 / over : 0;
     const double policy = all[1] * share, kl = all[2] * share, entropy = all[3] * share;
-    const float loss = (float)(policy + (p.ref ? p.kl_coef * kl : 0) - (p.entropy ? p.entropy_coef * entropy : 0));
+    // a coefficient of 0 leaves its term out, also where that is not finite
+    const float loss = (float)(policy + (p.ref && p.kl_coef != 0 ? p.kl_coef * kl : 0) -
+                               (p.entropy && p.entropy_coef != 0 ? p.entropy_coef * entropy : 0));
     p.out[0] = loss;
     if (p.loss) *p.loss = loss;
     p.out[1] = (float)policy;
@@ -556,7 +558,7 @@ hipError_t launch_policy(const PolicyParams& p, hipStream_t st) {
 }
 hipError_t launch_policy_backward(const PolicyParams& p, hipStream_t st) {
   const int64_t cells = cells_of_all(p.q, ONE);
-  if (!p.ref) ON_CELLS(k_policy_backward<NO_REF>, st, p);
+  if (!p.ref || (float)p.kl_coef == 0) ON_CELLS(k_policy_backward<NO_REF>, st, p);
   else if (p.kl == 0) ON_CELLS(k_policy_backward<0>, st, p);
   else if (p.kl == 1) ON_CELLS(k_policy_backward<1>, st, p);
   else ON_CELLS(k_policy_backward<2>, st, p);

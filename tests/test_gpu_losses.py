@@ -1116,3 +1116,26 @@ def test_policy_of_an_advantage_of_zero(T, reduce):
     out, w = M.moara_policy_loss(cfg, logp, adv, old_logp=old)
     grad, _ = M.moara_policy_loss_backward(cfg, logp, adv, w, one, old_logp=old)
     assert out[0].isnan() and grad[0, 1].isnan() and torch.isfinite(grad[0, [0, 2, 3, 4]]).all()
+
+
+@pytest.mark.parametrize("T", [8, 3000, 70001])
+@pytest.mark.parametrize("kl", ["exp", "linear", "square"])
+def test_policy_terms_with_a_coefficient_of_zero(T, kl):
+    """Distances and entropies that are only reported leave the loss and the gradients, bit by bit, as they are without."""
+    M = _M()
+    r = rng(41, T)
+    logp, old, adv = (_gpu(r.standard_normal((2, T)), F32) for _ in range(3))
+    ref = logp + 0.1
+    ref[0, :3] = torch.tensor([150.0, -math.inf, math.inf], device="cuda")
+    ref[1, 5] = math.nan
+    H = torch.ones(2, T, device="cuda")
+    H[1, 2], H[0, 1] = math.inf, math.nan
+    one = torch.ones(1, device="cuda")
+    cfg = _policy_cfg(M, dict(kl=kl))
+    plain, w0 = M.moara_policy_loss(cfg, logp, adv, old_logp=old)
+    g0, _ = M.moara_policy_loss_backward(cfg, logp, adv, w0, one, old_logp=old)
+    out, w = M.moara_policy_loss(cfg, logp, adv, old_logp=old, ref_logp=ref, entropy=H)
+    g, h = M.moara_policy_loss_backward(cfg, logp, adv, w, one, old_logp=old, ref_logp=ref, entropy=H)
+    assert torch.isfinite(plain).all() and torch.equal(w, w0)
+    assert torch.equal(out[[0, 1, 4, 5]], plain[[0, 1, 4, 5]]) and out[2:4].isnan().all()       # the reports say what there is
+    assert torch.equal(g, g0) and not h.any()
