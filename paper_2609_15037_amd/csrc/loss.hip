@@ -226,7 +226,8 @@ template <int SHIFT, int W> __device__ __forceinline__ void preference_end(const
       if (p.kind == 0) {
         // log(1 + e^-z) = max(-z, 0) + log(1 + u), u = e^-|z|, and the same of z; 1 / (1 + e^z) from u too
         const double u = exp(-fabs(z)), log = log1p(u), y = 1 / (1 + u);
-        l = (1 - p.smoothing) * (fmax(-z, 0.0) + log) + (p.smoothing != 0 ? p.smoothing * (fmax(z, 0.0) + log) : 0);
+        l = (p.smoothing != 1 ? (1 - p.smoothing) * (fmax(-z, 0.0) + log) : 0) +
+            (p.smoothing != 0 ? p.smoothing * (fmax(z, 0.0) + log) : 0);
         dl = p.beta * (p.smoothing - (z > 0 ? u * y : y));
       } else if (p.kind == 1) {
         l = z < 1 ? 1 - z : z != z ? z : 0;

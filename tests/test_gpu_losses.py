@@ -1139,3 +1139,16 @@ def test_policy_terms_with_a_coefficient_of_zero(T, kl):
     assert torch.isfinite(plain).all() and torch.equal(w, w0)
     assert torch.equal(out[[0, 1, 4, 5]], plain[[0, 1, 4, 5]]) and out[2:4].isnan().all()       # the reports say what there is
     assert torch.equal(g, g0) and not h.any()
+
+
+def test_preference_of_a_smoothing_of_one():
+    """Only the other label's term counts: 0 where the difference is -infinity."""
+    M = _M()
+    logp = torch.tensor([[-math.inf, -1.0], [-1.0, -1.0], [-1.0, -2.0], [-1.5, -2.0]], device="cuda")
+    cfg = M.moara_preference_default_config(beta=0.5, smoothing=1.0)
+    out, rewards, slope = M.moara_preference_loss(cfg, logp)
+    z = 0.5 * 0.5
+    assert float(out[0]) == pytest.approx(math.log1p(math.exp(z)) / 2, rel=4 * U)
+    grad = M.moara_preference_loss_backward(cfg, logp, slope, torch.ones(1, device="cuda"))
+    s = 0.5 / (1 + math.exp(-z)) / 2
+    np.testing.assert_allclose(_np(grad), [[0, 0], [0, 0], [s, s], [-s, -s]], rtol=8 * U)
