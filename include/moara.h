@@ -490,7 +490,8 @@ int moara_route_balance(int32_t experts, int64_t* counts, float* bias, float rat
  * parts (tokens is a multiple of sequences). mask (tokens bytes, or null): a token with 0 is
  * left out, as are tokens before the first and behind the last sequence: whatever values they
  * have, they add nothing, and their gradients are 0. What is outside [0, tokens) is never read
- * or written, whatever the offsets are; offsets that fall give sums of some of the tokens.
+ * or written, whatever the offsets are; offsets that fall give sums of some of the tokens, and
+ * gradients that for some tokens are not written, or another sequence's.
  * Without tokens (tokens 0) the inputs, the sequences' advantages among them, may be null.
  * out_loss: one float, or null: the loss, out[0], once more, for callers that keep it by itself.
  * ------------------------------------------------------------------------------------ */

@@ -106,13 +106,15 @@ template <int N, int W> struct CellSums {
   double sum[W][N];
   int64_t seq[W];
 };
-// What the workgroup's cells, from cell i0 on, leave: at the first cell of each sequence the sum of its cells among them.
+// What the workgroup's cells, from cell i0 on, leave: at the first cell of each sequence the sum of its cells among them, at the
+// others 0, which only offsets that fall lead to.
 template <int N, int W> __device__ __forceinline__ void leave(const CellSums<N, W>& s, int64_t i0, int64_t cells, double* sums) {
   __syncthreads();
   const int w = threadIdx.x / N, k = threadIdx.x % N;
-  if (w >= W || i0 + w >= cells || (w > 0 && s.seq[w] == s.seq[w - 1])) return;
+  if (w >= W || i0 + w >= cells) return;
   double x = 0;
-  for (int v = w; v < W && i0 + v < cells && s.seq[v] == s.seq[w]; ++v) x += s.sum[v][k];
+  if (w == 0 || s.seq[w] != s.seq[w - 1])
+    for (int v = w; v < W && i0 + v < cells && s.seq[v] == s.seq[w]; ++v) x += s.sum[v][k];
   sums[(i0 + w) * N + k] = x;
 }
 // Adds up the sums of K sequences, of cells [first, last), by `lanes` lanes: those at its first cell and at each workgroup's

@@ -1152,3 +1152,29 @@ def test_preference_of_a_smoothing_of_one():
     grad = M.moara_preference_loss_backward(cfg, logp, slope, torch.ones(1, device="cuda"))
     s = 0.5 / (1 + math.exp(-z)) / 2
     np.testing.assert_allclose(_np(grad), [[0, 0], [0, 0], [s, s], [-s, -s]], rtol=8 * U)
+
+
+@pytest.mark.parametrize("T,S", [(1000, 4), (3000, 64), (100000, 300), (100000, 4)])
+@pytest.mark.parametrize("seed", range(3))
+def test_falling_offsets_give_the_same_sums_each_time(T, S, seed):
+    """Whatever the workspace held: sums of tokens, the same bits each time."""
+    import ctypes
+    M = _M()
+    r = rng(43, seed, T, S)
+    offsets = _gpu(r.integers(-5, T + 5, S + 1))
+    logp = _gpu(-r.exponential(size=T), F32)
+    pre, pol = M.moara_preference_default_config(kind=M.MOARA_PREF_SQUARE, beta=1.0), M.moara_policy_default_config()
+    found = []
+    for fill in (0.0, math.nan, 1e300):
+        work = torch.full((6 * (S + T // 512 + 130),), fill, dtype=torch.float64, device="cuda")
+        out, rewards, slope, about, weight = (torch.full((n,), 5.0, device="cuda") for n in (3, S, S + 1, 6, S + 1))
+        assert M.lib().moara_preference_loss(ctypes.byref(pre), logp.data_ptr(), None, None, T, offsets.data_ptr(), S, out.data_ptr(), None,
+                                             rewards.data_ptr(), slope.data_ptr(), work.data_ptr(), None) == M.MOARA_OK
+        work.fill_(fill)
+        assert M.lib().moara_policy_loss(ctypes.byref(pol), logp.data_ptr(), None, None, None, logp.data_ptr(), None, T, offsets.data_ptr(),
+                                         S, about.data_ptr(), None, weight.data_ptr(), work.data_ptr(), None) == M.MOARA_OK
+        torch.cuda.synchronize()
+        found.append(torch.cat([out, rewards, slope, about, weight]))
+        total = float(logp.double().sum())
+        assert torch.isfinite(found[-1]).all() and (rewards <= 0).all() and (rewards >= total * S).all()
+    assert torch.equal(found[0], found[1]) and torch.equal(found[0], found[2])
