@@ -527,7 +527,7 @@ int moara_token_logps_backward(const void* logits, int32_t logits_dtype, int64_t
 /* Bytes of the workspace of moara_preference_loss and moara_policy_loss: device memory, 8-byte
  * aligned, of any contents, for one call at a time. 0 for a few tokens: it may be null. */
 #define MOARA_LOSS_WORKSPACE(tokens, sequences) \
-  ((sequences) + ((tokens) + 255) / 256 <= 17 ? 0 : 48 * ((sequences) + (tokens) / 512 + 130))
+  ((sequences) + ((int64_t)(tokens) + 255) / 256 <= 17 ? 0 : 48 * ((sequences) + (int64_t)(tokens) / 512 + 130))
 
 enum { MOARA_PREF_SIGMOID = 0, MOARA_PREF_HINGE = 1, MOARA_PREF_SQUARE = 2 };
 
@@ -622,7 +622,8 @@ int moara_balance_default_config(moara_balance_config* out);
 
 /* Bytes of the workspace of moara_balance_loss: device memory, 8-byte aligned, of any contents, for
  * one call at a time. */
-#define MOARA_BALANCE_WORKSPACE(experts, tokens, sequences) ((8 * (experts) + 64) * (2 * (sequences) + (tokens) / 32 + 2))
+#define MOARA_BALANCE_WORKSPACE(experts, tokens, sequences) \
+  ((8 * (int64_t)(experts) + 64) * (2 * (int64_t)(sequences) + (tokens) / 32 + 2))
 
 /* Load-balancing loss of routed tokens. For each sequence with tokens, c_e the number of its tokens that
  * index gives to expert e, f_e = E c_e / sum_e c_e (0 where nothing is given), P_e the mean of its tokens'

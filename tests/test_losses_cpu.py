@@ -515,3 +515,26 @@ def test_vectors_are_accessed_with_the_alignment_they_are_declared_with(source):
     r = subprocess.run([hipcc, *build._flags(), "-Werror=align-mismatch", "--cuda-device-only", "-fsyntax-only",
                         os.path.join(build.CSRC, source)], capture_output=True, text=True)
     assert r.returncode == 0, r.stderr[-2000:]
+
+
+# ---------------------------------------------------------------- workspace sizes
+
+def test_workspaces_of_sizes_given_as_int(tmp_path):
+    """The header's macros count in 64 bits whatever type a C program's sizes have, and as the binding does."""
+    import shutil
+    import subprocess
+    from tests.conftest import ROOT
+    gcc = shutil.which("gcc")
+    if not gcc:
+        pytest.skip("no C compiler")
+    sizes = [(8, 0, 1), (64, 16384, 1), (256, 32768, 16), (1024, 1 << 24, 4), (64, 2 ** 31 - 1, 2), (1024, 2 ** 31 - 1, 1 << 21)]
+    lines = "".join(f"  {{ int e = {e}, t = {t}, s = {s}; printf(\"%lld %lld\\n\", (long long)MOARA_BALANCE_WORKSPACE(e, t, s), "
+                    f"(long long)MOARA_LOSS_WORKSPACE(t, s)); }}\n" for e, t, s in sizes)
+    src = tmp_path / "sizes.c"
+    src.write_text("#include <stdio.h>\n#include \"moara.h\"\nint main(void) {\n" + lines + "  return 0;\n}\n")
+    subprocess.run([gcc, "-I", os.path.join(ROOT, "include"), str(src), "-o", str(tmp_path / "sizes")], check=True, capture_output=True)
+    got = subprocess.run([str(tmp_path / "sizes")], check=True, capture_output=True, text=True).stdout.split()
+    want = []
+    for e, t, s in sizes:
+        want += [(8 * e + 64) * (2 * s + t // 32 + 2), 0 if s + (t + 255) // 256 <= 17 else 48 * (s + t // 512 + 130)]
+    assert [int(x) for x in got] == want
