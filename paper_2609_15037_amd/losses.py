@@ -9,10 +9,11 @@ of paired responses and of a clipped policy over them, and the load-balancing lo
     cfg = M.moara_policy_default_config(kl_coef=0.04, entropy_coef=0.01, sequence_advantages=1)
     loss, about = policy_loss(cfg, logp, advantages, old_logp=old, ref_logp=ref, entropy=entropy, mask=mask)
 
-Sequences are rows, or packed one after another with their offsets (int64, sequences + 1). Losses are scalars on the
-GPU; nothing is copied to the host, and a step can be captured into a graph, its backward pass too. As with any torch
-operator, first drop what was computed eagerly from the same parameters (losses of warm-up steps that are still held): their
-gradients' accumulation belongs to the stream of that time, which a capture cannot wait for.
+Sequences are rows, or packed one after another with their offsets (sequences + 1 integers). A mask is bool or integers, of
+any layout (`mask[:, 1:]` beside `logits[:, :-1]`); a token with 0 is left out. Losses are scalars on the GPU; nothing is
+copied to the host, and a step can be captured into a graph, its backward pass too. As with any torch operator, first drop
+what was computed eagerly from the same parameters (losses of warm-up steps that are still held): their gradients'
+accumulation belongs to the stream of that time, which a capture cannot wait for.
 Gradients of the gradients are refused.
 """
 from __future__ import annotations
@@ -32,6 +33,23 @@ def _plain(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
 
 def _rows(t: torch.Tensor) -> torch.Tensor:
     return t if t.dtype is torch.float32 and t.is_contiguous() else t.float().contiguous()
+
+
+def _mask(mask: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
+    """A mask as the library takes it: contiguous, bool or uint8. Integers are live where they are not 0; of floating point 0
+    could as well be what is added to a live token's score."""
+    if mask is None or (mask.dtype in (torch.bool, torch.uint8) and mask.is_contiguous()):
+        return mask
+    if mask.is_floating_point() or mask.is_complex():
+        raise ValueError(f"mask: need bool or integers, got {mask.dtype}")
+    return (mask if mask.dtype is torch.bool else mask.ne(0)).contiguous()
+
+
+def _offsets(offsets: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
+    """Offsets as the library takes them: contiguous, int64."""
+    if offsets is None or offsets.is_floating_point():      # these the library refuses
+        return offsets
+    return offsets.to(torch.int64).contiguous()
 
 
 class _Last(torch.autograd.Function):
@@ -125,7 +143,7 @@ def preference_loss(cfg: M.moara_preference_config, logp: torch.Tensor, ref_logp
     """(loss, rewards, about) of pairs of responses, sequences 2p (chosen) and 2p + 1 (rejected); differentiable in logp.
     rewards: one for each sequence; about: loss, share of the pairs with the chosen one ahead, mean difference of their
     rewards. logp, ref_logp, mask: sequences x length, or flat with offsets."""
-    return _Preference.apply(_rows(logp), cfg, _plain(ref_logp), offsets, mask)
+    return _Preference.apply(_rows(logp), cfg, _plain(ref_logp), _offsets(offsets), _mask(mask))
 
 
 class _Policy(torch.autograd.Function):
@@ -160,7 +178,7 @@ def policy_loss(cfg: M.moara_policy_config, logp: torch.Tensor, advantages: torc
     that sampled), ref_logp, entropy, mask: sequences x length, or flat with offsets; advantages alike, or one for each
     sequence where cfg.sequence_advantages."""
     return _Policy.apply(_rows(logp), None if entropy is None else _rows(entropy), cfg, _plain(advantages), _plain(old_logp),
-                         _plain(ref_logp), offsets, mask)
+                         _plain(ref_logp), _offsets(offsets), _mask(mask))
 
 
 class _Balance(torch.autograd.Function):
@@ -191,4 +209,4 @@ def balance_loss(cfg: M.moara_balance_config, logits: torch.Tensor, index: torch
     counts: each expert's tokens by sequence (int64); about: loss, mean balance, z. Each of the packed (offsets) or equal
     (`sequences`) sequences is balanced for itself; without either all tokens together. load: counts that take the
     place of this call's, e.g. those of all ranks."""
-    return _Balance.apply(logits, cfg, index, offsets, mask, load, sequences)
+    return _Balance.apply(logits, cfg, index, _offsets(offsets), _mask(mask), load, sequences)

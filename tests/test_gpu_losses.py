@@ -1178,3 +1178,22 @@ def test_falling_offsets_give_the_same_sums_each_time(T, S, seed):
         total = float(logp.double().sum())
         assert torch.isfinite(found[-1]).all() and (rewards <= 0).all() and (rewards >= total * S).all()
     assert torch.equal(found[0], found[1]) and torch.equal(found[0], found[2])
+
+
+@pytest.mark.parametrize("kind", [torch.int64, torch.int32, torch.uint8, torch.bool])
+def test_losses_of_masks_beside_views(kind):
+    """A tokenizer's mask without its first position, and int32 offsets: as the library's own types, gradients too."""
+    M, L = _M(), _L()
+    r = rng(47)
+    whole = _gpu((r.random((6, 41)) < 0.7).astype(np.int64)).to(kind)
+    logp, ref, adv = (_gpu(-r.exponential(size=(6, 40)), F32) for _ in range(3))
+    pre, pol = M.moara_preference_default_config(), M.moara_policy_default_config()
+    o = _gpu(np.array([0, 40, 41, 90, 240]))
+    found = []
+    for mask, offsets in ((whole[:, 1:], o.int()), ((whole[:, 1:] != 0).contiguous(), o)):
+        x = logp.clone().requires_grad_()
+        flat = dict(offsets=offsets, mask=mask.reshape(-1))
+        losses = [L.preference_loss(pre, x, ref, mask=mask)[0], L.policy_loss(pol, x, adv, ref, mask=mask)[0],
+                  L.preference_loss(pre, x.view(-1), **flat)[0], L.policy_loss(pol, x.view(-1), adv.view(-1), **flat)[0]]
+        found.append([loss.detach() for loss in losses] + [torch.autograd.grad(loss, x)[0] for loss in losses])
+    assert all(torch.equal(a, b) and a.any() for a, b in zip(*found))

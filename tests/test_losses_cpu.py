@@ -538,3 +538,40 @@ def test_workspaces_of_sizes_given_as_int(tmp_path):
     for e, t, s in sizes:
         want += [(8 * e + 64) * (2 * s + t // 32 + 2), 0 if s + (t + 255) // 256 <= 17 else 48 * (s + t // 512 + 130)]
     assert [int(x) for x in got] == want
+
+
+# ---------------------------------------------------------------- masks and offsets of a training program
+
+def test_masks_and_offsets_of_other_types_and_layouts(calls):
+    """A mask beside `logits[:, :-1]` is `mask[:, 1:]`, often of integers, and offsets may be int32: the losses take them as they
+    take log-probabilities, forward and backward; ones that the library takes are passed on as they are."""
+    whole = torch.tensor([[1, 1, 0, 1, 1], [1, 0, 0, 1, 2]] * 2)
+    want = whole[:, 1:].ne(0)
+    x = torch.randn(4, 4, requires_grad=True)
+    pre, pol, adv = M.moara_preference_config(beta=0.1), M.moara_policy_config(), torch.ones(4, 4)
+    bal, index = M.moara_balance_config(experts=4, top_k=1), torch.zeros(4, 1, dtype=torch.int32)
+
+    def passed(call, key):
+        call.backward()
+        for _, a, kw in calls[-2:]:
+            yield kw[key]
+    for kind in (torch.int64, torch.int32, torch.uint8, torch.bool):
+        mask = (whole != 0 if kind == torch.bool else whole).to(kind)[:, 1:]
+        for loss in (L.preference_loss(pre, x, mask=mask)[0], L.policy_loss(pol, x, adv, mask=mask)[0]):
+            for m in passed(loss, "mask"):
+                assert m.is_contiguous() and m.dtype in (torch.bool, torch.uint8) and torch.equal(m != 0, want)
+        for m in passed(L.balance_loss(bal, x, index, mask=mask[:, 1])[0], "mask"):
+            assert m.is_contiguous() and m.dtype in (torch.bool, torch.uint8) and torch.equal(m != 0, want[:, 1])
+    for same in (want.contiguous(), want.to(torch.uint8)):
+        assert next(passed(L.preference_loss(pre, x, mask=same)[0], "mask")) is same
+    flat = torch.randn(16, requires_grad=True)
+    for o in (torch.tensor([0, 4, 16], dtype=torch.int32), torch.tensor([0, 1, 4, 1, 16])[::2]):
+        for loss in (L.preference_loss(pre, flat, offsets=o)[0], L.policy_loss(pol, flat, flat.detach(), offsets=o)[0],
+                     L.balance_loss(bal, x, index, offsets=o)[0]):
+            for got in passed(loss, "offsets"):
+                assert got.dtype == torch.int64 and got.is_contiguous() and torch.equal(got, o.long())
+    o = torch.tensor([0, 16])
+    assert next(passed(L.preference_loss(pre, flat, offsets=o)[0], "offsets")) is o
+    for mask in (torch.ones(4, 4), torch.zeros(4, 4, dtype=torch.bfloat16)):       # 1 and 0, or 0 and -infinity: not guessed
+        with pytest.raises(ValueError, match="mask"):
+            L.preference_loss(pre, x, mask=mask)
