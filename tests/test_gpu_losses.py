@@ -1197,3 +1197,76 @@ def test_losses_of_masks_beside_views(kind):
                   L.preference_loss(pre, x.view(-1), **flat)[0], L.policy_loss(pol, x.view(-1), adv.view(-1), **flat)[0]]
         found.append([loss.detach() for loss in losses] + [torch.autograd.grad(loss, x)[0] for loss in losses])
     assert all(torch.equal(a, b) and a.any() for a, b in zip(*found))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("MiB", [200, 340])
+@pytest.mark.parametrize("gap", [0, 3])
+def test_logps_past_the_caches(dtype, MiB, gap):
+    """Sizes whose gradients, and whose logits too, are read and written past the caches, and the vocabularies that narrow and
+    wide rows take; a few rows with a label, all others' gradients 0 and as many as there are."""
+    M = _M()
+    for V in (300, 3001, 40000):
+        T = (MiB << 20) // (V * (4 if dtype == F32 else 2))
+        x = torch.zeros(T, V + gap, dtype=dtype, device="cuda")[:, :V]
+        rows = torch.tensor([0, 1, T // 2, T - 1], device="cuda")
+        small, lab_small, g_small, h_small = _case(V, 4, V, dtype)
+        lab_small[2:] = torch.tensor([V // 2, V - 1], device="cuda")
+        x[rows] = small
+        lab, g, h = torch.full((T,), -100, device="cuda"), torch.ones(T, device="cuda"), torch.ones(T, device="cuda")
+        lab[rows], g[rows], h[rows] = lab_small, g_small + 0.5, h_small - 0.5
+        X, labels, gn, hn = _np(small), _np(lab_small), _np(g[rows]), _np(h[rows])
+        want, wantH = O.token_logps(X, labels)
+        tol, tolH, _ = _logps_tol(X, labels, 1.0)       # as few rows add up: on 16, 64 and at least 256 lanes
+        for entropy in (False, True):
+            logp, H, stats = M.moara_token_logps(x, lab, entropy=entropy)
+            _close(_np(logp[rows]), want, tol, "logp")
+            assert int(logp.count_nonzero()) <= 4
+            if entropy:
+                _close(_np(H[rows]), wantH, tolH, "entropy")
+                assert int(H.count_nonzero()) <= 4
+            grad = M.moara_token_logps_backward(x, lab, stats, g, entropy=H, grad_entropy=h if entropy else None)
+            ref = O.token_logps_grad(X, labels, gn, hn if entropy else None)
+            _close(_np(grad[rows]), ref, _grad_tol(X, labels, gn, hn if entropy else None, 1.0, ref, dtype), "gradient")
+            grad[rows] = 0
+            assert not grad.any()
+
+
+@pytest.mark.parametrize("E,T,S", [(256, 40000, 1), (1000, 9000, 1), (256, 70000, 2)])
+def test_balance_of_many_cells_with_another_load(E, T, S):
+    """Cells that are added up by columns first, with counts given for f: this call's counts stay its own."""
+    M = _M()
+    r, seqs, x, index, kw = _balance_case(53, T, E, 4, S, None, "random", F32)
+    load = r.integers(0, 900, E)
+    cfg = M.moara_balance_default_config(experts=E, top_k=4, z_coef=1e-3)
+    kw = dict(mask=kw["mask"], sequences=S)
+    out, counts, slope = M.moara_balance_loss(cfg, x, _gpu(index), load=_gpu(load), **kw)
+    grad = M.moara_balance_loss_backward(cfg, x, slope, torch.ones((), device="cuda"), **kw)
+    X, spec = _np(x), dict(z_coef=1e-3)
+    w_out, w_counts, w_grad = O.balance(X, index, seqs, False, load=load, **spec)
+    t_out, t_grad = _balance_tol(X, index, seqs, False, {**spec, "load": load}, F32, w_grad)
+    _close(_np(out), w_out, t_out + 2 * U * np.abs(w_out), "out")
+    assert np.array_equal(_np(counts), w_counts)
+    _close(_np(grad), w_grad, t_grad, "gradient")
+
+
+def test_losses_from_two_threads_all_return():
+    """As test_losses_from_two_threads_at_once, counting the calls that came back: an error in a thread fails too."""
+    inputs = [_policy_inputs(T=4000, V=700), _policy_inputs(T=300, V=9000, dtype=F32)]
+    want = [_every_call(*a) for a in inputs]
+    torch.cuda.synchronize()
+    same = [0, 0]
+
+    def work(i):
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            for _ in range(10):
+                got = _every_call(*inputs[i])
+                s.synchronize()
+                same[i] += all(torch.equal(a, b) for a, b in zip(got, want[i]))
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert same == [10, 10]
