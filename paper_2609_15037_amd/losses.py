@@ -47,8 +47,8 @@ def _mask(mask: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
 
 def _offsets(offsets: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
     """Offsets as the library takes them: contiguous, int64."""
-    if offsets is None or offsets.is_floating_point():      # these the library refuses
-        return offsets
+    if offsets is None or (offsets.dtype is torch.int64 and offsets.is_contiguous()) or offsets.is_floating_point():
+        return offsets          # the library refuses the last
     return offsets.to(torch.int64).contiguous()
 
 
