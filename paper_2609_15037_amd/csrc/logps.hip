@@ -79,8 +79,9 @@ template <int LANES, bool ENTROPY> __device__ __forceinline__ Part together(cons
 // the probability: log p = a - log1p(sum + (e_label - 1)) with a = scale (x_label - top) keeps its relative accuracy.
 // A lane's sum is fp32, rescaled when its maximum grows (once for U vectors), the lanes' are joined in 64 bits. Of its last
 // turn a wave skips the vectors that it has nothing of (2039 x 50021 fp32 on 512 threads 75 us with them, 67 without). Bound
-// by reads: 4096 x 131072 bf16 in 167 us, 6.4 TB/s; 2039 x 50021 fp32 with entropies, rows 50048 apart, 60 us, 6.8 TB/s; 8 x
-// 32000 4.7 us, a launch and the latencies of a row. One vector more in flight for each lane, a fetch ahead of the next turn,
+// by reads; with a label in every row, two sets of logits in turn: 4096 x 131072 bf16 1.07 GB in 163 us, 6.6 TB/s, with entropies
+// 191, 5.6; fp32 2.1 GB in 340 us, 6.3 TB/s; 2039 x 50021 fp32 with entropies, rows 50048 apart, 408 MB in 76 us, 5.4 TB/s (a tenth
+// without a label: 58). 8 x 32000 4.7 us, a launch and the latencies of a row. One vector more in flight for each lane, a fetch ahead of the next turn,
 // or registers held down for more waves (64: 120 us instead of 96 at 8192 x 32000) gained nothing.
 template <typename T, int THREADS, int U, bool ENTROPY, bool ONCE>
 __global__ __launch_bounds__(THREADS <= 64 ? 256 : THREADS) void k_logps(LogpsParams p) {
@@ -184,8 +185,9 @@ __global__ __launch_bounds__(THREADS <= 64 ? 256 : THREADS) void k_logps(LogpsPa
 
 // 2^((x - top) k - log2 sum) is p; GROUP threads take U vectors a lane of a row. The label's own value has 1 - p and
 // log p from the forward pass: no difference of values near 1. Parts of rows, not rows, so that a large vocabulary's few rows
-// fill the GPU. The gradient is rounded once, to its type. Bound by memory: 4096 x 131072 bf16 in 320 us, 2.1 GB at 6.7 TB/s;
-// 2039 x 50021 fp32 with entropies 139 us, 5.9 TB/s.
+// fill the GPU. The gradient is rounded once, to its type. Bound by memory; every row with a label and a gradient: 4096 x 131072
+// bf16 2.15 GB in 345 us, 6.2 TB/s, with entropies 359, 6.0; fp32 4.3 GB in 734, 5.9; 2039 x 50021 fp32 with entropies 816 MB in
+// 150 us, 5.4 TB/s.
 template <typename T, int GROUP, bool ENTROPY, bool ONCE_IN, bool ONCE_OUT>
 __global__ __launch_bounds__(256) void k_logps_backward(LogpsParams p, uint32_t parts) {
   constexpr int N = 16 / sizeof(T), U = 4, SPAN = GROUP * N * U, GROUPS = 256 / GROUP;

@@ -5,7 +5,8 @@
 // launch: 4 pairs of 1000 tokens 7.7 us, of which half is the chain of a search, a load, two sums over the workgroup and the
 // loss itself. Their gradients are one launch, a wave for each cell.
 // Tiles of 512 tokens: of 256, twice the sums to be gathered in the last step; of 1024, too few waves, both slower at 2 M
-// tokens; up to 65536 tokens 256, for the waves. Times below are of 2 M tokens in 2048 (pairs) and 1024 (policy) sequences.
+// tokens; up to 65536 tokens 256, for the waves. Times below are of 2 M tokens in 2048 (pairs) and 1024 (policy) sequences, in a
+// captured graph of many such calls; in a trace of whole steps a kernel takes up to 1.5 us more.
 #include "packed.h"
 
 namespace {
@@ -284,8 +285,10 @@ __global__ __launch_bounds__(END_THREADS) void k_preference_small(PreferencePara
   preference_end<ONE, FEW>(p, sums);
 }
 
-// A token's gradient is its sequence's slope: written once, nothing but the mask is read for it. 8 us: the search's latencies
-// over 1.2 sets of waves; its 10 MB alone would take 2.
+// A token's gradient is its sequence's slope: written once, nothing but the mask is read for it. 8.0 us where its 10 MB alone
+// would take 2: with two sequences of equal rows it takes 5.8 (a launch, then search, mask and store one after another, once for
+// each wave), with 2048 of them 7.0 (a round of the search more), with offsets of the same rows 7.7 (their loads), of uneven
+// ones 8.0.
 __global__ __launch_bounds__(256) void k_preference_backward(Packed q, const float* __restrict__ slope,
                                                              const float* __restrict__ grad_loss, float* __restrict__ grad,
                                                              int64_t cells) {
@@ -448,7 +451,7 @@ template <int SHIFT, int W> __device__ __forceinline__ void policy_end(const Pol
   }
 }
 
-// 15.5 us for 42 MB, 2.7 TB/s: all waves are resident, and their phases follow one another: the search, the loads, some 80
+// 15.5 us for 42 MB, 2.7 TB/s: all waves are resident, and their phases follow one another: the search, the loads, some 100
 // vector instructions a token, the sums; of its 10 us a wave waits 6.4 for memory and the workgroup. A kernel for each kind of
 // distance: as branches of each token, though alike for all, 16.2 (backward 13.4 for 12.3).
 template <int SHIFT, int KL> __global__ __launch_bounds__(64 * GROUP) void k_policy_cells(PolicyParams p, int64_t cells) {
